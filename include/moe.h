@@ -232,6 +232,50 @@ moe_status moe_forward_staged(const moe_config* cfg, const void* x, const void* 
                               void* y, void* workspace, size_t ws_bytes, void* stream,
                               void* const* events, int32_t n_events);
 
+/* ---- Training ---------------------------------------------------------------------------
+ * The gated feed-forward block with what its backward pass needs, that backward pass, and the gradient
+ * of the combine.  Rows are expert-contiguous as moe_permute leaves them; E = k = 1 with offsets {0, T}
+ * is a dense block (or the expert that all tokens share).  Weights are the row-major tensors, which a training
+ * program changes with every step.  A layer's step:
+ *   moe_route, moe_permute, moe_grouped_ffn_train, moe_combine;
+ *   moe_combine_backward, moe_grouped_ffn_backward; dx of a token = the sum of its k rows of dx_perm:
+ *   moe_combine(dx_perm, row_of, weights of 1).  d_topk_w is what the router's gradient starts from.
+ * offsets are trusted as in moe_grouped_ffn: ascending, offsets[E] <= R.  Rows from offsets[E] on are
+ * not written.  Where T == 0 the tensors of rows may be NULL.
+ * Beyond the limits above: d, F <= 2^20, else MOE_ERR_UNSUPPORTED.  No atomics: results are bit-reproducible. */
+
+/* moe_grouped_ffn that keeps the two projections: g = x W_gate^T, u = x W_up^T [R,F] bf16 (rounded once from fp32),
+ * h [R,F] = SiLU(g) (.) u from the fp32 values, y_perm [R,d] = h W_down^T.  h is not needed by the backward pass.
+ * workspace: moe_ffn_workspace_size(cfg) bytes. */
+moe_status moe_grouped_ffn_train(const moe_config* cfg, const void* x_perm, const int32_t* offsets,
+                                 const void* W_gate, const void* W_up, const void* W_down,
+                                 void* g, void* u, void* h, void* y_perm, void* workspace, size_t ws_bytes, void* stream);
+
+/* flags of moe_grouped_ffn_backward */
+#define MOE_GRAD_F32 1         /* dW_gate, dW_up, dW_down are fp32 tensors (else bf16) */
+#define MOE_GRAD_ACCUMULATE 2  /* they are added to what the tensors hold (in fp32, one rounding), else written */
+
+/* Gradients of moe_grouped_ffn_train at the kept g and u:
+ *   dh = dy_perm W_down;  dg = dh (.) u (.) SiLU'(g),  du = dh (.) SiLU(g)
+ *   dx_perm [R,d] = dg W_gate + du W_up
+ *   dW_gate, dW_up [E,F,d] = dg^T x, du^T x;  dW_down [E,d,F] = dy^T h, over each expert's rows
+ * dg, du and h = SiLU(g) (.) u (formed again) are rounded to bf16, the operands of the products that follow; all sums are fp32.
+ * dx_perm and each dW may be NULL: it is then not computed.  An expert without rows (and T == 0) has weight
+ * gradients of zero, which are written unless MOE_GRAD_ACCUMULATE is set.  Outputs must not overlap inputs.
+ * workspace: moe_ffn_backward_workspace_size(cfg) bytes (dg, du, h: 6*R*F), 256-byte aligned. */
+size_t moe_ffn_backward_workspace_size(const moe_config* cfg);
+moe_status moe_grouped_ffn_backward(const moe_config* cfg, const void* x_perm, const int32_t* offsets,
+                                    const void* W_gate, const void* W_up, const void* W_down,
+                                    const void* g, const void* u, const void* dy_perm,
+                                    void* dx_perm, void* dW_gate, void* dW_up, void* dW_down, int32_t flags,
+                                    void* workspace, size_t ws_bytes, void* stream);
+
+/* Gradients of moe_combine:  dy_perm[row_of[t*k+i],:] = topk_w[t,i] * dy[t,:] (one rounding to bf16),
+ * d_topk_w[t,i] = <dy[t,:], y_perm[row_of[t*k+i],:]> (fp32).  row_of: moe_permute's (every row once).
+ * dy_perm may be y_perm itself. */
+moe_status moe_combine_backward(const moe_config* cfg, const void* dy, const void* y_perm, const int32_t* row_of,
+                                const float* topk_w, void* dy_perm, float* d_topk_w, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

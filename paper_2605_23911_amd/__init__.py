@@ -6,6 +6,8 @@ the built library raises.
 """
 from .binding import (  # noqa: F401
     FLAG_FUSE_COMBINE,
+    GRAD_ACCUMULATE,
+    GRAD_F32,
     GATE_SIGMOID_NORM,
     GATE_SOFTMAX,
     GATE_SOFTMAX_RENORM,
@@ -14,6 +16,7 @@ from .binding import (  # noqa: F401
     WorkspaceLayout,
     forward_workspace_layout,
     forward_workspace_size,
+    ffn_backward_workspace_size,
     ffn_kernel_name,
     ffn_workspace_size,
     lib,
@@ -21,9 +24,12 @@ from .binding import (  # noqa: F401
     max_blocks,
     moe_block_schedule,
     moe_combine,
+    moe_combine_backward,
     moe_forward,
     moe_forward_staged,
     moe_grouped_ffn,
+    moe_grouped_ffn_backward,
+    moe_grouped_ffn_train,
     moe_pack_weights,
     packed_weights_size,
     moe_permute,

@@ -14,6 +14,8 @@ GATE_SOFTMAX = 0
 GATE_SOFTMAX_RENORM = 1
 GATE_SIGMOID_NORM = 2
 FLAG_FUSE_COMBINE = 1
+GRAD_F32 = 1
+GRAD_ACCUMULATE = 2
 
 _LIB_NAME = "libmoe_mi355x.so"
 _lib = None
@@ -22,6 +24,7 @@ EXPORTS = (
     "moe_status_string", "moe_tile_m", "moe_route_workspace_size", "moe_permute_workspace_size", "moe_ffn_workspace_size",
     "moe_forward_workspace_size", "moe_workspace_size", "moe_forward_workspace_layout", "moe_max_blocks", "moe_route",
     "moe_permute", "moe_permute_static", "moe_block_schedule", "moe_grouped_ffn", "moe_combine", "moe_forward", "moe_forward_staged", "moe_packed_weights_size", "moe_pack_weights", "moe_ffn_kernel_name",
+    "moe_grouped_ffn_train", "moe_ffn_backward_workspace_size", "moe_grouped_ffn_backward", "moe_combine_backward",
 )
 
 
@@ -70,7 +73,7 @@ def lib() -> C.CDLL:
     L.moe_max_blocks.restype = C.c_int32
     L.moe_max_blocks.argtypes = [cfgp, C.c_int32]
     for n in ("moe_route_workspace_size", "moe_permute_workspace_size", "moe_ffn_workspace_size", "moe_forward_workspace_size",
-              "moe_workspace_size", "moe_packed_weights_size"):
+              "moe_workspace_size", "moe_packed_weights_size", "moe_ffn_backward_workspace_size"):
         getattr(L, n).restype = C.c_size_t
         getattr(L, n).argtypes = [cfgp]
     L.moe_forward_workspace_layout.restype = C.c_int
@@ -94,6 +97,12 @@ def lib() -> C.CDLL:
     L.moe_forward_staged.restype = C.c_int
     L.moe_forward_staged.argtypes = [cfgp, vp, vp, f32p, vp, vp, vp, vp, vp, vp, C.c_size_t, vp, C.POINTER(C.c_void_p),
                                      C.c_int32]
+    L.moe_grouped_ffn_train.restype = C.c_int
+    L.moe_grouped_ffn_train.argtypes = [cfgp, vp, i32p, vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    L.moe_grouped_ffn_backward.restype = C.c_int
+    L.moe_grouped_ffn_backward.argtypes = [cfgp, vp, i32p] + [vp] * 10 + [C.c_int32, vp, C.c_size_t, vp]
+    L.moe_combine_backward.restype = C.c_int
+    L.moe_combine_backward.argtypes = [cfgp, vp, vp, i32p, f32p, vp, f32p, vp]
     L.moe_test_knob.restype = C.c_int32       # test hook, not part of include/moe.h
     L.moe_test_knob.argtypes = [C.c_int32, C.c_int32]
     L.moe_test_map_launch.restype = C.c_int32  # test hook (host arithmetic only), not part of include/moe.h
@@ -255,3 +264,76 @@ def moe_forward_staged(cfg, x, W_r, bias, W_gate, W_up, W_down, y, workspace, ev
     _check(lib().moe_forward_staged(C.byref(cfg), _ptr(x), _ptr(W_r), _ptr(bias), _ptr(W_gate), _ptr(W_up),
                                     _ptr(W_down), _ptr(W_packed), _ptr(y), _ptr(workspace), _nbytes(workspace),
                                     _stream(stream), arr, n), "moe_forward_staged")
+
+
+# ---- training ------------------------------------------------------------------------------------------------------------
+
+
+class _Call:
+    """Arguments of one call of the training and adapter entry points: sizes and types are checked here (the C ABI sees addresses only), all
+    tensors have to be on one GPU, and the call runs with that GPU current, on `stream` or that GPU's current stream."""
+
+    def __init__(self, stream=None):
+        self.device, self.stream = None, stream
+
+    def __call__(self, name, t, shape, dtype, optional=False):
+        if t is None:
+            if optional:
+                return None
+            raise ValueError(f"{name} is required")
+        if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name} has to be {dtype} {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+        return self.raw(name, t)
+
+    def raw(self, name, t):
+        p = _ptr(t)
+        if self.device is None:
+            self.device = t.device
+        if t.device != self.device:
+            raise ValueError(f"{name} is on {t.device}, the other tensors on {self.device}")
+        return p
+
+    def run(self, where, fn, *args):
+        with torch.cuda.device(self.device):
+            s = self.stream if self.stream is not None else torch.cuda.current_stream()
+            if s.device != self.device:
+                raise ValueError(f"{where}: the stream is on {s.device}, the tensors on {self.device}")
+            _check(fn(*args, C.c_void_p(s.cuda_stream)), where)
+
+
+def ffn_backward_workspace_size(cfg) -> int:
+    return lib().moe_ffn_backward_workspace_size(C.byref(cfg))
+
+
+def moe_grouped_ffn_train(cfg, x_perm, offsets, W_gate, W_up, W_down, g, u, h, y_perm, workspace, stream=None):
+    """The gated block over expert-contiguous rows, keeping g = x W_gate^T and u = x W_up^T [R, F] for the backward pass."""
+    a, b, R = _Call(stream), torch.bfloat16, cfg.T * cfg.k
+    a.run("moe_grouped_ffn_train", lib().moe_grouped_ffn_train, C.byref(cfg), a("x_perm", x_perm, (R, cfg.d), b),
+          a("offsets", offsets, (cfg.E + 1,), torch.int32), a("W_gate", W_gate, (cfg.E, cfg.F, cfg.d), b), a("W_up", W_up, (cfg.E, cfg.F, cfg.d), b),
+          a("W_down", W_down, (cfg.E, cfg.d, cfg.F), b), a("g", g, (R, cfg.F), b), a("u", u, (R, cfg.F), b), a("h", h, (R, cfg.F), b),
+          a("y_perm", y_perm, (R, cfg.d), b), a.raw("workspace", workspace), _nbytes(workspace))
+
+
+def moe_grouped_ffn_backward(cfg, x_perm, offsets, W_gate, W_up, W_down, g, u, dy_perm, dx_perm, dW_gate, dW_up, dW_down, workspace,
+                             accumulate=False, stream=None):
+    """Gradients of moe_grouped_ffn_train.  dx_perm and each dW may be None (not computed).  The weight gradients' tensors are all bf16 or all
+    fp32; accumulate: added to what they hold."""
+    a, b, R = _Call(stream), torch.bfloat16, cfg.T * cfg.k
+    f32 = any(t is not None and t.dtype == torch.float32 for t in (dW_gate, dW_up, dW_down))
+    w = torch.float32 if f32 else b
+    a.run("moe_grouped_ffn_backward", lib().moe_grouped_ffn_backward, C.byref(cfg), a("x_perm", x_perm, (R, cfg.d), b),
+          a("offsets", offsets, (cfg.E + 1,), torch.int32), a("W_gate", W_gate, (cfg.E, cfg.F, cfg.d), b), a("W_up", W_up, (cfg.E, cfg.F, cfg.d), b),
+          a("W_down", W_down, (cfg.E, cfg.d, cfg.F), b), a("g", g, (R, cfg.F), b), a("u", u, (R, cfg.F), b), a("dy_perm", dy_perm, (R, cfg.d), b),
+          a("dx_perm", dx_perm, (R, cfg.d), b, True), a("dW_gate", dW_gate, (cfg.E, cfg.F, cfg.d), w, True), a("dW_up", dW_up, (cfg.E, cfg.F, cfg.d), w, True),
+          a("dW_down", dW_down, (cfg.E, cfg.d, cfg.F), w, True), (GRAD_F32 if f32 else 0) | (GRAD_ACCUMULATE if accumulate else 0),
+          a.raw("workspace", workspace), _nbytes(workspace))
+
+
+def moe_combine_backward(cfg, dy, y_perm, row_of, topk_w, dy_perm, d_topk_w, stream=None):
+    """Gradients of moe_combine: of the rows and of the gate weights (fp32)."""
+    a, b, T, k, d = _Call(stream), torch.bfloat16, cfg.T, cfg.k, cfg.d
+    if row_of is not None and row_of.dim() == 1:
+        row_of = row_of.view(T, k) if row_of.numel() == T * k else row_of
+    a.run("moe_combine_backward", lib().moe_combine_backward, C.byref(cfg), a("dy", dy, (T, d), b), a("y_perm", y_perm, (T * k, d), b),
+          a("row_of", row_of, (T, k), torch.int32), a("topk_w", topk_w, (T, k), torch.float32), a("dy_perm", dy_perm, (T * k, d), b),
+          a("d_topk_w", d_topk_w, (T, k), torch.float32))

@@ -55,6 +55,14 @@ size_t hist_bytes(const moe_config* c) {
     return align_up(n ? n : 1);
 }
 
+// The training and adapter kernels hold a tile's rows as 32-bit byte offsets: 256 rows of 2^20 elements.
+constexpr int kMaxWidth = 1 << 20;
+moe_status check_train(const moe_config* c) {
+    const moe_status st = check_config(c);
+    if (st != MOE_OK) return st;
+    return c->d > kMaxWidth || c->F > kMaxWidth ? MOE_ERR_UNSUPPORTED : MOE_OK;
+}
+
 moe_status hip_status(hipError_t e) { return e == hipSuccess ? MOE_OK : MOE_ERR_HIP; }
 
 
@@ -350,6 +358,68 @@ moe_status moe_forward(const moe_config* c, const void* x, const void* W_r, cons
                        size_t ws_bytes, void* stream) {
     return moe_forward_staged(c, x, W_r, bias, W_gate, W_up, W_down, W_packed, y, workspace, ws_bytes, stream,
                               nullptr, 0);
+}
+
+moe_status moe_grouped_ffn_train(const moe_config* c, const void* x_perm, const int32_t* offsets, const void* W_gate, const void* W_up,
+                                 const void* W_down, void* g, void* u, void* h, void* y_perm, void* workspace, size_t ws_bytes, void* stream) {
+    const moe_status st = check_train(c);
+    if (st != MOE_OK) return st;
+    if (!offsets || !W_gate || !W_up || !W_down || !workspace) return MOE_ERR_NULL;
+    if (c->T > 0 && (!x_perm || !g || !u || !h || !y_perm)) return MOE_ERR_NULL;
+    for (const void* p : {x_perm, W_gate, W_up, W_down, (const void*)g, (const void*)u, (const void*)h, (const void*)y_perm, (const void*)workspace})
+        if (misaligned(p)) return MOE_ERR_ALIGN;
+    if (ws_bytes < moe_ffn_workspace_size(c)) return MOE_ERR_WORKSPACE;
+    if (c->T == 0) return MOE_OK;
+    hipStream_t s = (hipStream_t)stream;
+    const int M = moe_tile_m(c);
+    int32_t* blocks = (int32_t*)workspace;
+    int32_t* blocks_mix = (int32_t*)((char*)workspace + list_bytes(c, M));
+    int32_t* num_blocks = (int32_t*)((char*)workspace + schedule_bytes(c, M) - kAlign);
+    hipError_t e = launch_block_schedule(*c, offsets, M, blocks, num_blocks, blocks_mix, num_blocks + 1, s);
+    if (e == hipSuccess)
+        e = launch_gated_keep(*c, (const uint16_t*)x_perm, offsets, (const uint16_t*)W_gate, (const uint16_t*)W_up, (uint16_t*)g, (uint16_t*)u,
+                              (uint16_t*)h, s);
+    if (e == hipSuccess)
+        e = launch_down(*c, M, (const uint16_t*)h, c->F, offsets, blocks, num_blocks, blocks_mix, num_blocks + 1, (const uint16_t*)W_down, nullptr,
+                        (uint16_t*)y_perm, nullptr, s);
+    return hip_status(e);
+}
+
+size_t moe_ffn_backward_workspace_size(const moe_config* c) {
+    if (check_train(c) != MOE_OK) return 0;
+    const size_t rows = align_up((size_t)c->T * c->k * c->F * sizeof(uint16_t));
+    return rows ? 3 * rows : kAlign;
+}
+
+moe_status moe_grouped_ffn_backward(const moe_config* c, const void* x_perm, const int32_t* offsets, const void* W_gate, const void* W_up,
+                                    const void* W_down, const void* g, const void* u, const void* dy_perm, void* dx_perm, void* dW_gate,
+                                    void* dW_up, void* dW_down, int32_t flags, void* workspace, size_t ws_bytes, void* stream) {
+    const moe_status st = check_train(c);
+    if (st != MOE_OK) return st;
+    if ((flags & ~(MOE_GRAD_F32 | MOE_GRAD_ACCUMULATE)) != 0) return MOE_ERR_SHAPE;
+    if (!offsets || !W_gate || !W_up || !W_down || !workspace) return MOE_ERR_NULL;
+    if (c->T > 0 && (!x_perm || !g || !u || !dy_perm)) return MOE_ERR_NULL;
+    for (const void* p : {x_perm, W_gate, W_up, W_down, g, u, dy_perm, (const void*)dx_perm, (const void*)dW_gate, (const void*)dW_up, (const void*)dW_down})
+        if (misaligned(p)) return MOE_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(workspace) & (kAlign - 1)) != 0) return MOE_ERR_ALIGN;
+    if (ws_bytes < moe_ffn_backward_workspace_size(c)) return MOE_ERR_WORKSPACE;
+    const size_t rows = align_up((size_t)c->T * c->k * c->F * sizeof(uint16_t));
+    char* ws = (char*)workspace;
+    const FfnGrad p{(const uint16_t*)x_perm, (const uint16_t*)W_gate, (const uint16_t*)W_up, (const uint16_t*)W_down, (const uint16_t*)g, (const uint16_t*)u,
+                    (const uint16_t*)dy_perm, offsets, (uint16_t*)ws, (uint16_t*)(ws + rows), (uint16_t*)(ws + 2 * rows), (uint16_t*)dx_perm,
+                    dW_gate, dW_up, dW_down, flags & MOE_GRAD_F32, flags & MOE_GRAD_ACCUMULATE};
+    return hip_status(launch_ffn_backward(*c, p, (hipStream_t)stream));
+}
+
+moe_status moe_combine_backward(const moe_config* c, const void* dy, const void* y_perm, const int32_t* row_of, const float* topk_w, void* dy_perm,
+                                float* d_topk_w, void* stream) {
+    const moe_status st = check_config(c);
+    if (st != MOE_OK) return st;
+    if (c->T > 0 && (!dy || !y_perm || !row_of || !topk_w || !dy_perm || !d_topk_w)) return MOE_ERR_NULL;
+    if (misaligned(dy) || misaligned(y_perm) || misaligned(dy_perm)) return MOE_ERR_ALIGN;
+    if (c->T == 0) return MOE_OK;
+    return hip_status(launch_combine_backward(*c, (const uint16_t*)dy, (const uint16_t*)y_perm, row_of, topk_w, (uint16_t*)dy_perm, d_topk_w,
+                                              (hipStream_t)stream));
 }
 
 }  // extern "C"

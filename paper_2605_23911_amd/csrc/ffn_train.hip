@@ -1,0 +1,241 @@
+// The gated feed-forward block for training, over expert-contiguous rows (one expert: a dense block).
+//   forward   g = x Wg^T, u = x Wu^T, both kept; h = SiLU(g) (.) u                                  (Eq. 4)
+//   backward  dh = dy Wd;  dg = dh u SiLU'(g), du = dh SiLU(g), h again from g and u                (launch 1)
+//             dx = dg Wg + du Wu                                                                    (launch 2)
+//             dWg = dg^T x, dWu = du^T x, dWd = dy^T h, per expert                                  (launch 3)
+// with SiLU(g) = g s, SiLU'(g) = s (1 + g (1 - s)), s = 1 / (1 + exp(-g)).
+#include "mma_tile.hpp"
+
+namespace moe {
+
+namespace {
+
+// s = sigmoid(g); exp(-g) = inf gives 0.  v_rcp_f32 and v_exp_f32 (1 ulp each): what is formed from s is rounded to bf16.
+__device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
+
+struct GatedArgs {
+    const uint16_t *x, *wg, *wu;
+    const int32_t* offsets;
+    uint16_t *g, *u, *h;
+    int E, d, F;
+};
+
+// Tile: BM rows x BN / 2 features of both projections: the first half of B's rows are the gate's, the second the up projection's,
+// so that one copy of the token tile in LDS feeds both and the activation needs nothing but the tile.
+template <class S>
+__global__ __launch_bounds__(kMmaThreads) void gated_keep_kernel(GatedArgs a) {
+    __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
+    constexpr int FB = S::BN / 2;
+    RowTile t;
+    if (!find_tile(a.offsets, a.E, S::BM, (a.F + FB - 1) / FB, t)) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    const int f0 = t.n * FB, features = a.F - f0 < FB ? a.F - f0 : FB;
+    const bool up = wave >= kMmaWaves / 2;
+    Loader<S::BM, true> la;
+    Loader<S::BN, true> lb;
+    la.init(a.d, wave, lane);
+    lb.init(a.d, wave, lane, up ? FB : 0);
+    Acc<S> acc;
+    clear<S>(acc);
+    multiply<S, true, true>(acc, Stream<true>::make(a.x + (size_t)t.row0 * a.d, a.d, t.rows, 0),
+                            Stream<true>::make((up ? a.wu : a.wg) + ((size_t)t.e * a.F + f0) * a.d, a.d, features, 0), la, lb, a.d / kMmaK, lds);
+    by_rows<S, FB / 8>(acc, lds, [&](int r, int c, const float* row) {
+        if (r >= t.rows || c * 8 >= features) return;
+        float g[8], u[8], h[8];
+        load8(row + c * 8, g);
+        load8(row + FB + c * 8, u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] = g[i] * sigmoid(g[i]) * u[i];
+        const size_t at = (size_t)(t.row0 + r) * a.F + f0 + c * 8;
+        *reinterpret_cast<u32x4_t*>(a.g + at) = pack8(g);
+        *reinterpret_cast<u32x4_t*>(a.u + at) = pack8(u);
+        *reinterpret_cast<u32x4_t*>(a.h + at) = pack8(h);
+    });
+}
+
+struct GradArgs {
+    const uint16_t *x, *wg, *wu, *wd, *g, *u, *dy;
+    const int32_t* offsets;
+    uint16_t *dg, *du, *h, *dx;
+    void *dwg, *dwu, *dwd;     // bf16 or fp32; null: not wanted
+    int E, d, F;
+    int f32, add;              // weight gradients in fp32; added to what is there
+};
+
+// dh = dy Wd, and from the tile's dh and the kept g and u: dg, du and h.  dg and du are rounded to bf16, as the operands that the
+// products of launches 2 and 3 take; g and u are the rounded values that the forward pass kept.
+template <class S>
+__global__ __launch_bounds__(kMmaThreads) void gated_grad_kernel(GradArgs a) {
+    __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
+    RowTile t;
+    if (!find_tile(a.offsets, a.E, S::BM, (a.F + S::BN - 1) / S::BN, t)) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    const int f0 = t.n * S::BN;
+    Loader<S::BM, true> la;
+    Loader<S::BN, false> lb;
+    la.init(a.d, wave, lane);
+    lb.init(a.F, wave, lane);
+    Acc<S> acc;
+    clear<S>(acc);
+    multiply<S, true, false>(acc, Stream<true>::make(a.dy + (size_t)t.row0 * a.d, a.d, t.rows, 0),
+                             Stream<false>::make(a.wd + (size_t)t.e * a.d * a.F, a.F, f0, a.d), la, lb, a.d / kMmaK, lds);
+    by_rows<S, S::BN / 8>(acc, lds, [&](int r, int c, const float* row) {
+        if (r >= t.rows || f0 + c * 8 >= a.F) return;
+        const size_t at = (size_t)(t.row0 + r) * a.F + f0 + c * 8;
+        float dh[8], g[8], u[8], dg[8], du[8], h[8];
+        unpack8(*reinterpret_cast<const u32x4_t*>(a.g + at), g);
+        unpack8(*reinterpret_cast<const u32x4_t*>(a.u + at), u);
+        load8(row + c * 8, dh);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float s = sigmoid(g[i]), act = g[i] * s;
+            dg[i] = dh[i] * u[i] * (s + act * (1.0f - s));
+            du[i] = dh[i] * act;
+            h[i] = act * u[i];
+        }
+        *reinterpret_cast<u32x4_t*>(a.dg + at) = pack8(dg);
+        *reinterpret_cast<u32x4_t*>(a.du + at) = pack8(du);
+        *reinterpret_cast<u32x4_t*>(a.h + at) = pack8(h);
+    });
+}
+
+// dx = dg Wg + du Wu: one sum over 2 F.
+template <class S>
+__global__ __launch_bounds__(kMmaThreads) void rows_grad_kernel(GradArgs a) {
+    __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
+    RowTile t;
+    if (!find_tile(a.offsets, a.E, S::BM, (a.d + S::BN - 1) / S::BN, t)) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    const int n0 = t.n * S::BN;
+    Loader<S::BM, true> la;
+    Loader<S::BN, false> lb;
+    la.init(a.F, wave, lane);
+    lb.init(a.d, wave, lane);
+    Acc<S> acc;
+    clear<S>(acc);
+#pragma unroll 1
+    for (int m = 0; m < 2; ++m)
+        multiply<S, true, false>(acc, Stream<true>::make((m ? a.du : a.dg) + (size_t)t.row0 * a.F, a.F, t.rows, 0),
+                                 Stream<false>::make((m ? a.wu : a.wg) + (size_t)t.e * a.F * a.d, a.d, n0, a.F), la, lb, a.F / kMmaK, lds);
+    by_rows<S, S::BN / 8>(acc, lds, [&](int r, int c, const float* row) {
+        if (r >= t.rows || n0 + c * 8 >= a.d) return;
+        float v[8];
+        load8(row + c * 8, v);
+        *reinterpret_cast<u32x4_t*>(a.dx + (size_t)(t.row0 + r) * a.d + n0 + c * 8) = pack8(v);
+    });
+}
+
+// dW[m, n] = sum over the expert's rows of P[row, m] Q[row, n] for the three matrices in one launch (the tails of three would add
+// up): tiles [expert][matrix][patch].  An expert without rows gets zeros.
+template <class S>
+__global__ __launch_bounds__(kMmaThreads) void weights_grad_kernel(GradArgs a) {
+    __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
+    const int tm_f = (a.F + S::BM - 1) / S::BM, tn_d = (a.d + S::BN - 1) / S::BN;     // gate, up: [F, d]
+    const int tm_d = (a.d + S::BM - 1) / S::BM, tn_f = (a.F + S::BN - 1) / S::BN;     // down: [d, F]
+    const int n_g = a.dwg ? tm_f * tn_d : 0, n_u = a.dwu ? tm_f * tn_d : 0, n_d = a.dwd ? tm_d * tn_f : 0, each = n_g + n_u + n_d;
+    int t = xcd_tile(a.E * each);
+    if (t < 0) return;
+    const int e = t / each;
+    t -= e * each;
+    const int which = t < n_g ? 0 : t < n_g + n_u ? 1 : 2;
+    t -= which == 0 ? 0 : which == 1 ? n_g : n_g + n_u;
+    int tm, tn;
+    patch(t, which < 2 ? tm_f : tm_d, which < 2 ? tn_d : tn_f, tm, tn);
+    const int M = which < 2 ? a.F : a.d, N = which < 2 ? a.d : a.F, m0 = tm * S::BM, n0 = tn * S::BN;
+    const uint16_t* P = which == 0 ? a.dg : which == 1 ? a.du : a.dy;
+    const uint16_t* Q = which < 2 ? a.x : a.h;
+    const int row0 = a.offsets[e], rows = a.offsets[e + 1] - row0;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    Loader<S::BM, false> la;
+    Loader<S::BN, false> lb;
+    la.init(M, wave, lane);
+    lb.init(N, wave, lane);
+    Acc<S> acc;
+    clear<S>(acc);
+    multiply<S, false, false>(acc, Stream<false>::make(P + (size_t)row0 * M, M, m0, rows), Stream<false>::make(Q + (size_t)row0 * N, N, n0, rows),
+                              la, lb, (rows + kMmaK - 1) / kMmaK, lds);
+    void* const out = which == 0 ? a.dwg : which == 1 ? a.dwu : a.dwd;
+    by_rows<S, S::BN / 8>(acc, lds, [&](int r, int c, const float* row) {
+        if (m0 + r >= M || n0 + c * 8 >= N) return;
+        const size_t at = ((size_t)e * M + m0 + r) * N + n0 + c * 8;
+        float v[8];
+        load8(row + c * 8, v);
+        if (a.f32) {
+            float* dst = reinterpret_cast<float*>(out) + at;
+            if (a.add) {
+                float o[8];
+                load8(dst, o);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] += o[i];
+            }
+            *reinterpret_cast<f32x4*>(dst) = f32x4{v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<f32x4*>(dst + 4) = f32x4{v[4], v[5], v[6], v[7]};
+        } else {
+            u32x4_t* dst = reinterpret_cast<u32x4_t*>(reinterpret_cast<uint16_t*>(out) + at);
+            if (a.add) {
+                float o[8];
+                unpack8(*dst, o);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] += o[i];
+            }
+            *dst = pack8(v);
+        }
+    });
+}
+
+__global__ __launch_bounds__(256) void zero_kernel(u32x4_t* p, size_t n) {
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) p[i] = u32x4_t{0, 0, 0, 0};
+}
+
+template <class S>
+void go_keep(const GatedArgs& a, const moe_config& c, hipStream_t s) {
+    const long long tiles = most_blocks(c, S::BM) * ((a.F + S::BN / 2 - 1) / (S::BN / 2));
+    hipLaunchKernelGGL(gated_keep_kernel<S>, dim3(xcd_grid(tiles)), dim3(kMmaThreads), 0, s, a);
+}
+template <class S>
+void go_gated_grad(const GradArgs& a, const moe_config& c, hipStream_t s) {
+    hipLaunchKernelGGL(gated_grad_kernel<S>, dim3(xcd_grid(most_blocks(c, S::BM) * ((a.F + S::BN - 1) / S::BN))), dim3(kMmaThreads), 0, s, a);
+}
+template <class S>
+void go_rows_grad(const GradArgs& a, const moe_config& c, hipStream_t s) {
+    hipLaunchKernelGGL(rows_grad_kernel<S>, dim3(xcd_grid(most_blocks(c, S::BM) * ((a.d + S::BN - 1) / S::BN))), dim3(kMmaThreads), 0, s, a);
+}
+template <class S>
+void go_weights_grad(const GradArgs& a, hipStream_t s) {
+    const long long fd = (long long)((a.F + S::BM - 1) / S::BM) * ((a.d + S::BN - 1) / S::BN), df = (long long)((a.d + S::BM - 1) / S::BM) * ((a.F + S::BN - 1) / S::BN);
+    hipLaunchKernelGGL(weights_grad_kernel<S>, dim3(xcd_grid(a.E * ((a.dwg ? fd : 0) + (a.dwu ? fd : 0) + (a.dwd ? df : 0)))), dim3(kMmaThreads), 0, s, a);
+}
+
+}  // namespace
+
+hipError_t launch_gated_keep(const moe_config& c, const uint16_t* x_rows, const int32_t* offsets, const uint16_t* wg, const uint16_t* wu,
+                             uint16_t* g, uint16_t* u, uint16_t* h, hipStream_t s) {
+    const GatedArgs a{x_rows, wg, wu, offsets, g, u, h, c.E, c.d, c.F};
+    if ((long long)c.T * c.k <= 128ll * c.E) go_keep<Half>(a, c, s);
+    else go_keep<Wide>(a, c, s);
+    return hipGetLastError();
+}
+
+hipError_t launch_ffn_backward(const moe_config& c, const FfnGrad& p, hipStream_t s) {
+    const GradArgs a{p.x, p.wg, p.wu, p.wd, p.g, p.u, p.dy, p.offsets, p.dg, p.du, p.h, p.dx, p.dwg, p.dwu, p.dwd, c.E, c.d, c.F, p.f32, p.add};
+    if (c.T == 0) {            // no rows: weight gradients of zero, unless they are added to
+        const size_t n = (size_t)c.E * c.d * c.F * (p.f32 ? 4 : 2) / 16;
+        for (void* w : {p.dwg, p.dwu, p.dwd})
+            if (w && !p.add) hipLaunchKernelGGL(zero_kernel, dim3((unsigned)(n / 256 + 1 < 4096 ? n / 256 + 1 : 4096)), dim3(256), 0, s, (u32x4_t*)w, n);
+        return hipGetLastError();
+    }
+    const bool few = (long long)c.T * c.k <= 128ll * c.E;
+    if (few) go_gated_grad<Half>(a, c, s);
+    else go_gated_grad<Wide>(a, c, s);
+    if (p.dx) {
+        if (few) go_rows_grad<Half>(a, c, s);
+        else go_rows_grad<Wide>(a, c, s);
+    }
+    if (p.dwg || p.dwu || p.dwd) {
+        if (few) go_weights_grad<Half>(a, s);
+        else go_weights_grad<Wide>(a, s);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace moe

@@ -133,6 +133,22 @@ hipError_t launch_pack(const moe_config& c, const uint16_t* wg, const uint16_t* 
 hipError_t launch_combine(const moe_config& c, const uint16_t* y_perm, const int32_t* row_of,
                           const float* topk_w, uint16_t* y, hipStream_t s);
 
+// ---- training -----------------------------------------------------------------------------
+// g, u [R, F]: the two projections, h = SiLU(g) (.) u, over expert-contiguous rows (row-major weights)
+hipError_t launch_gated_keep(const moe_config& c, const uint16_t* x_rows, const int32_t* offsets, const uint16_t* wg, const uint16_t* wu,
+                             uint16_t* g, uint16_t* u, uint16_t* h, hipStream_t s);
+struct FfnGrad {
+    const uint16_t *x, *wg, *wu, *wd, *g, *u, *dy;
+    const int32_t* offsets;
+    uint16_t *dg, *du, *h;      // [R, F] scratch
+    uint16_t* dx;               // null: not wanted; so the three below
+    void *dwg, *dwu, *dwd;
+    int f32, add;               // weight gradients: in fp32; added to what the buffers hold
+};
+hipError_t launch_ffn_backward(const moe_config& c, const FfnGrad& p, hipStream_t s);
+hipError_t launch_combine_backward(const moe_config& c, const uint16_t* dy, const uint16_t* y_perm, const int32_t* row_of, const float* topk_w,
+                                   uint16_t* dy_perm, float* d_topk_w, hipStream_t s);
+
 // Many experts with a few rows each (Qwen2-MoE and DeepSeek-V3 shapes at up to 128 tokens): a
 // projection is thousands of short workgroups that stream a weight panel each, and what a CU
 // loses between two of them (schedule look-up, first loads, epilogue, launch of the next: ~5 us
