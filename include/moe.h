@@ -276,6 +276,36 @@ moe_status moe_grouped_ffn_backward(const moe_config* cfg, const void* x_perm, c
 moe_status moe_combine_backward(const moe_config* cfg, const void* dy, const void* y_perm, const int32_t* row_of,
                                 const float* topk_w, void* dy_perm, float* d_topk_w, void* stream);
 
+/* ---- Low-rank adapters of many requests beside a shared projection -------------------------
+ * Serving requests that have each their own low-rank update of a projection (a shared expert's, a dense block's), in one call:
+ *   y[t] = (base[t] +) x[t] W^T + scale[a] * (x[t] A[a]^T) B[a]^T,   a = adapter_of[t]
+ * Tokens in any order and number per adapter; an id outside 0 .. adapters-1 (by convention -1) is a token without one.
+ * Stored [out, in] as everywhere: W [N,K], A [adapters, rank, K], B [adapters, N, rank], bf16.  Adapters of a smaller rank are
+ * padded with rows (columns) of zeros.  scale [adapters] fp32 or NULL (1).
+ * x A^T is summed and scaled in fp32 and rounded to bf16 before the product with B; the sum of all parts is rounded once.
+ * Limits: N % 64 == 0, K % 64 == 0, N, K <= 2^20, rank % 8 == 0, 8 <= rank <= 128, adapters <= 65536, T*max(N,K)*2 bytes below
+ * 4 GiB, else MOE_ERR_UNSUPPORTED.  T == 0 returns MOE_OK and enqueues nothing.  Every pointer 16-byte aligned but adapter_of and scale.
+ * workspace: moe_adapter_workspace_size(cfg) bytes.  No atomics: results are bit-reproducible. */
+typedef struct {
+    int32_t T, N, K;           /* tokens, output and input features */
+    int32_t adapters, rank;
+} moe_adapter_config;
+
+size_t moe_adapter_workspace_size(const moe_adapter_config* cfg);
+
+/* base [T,N] bf16 or NULL: added before the rounding; may be y itself (e.g. the routed experts' result, to which the shared
+ * expert's down projection is added).  W may be NULL: the adapters' part alone, for a projection that is computed elsewhere. */
+moe_status moe_adapter_linear(const moe_adapter_config* cfg, const void* x, const void* W, const void* A, const void* B,
+                              const float* scale, const int32_t* adapter_of, const void* base, void* y,
+                              void* workspace, size_t ws_bytes, void* stream);
+
+/* The first half of a gated block with adapters: h [T,N] = SiLU(gate) (.) up, gate and up being two such projections of x, with the
+ * same adapter ids and scales; activation and product in fp32, one rounding. */
+moe_status moe_adapter_gated_up(const moe_adapter_config* cfg, const void* x, const void* W_gate, const void* W_up,
+                                const void* A_gate, const void* A_up, const void* B_gate, const void* B_up,
+                                const float* scale, const int32_t* adapter_of, void* h,
+                                void* workspace, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

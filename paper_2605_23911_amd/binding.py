@@ -25,6 +25,7 @@ EXPORTS = (
     "moe_forward_workspace_size", "moe_workspace_size", "moe_forward_workspace_layout", "moe_max_blocks", "moe_route",
     "moe_permute", "moe_permute_static", "moe_block_schedule", "moe_grouped_ffn", "moe_combine", "moe_forward", "moe_forward_staged", "moe_packed_weights_size", "moe_pack_weights", "moe_ffn_kernel_name",
     "moe_grouped_ffn_train", "moe_ffn_backward_workspace_size", "moe_grouped_ffn_backward", "moe_combine_backward",
+    "moe_adapter_workspace_size", "moe_adapter_linear", "moe_adapter_gated_up",
 )
 
 
@@ -42,6 +43,15 @@ class MoEConfig(C.Structure):
     @classmethod
     def of(cls, T, d, F, E, k, gating=GATE_SOFTMAX, tile_m=0, flags=0):
         return cls(T, d, F, E, k, gating, tile_m, flags)
+
+
+class AdapterConfig(C.Structure):
+    """moe_adapter_config: T tokens, N output and K input features, `adapters` stacked adapters of one rank."""
+    _fields_ = [("T", C.c_int32), ("N", C.c_int32), ("K", C.c_int32), ("adapters", C.c_int32), ("rank", C.c_int32)]
+
+    @classmethod
+    def of(cls, T, N, K, adapters, rank):
+        return cls(T, N, K, adapters, rank)
 
 
 class WorkspaceLayout(C.Structure):
@@ -103,6 +113,13 @@ def lib() -> C.CDLL:
     L.moe_grouped_ffn_backward.argtypes = [cfgp, vp, i32p] + [vp] * 10 + [C.c_int32, vp, C.c_size_t, vp]
     L.moe_combine_backward.restype = C.c_int
     L.moe_combine_backward.argtypes = [cfgp, vp, vp, i32p, f32p, vp, f32p, vp]
+    acfgp = C.POINTER(AdapterConfig)
+    L.moe_adapter_workspace_size.restype = C.c_size_t
+    L.moe_adapter_workspace_size.argtypes = [acfgp]
+    L.moe_adapter_linear.restype = C.c_int
+    L.moe_adapter_linear.argtypes = [acfgp, vp, vp, vp, vp, f32p, i32p, vp, vp, vp, C.c_size_t, vp]
+    L.moe_adapter_gated_up.restype = C.c_int
+    L.moe_adapter_gated_up.argtypes = [acfgp] + [vp] * 7 + [f32p, i32p, vp, vp, C.c_size_t, vp]
     L.moe_test_knob.restype = C.c_int32       # test hook, not part of include/moe.h
     L.moe_test_knob.argtypes = [C.c_int32, C.c_int32]
     L.moe_test_map_launch.restype = C.c_int32  # test hook (host arithmetic only), not part of include/moe.h
@@ -337,3 +354,29 @@ def moe_combine_backward(cfg, dy, y_perm, row_of, topk_w, dy_perm, d_topk_w, str
     a.run("moe_combine_backward", lib().moe_combine_backward, C.byref(cfg), a("dy", dy, (T, d), b), a("y_perm", y_perm, (T * k, d), b),
           a("row_of", row_of, (T, k), torch.int32), a("topk_w", topk_w, (T, k), torch.float32), a("dy_perm", dy_perm, (T * k, d), b),
           a("d_topk_w", d_topk_w, (T, k), torch.float32))
+
+
+# ---- adapters ------------------------------------------------------------------------------------------------------------
+
+
+def adapter_workspace_size(cfg) -> int:
+    return lib().moe_adapter_workspace_size(C.byref(cfg))
+
+
+def moe_adapter_linear(cfg, x, W, A, B, scale, adapter_of, y, workspace, base=None, stream=None):
+    """y = (base +) x W^T + scale[a] (x A[a]^T) B[a]^T, a = adapter_of[t]; W None: without the shared projection; scale None: 1."""
+    a, b, c = _Call(stream), torch.bfloat16, cfg
+    a.run("moe_adapter_linear", lib().moe_adapter_linear, C.byref(c), a("x", x, (c.T, c.K), b), a("W", W, (c.N, c.K), b, True),
+          a("A", A, (c.adapters, c.rank, c.K), b), a("B", B, (c.adapters, c.N, c.rank), b), a("scale", scale, (c.adapters,), torch.float32, True),
+          a("adapter_of", adapter_of, (c.T,), torch.int32), a("base", base, (c.T, c.N), b, True), a("y", y, (c.T, c.N), b),
+          a.raw("workspace", workspace), _nbytes(workspace))
+
+
+def moe_adapter_gated_up(cfg, x, W_gate, W_up, A_gate, A_up, B_gate, B_up, scale, adapter_of, h, workspace, stream=None):
+    """h = SiLU(gate) (.) up, both projections of x with adapters as in moe_adapter_linear."""
+    a, b, c = _Call(stream), torch.bfloat16, cfg
+    a.run("moe_adapter_gated_up", lib().moe_adapter_gated_up, C.byref(c), a("x", x, (c.T, c.K), b), a("W_gate", W_gate, (c.N, c.K), b),
+          a("W_up", W_up, (c.N, c.K), b), a("A_gate", A_gate, (c.adapters, c.rank, c.K), b), a("A_up", A_up, (c.adapters, c.rank, c.K), b),
+          a("B_gate", B_gate, (c.adapters, c.N, c.rank), b), a("B_up", B_up, (c.adapters, c.N, c.rank), b),
+          a("scale", scale, (c.adapters,), torch.float32, True), a("adapter_of", adapter_of, (c.T,), torch.int32), a("h", h, (c.T, c.N), b),
+          a.raw("workspace", workspace), _nbytes(workspace))

@@ -1,0 +1,445 @@
+// Low-rank adapters of many requests at once beside a shared projection:
+//   y[t] = (base[t] +) x[t] W^T + scale[a] (x[t] A[a]^T) B[a]^T,   a = adapter_of[t]
+// and the gated pair of two such projections of one input, h = SiLU(gate) (.) up.
+// Two launches.  low_rank_kernel forms v[t] = scale[a] x[t] A[a]^T; the projection's kernel then takes v[t] B[a]^T as `rank` more
+// elements of its reduction, so the result is rounded once and never read back.  Tokens stay in the caller's order: a block
+// of tokens goes through the adapters that occur in it one after the other, the other tokens' v masked to zero.  Tokens of a
+// request lie together in a prompt (one adapter per block); in a decode batch every adapter is needed anyway.
+#include "mma_tile.hpp"
+
+namespace moe {
+
+namespace {
+
+struct AdapterArgs {
+    const uint16_t* x;                // [T, K]
+    const uint16_t *w[2], *a[2], *b[2];   // [N, K], [n, rank, K], [n, N, rank]; the gated pair has two of each
+    const float* scale;               // [n] or null
+    const int32_t* of;                // [T]
+    const uint16_t* base;             // [T, N] or null
+    float* v;                         // [parts][matrices][T][rank] partial sums over K
+    uint16_t* y;                      // [T, N]
+    int T, N, K, n, rank;
+    int parts, lists;                 // low_rank_kernel: pieces of K, workgroups per token block
+};
+
+__device__ __forceinline__ bf16x8 zeros8() { return bf16x8{0, 0, 0, 0, 0, 0, 0, 0}; }
+// Adapter of a token; -1 where it has none (an id outside 0 .. n - 1 means that too).
+__device__ __forceinline__ int adapter_of(const AdapterArgs& p, int t) {
+    const int a = t < p.T ? p.of[t] : -1;
+    return a >= 0 && a < p.n ? a : -1;
+}
+
+// v: a workgroup takes 32 tokens, one piece of K, and of the adapters that occur in the block every lists-th.  Its eight wavefronts split the
+// piece again and are joined through LDS.  Bound by reading A (once per block of 32 tokens that has the adapter).
+template <int RB, int MATS>
+__global__ __launch_bounds__(kMmaThreads) void low_rank_kernel(AdapterArgs p) {
+    __shared__ float part[kMmaWaves][32][RB * 32 + 1];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, r = lane & 31, half = lane >> 5;
+    const int block = blockIdx.x / (p.lists * p.parts), rest = blockIdx.x % (p.lists * p.parts), list = rest / p.parts, piece = rest % p.parts;
+    const int t0 = block * 32, t = t0 + r;
+    const int steps = p.K / 16, each = (steps + p.parts * kMmaWaves - 1) / (p.parts * kMmaWaves);
+    const int s0 = (piece * kMmaWaves + wave) * each, s1 = s0 + each < steps ? s0 + each : steps;
+    const int id = adapter_of(p, t);
+    unsigned long long left = __ballot(id >= 0) & 0xffffffffull;
+    const uint16_t* x = p.x + (size_t)(t < p.T ? t : p.T - 1) * p.K + half * 8;
+    for (int i = 0; left != 0; ++i) {
+        const int a = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+        const bool mine = id == a;
+        left &= ~__ballot(mine);
+        if (i % p.lists != list) continue;
+        f32x16 acc[MATS][RB];
+#pragma unroll
+        for (int m = 0; m < MATS; ++m)
+#pragma unroll
+            for (int b = 0; b < RB; ++b)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) acc[m][b][q] = 0.0f;
+        const uint16_t* rows[MATS][RB];
+#pragma unroll
+        for (int m = 0; m < MATS; ++m)
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
+                const int row = b * 32 + r;
+                rows[m][b] = p.a[m] + ((size_t)a * p.rank + (row < p.rank ? row : p.rank - 1)) * p.K + half * 8;
+            }
+        auto step = [&](int s, auto count) {
+            constexpr int U = decltype(count)::value;            // steps whose loads are under way at once
+            bf16x8 fx[U], fa[U][MATS][RB];
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                fx[i] = *reinterpret_cast<const bf16x8*>(x + (s + i) * 16);
+#pragma unroll
+                for (int m = 0; m < MATS; ++m)
+#pragma unroll
+                    for (int b = 0; b < RB; ++b) fa[i][m][b] = *reinterpret_cast<const bf16x8*>(rows[m][b] + (s + i) * 16);
+            }
+#pragma unroll
+            for (int i = 0; i < U; ++i)
+#pragma unroll
+                for (int m = 0; m < MATS; ++m)
+#pragma unroll
+                    for (int b = 0; b < RB; ++b) acc[m][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i][m][b], fx[i], acc[m][b], 0, 0, 0);
+        };
+        constexpr int U = MATS * RB >= 4 ? 4 : 8;
+        int s = s0;
+        for (; s + U <= s1; s += U) step(s, std::integral_constant<int, U>{});
+        for (; s < s1; ++s) step(s, std::integral_constant<int, 1>{});
+        const float scale = p.scale ? p.scale[a] : 1.0f;
+        const unsigned here = (unsigned)__ballot(mine);          // the block's tokens with this adapter
+#pragma unroll
+        for (int m = 0; m < MATS; ++m) {
+            __syncthreads();
+#pragma unroll
+            for (int b = 0; b < RB; ++b)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) part[wave][r][b * 32 + (q / 4) * 8 + half * 4 + q % 4] = acc[m][b][q];
+            __syncthreads();
+            for (int j = threadIdx.x; j < 32 * p.rank; j += kMmaThreads) {
+                const int row = j / p.rank, c = j % p.rank;
+                if (!((here >> row) & 1)) continue;
+                float sum = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kMmaWaves; ++w) sum += part[w][row][c];
+                p.v[(((size_t)piece * MATS + m) * p.T + t0 + row) * p.rank + c] = sum * scale;
+            }
+        }
+    }
+}
+
+// Takes over what an adapter adds for the lanes whose token (a lane holds one token's results) has it: a masked zero times an infinity or a
+// NaN in another request's adapter would be NaN.
+template <class V>
+__device__ __forceinline__ void keep_mine(V& acc, V with, bool mine) {
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(V) / 4); ++i) acc[i] = mine ? with[i] : acc[i];
+}
+
+// Eight elements of a token's v: the pieces' sum, rounded to bf16 as the operand that B is multiplied with (as h is for the down
+// projection: its error, 2^-8 of the adapter's part at most per element and of random sign, is below that of rounding y).
+__device__ __forceinline__ bf16x8 low_rank8(const AdapterArgs& p, int mats, int m, int t, int c) {
+    float sum[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+    for (int q = 0; q < p.parts; ++q) {
+        float v[8];
+        load8(p.v + (((size_t)q * mats + m) * p.T + t) * p.rank + c, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += v[i];
+    }
+    return __builtin_bit_cast(bf16x8, pack8(sum));
+}
+
+__device__ __forceinline__ float silu(float g) { return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
+
+constexpr int kMaxRank = 128;
+
+// Many tokens: tiles of the projection as in ffn_train.hip, then the adapters of the tile's tokens.
+template <class S, int MATS>
+__global__ __launch_bounds__(kMmaThreads) void adapter_rows_kernel(AdapterArgs p) {
+    constexpr int FB = S::BN / MATS, kRow = kMaxRank * 2 + 16, kV = MATS * S::BM * kRow;     // bytes of a token's v in LDS
+    __shared__ __attribute__((aligned(1024))) char lds[(S::kLds > kV ? S::kLds : kV) + S::BM * 4];
+    const int tm_n = (p.T + S::BM - 1) / S::BM, tn_n = (p.N + FB - 1) / FB;
+    const int t = xcd_tile(tm_n * tn_n);
+    if (t < 0) return;
+    int tm, tn;
+    patch(t, tm_n, tn_n, tm, tn);
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid % kWave;
+    const int wm = wave / S::WN, wn = wave % S::WN;
+    const int t0 = tm * S::BM, rows = p.T - t0 < S::BM ? p.T - t0 : S::BM, n0 = tn * FB, cols = p.N - n0 < FB ? p.N - n0 : FB;
+    int32_t* const ids = reinterpret_cast<int32_t*>(lds + (S::kLds > kV ? S::kLds : kV));
+    for (int i = tid; i < S::BM; i += kMmaThreads) ids[i] = adapter_of(p, t0 + i);
+    Acc<S> acc;
+    clear<S>(acc);
+    {
+        const bool second = MATS == 2 && wave >= kMmaWaves / 2;
+        Loader<S::BM, true> la;
+        Loader<S::BN, true> lb;
+        la.init(p.K, wave, lane);
+        lb.init(p.K, wave, lane, second ? FB : 0);
+        const uint16_t* w = second ? p.w[1] : p.w[0];
+        multiply<S, true, true>(acc, Stream<true>::make(p.x + (size_t)t0 * p.K, p.K, rows, 0), Stream<true>::make(w + (size_t)n0 * p.K, p.K, cols, 0),
+                                la, lb, w ? p.K / kMmaK : 0, lds);
+    }
+    // What the rest derives from the thread's number is worked out here, not held in registers through the reduction.
+    int again = threadIdx.x;
+    asm volatile("" : "+v"(again));
+    const int tid2 = again, lane2 = again % kWave;
+    // the tile's v as bf16
+    for (int j = tid2; j < MATS * S::BM * (p.rank / 8); j += kMmaThreads) {
+        const int c = j % (p.rank / 8), row = j / (p.rank / 8) % S::BM, m = j / (p.rank / 8) / S::BM;
+        if (ids[row] >= 0) *reinterpret_cast<bf16x8*>(lds + (m * S::BM + row) * kRow + c * 16) = low_rank8(p, MATS, m, t0 + row, c * 8);
+    }
+    __syncthreads();
+    {
+        const int r = lane2 & 31, half = lane2 >> 5, c0 = wn * S::NB * 32, m2 = MATS == 2 && c0 >= FB ? 1 : 0;
+        int id[S::MB];
+        unsigned left[S::MB], any = 0;
+#pragma unroll
+        for (int m = 0; m < S::MB; ++m) {
+            id[m] = ids[(wm * S::MB + m) * 32 + r];
+            left[m] = (unsigned)__ballot(id[m] >= 0);
+            any |= left[m];
+        }
+        const uint16_t* brow[S::NB];
+#pragma unroll
+        for (int n = 0; n < S::NB; ++n) {
+            int col = n0 + c0 - m2 * FB + n * 32 + r;
+            brow[n] = p.b[m2] + (size_t)(col < p.N ? col : p.N - 1) * p.rank;
+        }
+        while (any) {
+            int a = -1;
+#pragma unroll
+            for (int m = S::MB - 1; m >= 0; --m)
+                if (left[m]) a = __builtin_amdgcn_readlane(id[m], __builtin_ctz(left[m]));
+            unsigned here[S::MB];
+            any = 0;
+#pragma unroll
+            for (int m = 0; m < S::MB; ++m) {
+                here[m] = (unsigned)__ballot(id[m] == a);
+                left[m] &= ~here[m];
+                any |= left[m];
+            }
+            for (int c = 0; c < p.rank; c += 16) {
+                const bool in = c + half * 8 < p.rank;
+                bf16x8 fb[S::NB];
+#pragma unroll
+                for (int n = 0; n < S::NB; ++n)
+                    fb[n] = in ? *reinterpret_cast<const bf16x8*>(brow[n] + (size_t)a * p.N * p.rank + c + half * 8) : zeros8();
+#pragma unroll
+                for (int m = 0; m < S::MB; ++m) {
+                    if (!here[m]) continue;
+                    const bf16x8 fv = in && id[m] == a
+                        ? *reinterpret_cast<const bf16x8*>(lds + (m2 * S::BM + (wm * S::MB + m) * 32 + r) * kRow + (c + half * 8) * 2) : zeros8();
+#pragma unroll
+                    for (int n = 0; n < S::NB; ++n) keep_mine<f32x16>(acc[n][m], __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[n], fv, acc[n][m], 0, 0, 0), id[m] == a);
+                }
+            }
+        }
+    }
+    __syncthreads();
+    by_rows<S, FB / 8>(acc, lds, [&](int r, int c, const float* row) {
+        if (r >= rows || c * 8 >= cols) return;
+        float v[8];
+        load8(row + c * 8, v);
+        const size_t at = (size_t)(t0 + r) * p.N + n0 + c * 8;
+        if constexpr (MATS == 2) {
+            float u[8];
+            load8(row + FB + c * 8, u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = silu(v[i]) * u[i];
+        } else if (p.base) {
+            float o[8];
+            unpack8(*reinterpret_cast<const u32x4_t*>(p.base + at), o);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += o[i];
+        }
+        *reinterpret_cast<u32x4_t*>(p.y + at) = pack8(v);
+    });
+}
+
+// Up to 64 tokens: bound by streaming W.  A workgroup takes NB blocks of 16 features (of each matrix) and all tokens (MB blocks of 16); its
+// eight wavefronts split K, and the adapters that occur, and are joined through LDS.  Weights go from memory to registers: 16x16x32
+// MFMAs, so that four lanes read 64 consecutive bytes of a weight row.
+template <int MB, int NB, int MATS>
+__global__ __launch_bounds__(kMmaThreads) void adapter_few_kernel(AdapterArgs p) {
+    constexpr int kRow = kMaxRank * 2 + 16, kV = MATS * MB * 16 * kRow, kPart = kMmaWaves * MATS * NB * MB * 64 * 16;
+    __shared__ __attribute__((aligned(1024))) char lds[kPart > kV ? kPart : kV];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid % kWave, r = lane & 15, quad = lane >> 4;
+    const int n0 = blockIdx.x * (NB * 16);
+    f32x4 acc[MATS][NB][MB];
+#pragma unroll
+    for (int m = 0; m < MATS; ++m)
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int b = 0; b < MB; ++b) acc[m][n][b] = f32x4{0, 0, 0, 0};
+    const int steps = p.w[0] ? p.K / 32 : 0, each = (steps + kMmaWaves - 1) / kMmaWaves;
+    const int s0 = wave * each < steps ? wave * each : steps, s1 = s0 + each < steps ? s0 + each : steps;
+    const uint16_t *wrow[MATS][NB], *xrow[MB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+        const int col = n0 + n * 16 + r;
+#pragma unroll
+        for (int m = 0; m < MATS; ++m) wrow[m][n] = p.w[m] + (size_t)(col < p.N ? col : p.N - 1) * p.K + quad * 8;
+    }
+#pragma unroll
+    for (int b = 0; b < MB; ++b) xrow[b] = p.x + (size_t)(b * 16 + r < p.T ? b * 16 + r : p.T - 1) * p.K + quad * 8;
+    auto step = [&](int s, auto count) {
+        constexpr int U = decltype(count)::value;                // steps whose weights are under way at once
+        u32x4_t fw[U][MATS][NB];
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+#pragma unroll
+            for (int m = 0; m < MATS; ++m)
+#pragma unroll
+                for (int n = 0; n < NB; ++n) fw[i][m][n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(wrow[m][n] + (s + i) * 32));
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            bf16x8 fx[MB];
+#pragma unroll
+            for (int b = 0; b < MB; ++b) fx[b] = *reinterpret_cast<const bf16x8*>(xrow[b] + (s + i) * 32);
+#pragma unroll
+            for (int m = 0; m < MATS; ++m)
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int b = 0; b < MB; ++b)
+                        acc[m][n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fw[i][m][n]), fx[b], acc[m][n][b], 0, 0, 0);
+        }
+    };
+    constexpr int U = 8 / (MATS * NB);
+    int s = s0;
+    for (; s + U <= s1; s += U) step(s, std::integral_constant<int, U>{});
+    for (; s < s1; ++s) step(s, std::integral_constant<int, 1>{});
+    // v of all tokens as bf16
+    const int chunks = p.rank / 8;
+    for (int j = tid; j < MATS * MB * 16 * chunks; j += kMmaThreads) {
+        const int c = j % chunks, t = j / chunks % (MB * 16), m = j / chunks / (MB * 16);
+        if (adapter_of(p, t) >= 0) *reinterpret_cast<bf16x8*>(lds + (m * MB * 16 + t) * kRow + c * 16) = low_rank8(p, MATS, m, t, c * 8);
+    }
+    __syncthreads();
+    const int id = adapter_of(p, lane);
+    int idb[MB];
+#pragma unroll
+    for (int b = 0; b < MB; ++b) idb[b] = __shfl(id, b * 16 + r, kWave);
+    unsigned long long left = __ballot(id >= 0);
+    for (int i = 0; left != 0; ++i) {
+        const int a = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+        const unsigned long long here = __ballot(id == a);
+        left &= ~here;
+        if (i % kMmaWaves != wave) continue;
+        for (int c = 0; c < p.rank; c += 32) {
+            const bool in = c + quad * 8 < p.rank;
+            bf16x8 fb[MATS][NB];
+#pragma unroll
+            for (int m = 0; m < MATS; ++m)
+#pragma unroll
+                for (int n = 0; n < NB; ++n) {
+                    const int col = n0 + n * 16 + r;
+                    fb[m][n] = in ? *reinterpret_cast<const bf16x8*>(p.b[m] + ((size_t)a * p.N + (col < p.N ? col : p.N - 1)) * p.rank + c + quad * 8) : zeros8();
+                }
+#pragma unroll
+            for (int b = 0; b < MB; ++b) {
+                if (!((here >> (b * 16)) & 0xffff)) continue;
+#pragma unroll
+                for (int m = 0; m < MATS; ++m) {
+                    const bf16x8 fv = in && idb[b] == a ? *reinterpret_cast<const bf16x8*>(lds + (m * MB * 16 + b * 16 + r) * kRow + (c + quad * 8) * 2) : zeros8();
+#pragma unroll
+                    for (int n = 0; n < NB; ++n)
+                        keep_mine<f32x4>(acc[m][n][b], __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[m][n], fv, acc[m][n][b], 0, 0, 0), idb[b] == a);
+                }
+            }
+        }
+    }
+    __syncthreads();
+    f32x4* const part = reinterpret_cast<f32x4*>(lds);       // [wave][matrix][n][b][lane]
+#pragma unroll
+    for (int m = 0; m < MATS; ++m)
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int b = 0; b < MB; ++b) part[(((wave * MATS + m) * NB + n) * MB + b) * 64 + lane] = acc[m][n][b];
+    __syncthreads();
+    for (int j = tid; j < NB * MB * 64; j += kMmaThreads) {
+        const int l = j % 64, b = j / 64 % MB, n = j / 64 / MB, t = b * 16 + (l & 15), col = n0 + n * 16 + (l >> 4) * 4;
+        if (t >= p.T || col >= p.N) continue;
+        f32x4 v[MATS];
+#pragma unroll
+        for (int m = 0; m < MATS; ++m) {
+            v[m] = part[((m * NB + n) * MB + b) * 64 + l];
+#pragma unroll
+            for (int w = 1; w < kMmaWaves; ++w) {
+                const f32x4 o = part[(((w * MATS + m) * NB + n) * MB + b) * 64 + l];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[m][i] += o[i];
+            }
+        }
+        const size_t at = (size_t)t * p.N + col;
+        if constexpr (MATS == 2) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[0][i] = silu(v[0][i]) * v[1][i];
+        } else if (p.base) {
+            const uint2 o = *reinterpret_cast<const uint2*>(p.base + at);
+            v[0][0] += __uint_as_float(o.x << 16), v[0][1] += __uint_as_float(o.x & 0xffff0000u);
+            v[0][2] += __uint_as_float(o.y << 16), v[0][3] += __uint_as_float(o.y & 0xffff0000u);
+        }
+        *reinterpret_cast<uint2*>(p.y + at) = make_uint2(pack2_bf16(v[0][0], v[0][1]), pack2_bf16(v[0][2], v[0][3]));
+    }
+}
+
+constexpr int kFewTokens = 64;
+
+// Pieces of K and workgroups per block of 32 tokens of low_rank_kernel.  Every occurring adapter of a block can have a workgroup of its own
+// while that keeps the launch within 4096; K is cut until there is a workgroup per CU, into eight pieces at most, which the
+// projection's kernel adds up, and no finer than 64 elements per wavefront.
+struct Split {
+    int blocks, lists, parts;
+};
+Split split(const moe_adapter_config& c) {
+    Split s;
+    s.blocks = (c.T + 31) / 32;
+    s.lists = c.adapters < 32 ? c.adapters : 32;
+    if (c.T < s.lists) s.lists = c.T;
+    while (s.lists > 1 && (long long)s.blocks * s.lists > 4096) s.lists = (s.lists + 1) / 2;
+    s.parts = 1;
+    while (s.parts < 8 && (long long)s.blocks * s.lists * s.parts < 256 && c.K >= s.parts * 2 * kMmaWaves * 64) s.parts *= 2;
+    return s;
+}
+
+template <int MATS>
+void low_rank(const AdapterArgs& p, unsigned grid, hipStream_t s) {
+    const int rb = (p.rank + 31) / 32;
+    if (rb == 1) hipLaunchKernelGGL((low_rank_kernel<1, MATS>), dim3(grid), dim3(kMmaThreads), 0, s, p);
+    else if (rb == 2) hipLaunchKernelGGL((low_rank_kernel<2, MATS>), dim3(grid), dim3(kMmaThreads), 0, s, p);
+    else hipLaunchKernelGGL((low_rank_kernel<4, MATS>), dim3(grid), dim3(kMmaThreads), 0, s, p);
+}
+
+template <int MB, int MATS>
+void few(const AdapterArgs& p, hipStream_t s) {
+    hipLaunchKernelGGL((adapter_few_kernel<MB, 1, MATS>), dim3((p.N + 15) / 16), dim3(kMmaThreads), 0, s, p);
+}
+
+template <class S, int MATS>
+void many(const AdapterArgs& p, hipStream_t s) {
+    const long long tiles = (long long)((p.T + S::BM - 1) / S::BM) * ((p.N + S::BN / MATS - 1) / (S::BN / MATS));
+    hipLaunchKernelGGL((adapter_rows_kernel<S, MATS>), dim3(xcd_grid(tiles)), dim3(kMmaThreads), 0, s, p);
+}
+
+template <int MATS>
+hipError_t launch(AdapterArgs p, const moe_adapter_config& c, hipStream_t s) {
+    const Split sp = split(c);
+    p.parts = sp.parts;
+    p.lists = sp.lists;
+    low_rank<MATS>(p, (unsigned)(sp.blocks * sp.lists * sp.parts), s);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (p.T <= kFewTokens) {
+        switch ((p.T + 15) / 16) {
+            case 1: few<1, MATS>(p, s); break;
+            case 2: few<2, MATS>(p, s); break;
+            case 3: few<3, MATS>(p, s); break;
+            default: few<4, MATS>(p, s);
+        }
+    } else {
+        const long long wide = (long long)((p.T + 255) / 256) * ((p.N * MATS + 255) / 256);
+        if (wide >= 256) many<Wide, MATS>(p, s);
+        else many<Half, MATS>(p, s);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t adapter_workspace_bytes(const moe_adapter_config& c) {
+    return (size_t)split(c).parts * 2 * c.T * c.rank * sizeof(float);
+}
+
+hipError_t launch_adapter(const moe_adapter_config& c, int mats, const uint16_t* x, const uint16_t* const w[2], const uint16_t* const a[2],
+                          const uint16_t* const b[2], const float* scale, const int32_t* adapter_of, const uint16_t* base, uint16_t* y, float* v,
+                          hipStream_t s) {
+    const AdapterArgs p{x, {w[0], w[1]}, {a[0], a[1]}, {b[0], b[1]}, scale, adapter_of, base, v, y, c.T, c.N, c.K, c.adapters, c.rank, 0, 0};
+    return mats == 2 ? launch<2>(p, c, s) : launch<1>(p, c, s);
+}
+
+}  // namespace moe

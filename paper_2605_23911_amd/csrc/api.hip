@@ -63,6 +63,15 @@ moe_status check_train(const moe_config* c) {
     return c->d > kMaxWidth || c->F > kMaxWidth ? MOE_ERR_UNSUPPORTED : MOE_OK;
 }
 
+moe_status check_adapter(const moe_adapter_config* c) {
+    if (c == nullptr) return MOE_ERR_NULL;
+    if (c->T < 0 || c->N < 1 || c->K < 1 || c->adapters < 1 || c->rank < 1) return MOE_ERR_SHAPE;
+    if (c->N % 64 != 0 || c->K % 64 != 0 || c->N > kMaxWidth || c->K > kMaxWidth) return MOE_ERR_UNSUPPORTED;
+    if (c->rank % 8 != 0 || c->rank > 128 || c->adapters > 65536) return MOE_ERR_UNSUPPORTED;
+    if ((unsigned long long)c->T * (unsigned long long)(c->N > c->K ? c->N : c->K) * 2ull >= (1ull << 32)) return MOE_ERR_UNSUPPORTED;
+    return MOE_OK;
+}
+
 moe_status hip_status(hipError_t e) { return e == hipSuccess ? MOE_OK : MOE_ERR_HIP; }
 
 
@@ -420,6 +429,39 @@ moe_status moe_combine_backward(const moe_config* c, const void* dy, const void*
     if (c->T == 0) return MOE_OK;
     return hip_status(launch_combine_backward(*c, (const uint16_t*)dy, (const uint16_t*)y_perm, row_of, topk_w, (uint16_t*)dy_perm, d_topk_w,
                                               (hipStream_t)stream));
+}
+
+size_t moe_adapter_workspace_size(const moe_adapter_config* c) {
+    return check_adapter(c) == MOE_OK ? align_up(adapter_workspace_bytes(*c) + 1) : 0;
+}
+
+moe_status moe_adapter_linear(const moe_adapter_config* c, const void* x, const void* W, const void* A, const void* B, const float* scale,
+                              const int32_t* adapter_of, const void* base, void* y, void* workspace, size_t ws_bytes, void* stream) {
+    const moe_status st = check_adapter(c);
+    if (st != MOE_OK) return st;
+    if (!A || !B || !workspace || (c->T > 0 && (!x || !adapter_of || !y))) return MOE_ERR_NULL;
+    for (const void* p : {x, W, A, B, base, (const void*)y, (const void*)workspace})
+        if (misaligned(p)) return MOE_ERR_ALIGN;
+    if (ws_bytes < moe_adapter_workspace_size(c)) return MOE_ERR_WORKSPACE;
+    if (c->T == 0) return MOE_OK;
+    const uint16_t *const w[2] = {(const uint16_t*)W, nullptr}, *const a[2] = {(const uint16_t*)A, nullptr}, *const b[2] = {(const uint16_t*)B, nullptr};
+    return hip_status(launch_adapter(*c, 1, (const uint16_t*)x, w, a, b, scale, adapter_of, (const uint16_t*)base, (uint16_t*)y, (float*)workspace,
+                                     (hipStream_t)stream));
+}
+
+moe_status moe_adapter_gated_up(const moe_adapter_config* c, const void* x, const void* W_gate, const void* W_up, const void* A_gate, const void* A_up,
+                                const void* B_gate, const void* B_up, const float* scale, const int32_t* adapter_of, void* h, void* workspace,
+                                size_t ws_bytes, void* stream) {
+    const moe_status st = check_adapter(c);
+    if (st != MOE_OK) return st;
+    if (!W_gate || !W_up || !A_gate || !A_up || !B_gate || !B_up || !workspace || (c->T > 0 && (!x || !adapter_of || !h))) return MOE_ERR_NULL;
+    for (const void* p : {x, W_gate, W_up, A_gate, A_up, B_gate, B_up, (const void*)h, (const void*)workspace})
+        if (misaligned(p)) return MOE_ERR_ALIGN;
+    if (ws_bytes < moe_adapter_workspace_size(c)) return MOE_ERR_WORKSPACE;
+    if (c->T == 0) return MOE_OK;
+    const uint16_t *const w[2] = {(const uint16_t*)W_gate, (const uint16_t*)W_up}, *const a[2] = {(const uint16_t*)A_gate, (const uint16_t*)A_up},
+                   *const b[2] = {(const uint16_t*)B_gate, (const uint16_t*)B_up};
+    return hip_status(launch_adapter(*c, 2, (const uint16_t*)x, w, a, b, scale, adapter_of, nullptr, (uint16_t*)h, (float*)workspace, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -149,6 +149,13 @@ hipError_t launch_ffn_backward(const moe_config& c, const FfnGrad& p, hipStream_
 hipError_t launch_combine_backward(const moe_config& c, const uint16_t* dy, const uint16_t* y_perm, const int32_t* row_of, const float* topk_w,
                                    uint16_t* dy_perm, float* d_topk_w, hipStream_t s);
 
+// ---- adapters -----------------------------------------------------------------------------
+size_t adapter_workspace_bytes(const moe_adapter_config& c);
+// mats: 1 (w[0], a[0], b[0]; base may be null, so may w[0]) or 2, the gated pair.  v: the workspace.
+hipError_t launch_adapter(const moe_adapter_config& c, int mats, const uint16_t* x, const uint16_t* const w[2], const uint16_t* const a[2],
+                          const uint16_t* const b[2], const float* scale, const int32_t* adapter_of, const uint16_t* base, uint16_t* y, float* v,
+                          hipStream_t s);
+
 // Many experts with a few rows each (Qwen2-MoE and DeepSeek-V3 shapes at up to 128 tokens): a
 // projection is thousands of short workgroups that stream a weight panel each, and what a CU
 // loses between two of them (schedule look-up, first loads, epilogue, launch of the next: ~5 us
