@@ -23,6 +23,8 @@ struct AdapterArgs {
     int parts, lists;                 // low_rank_kernel: pieces of K, workgroups per token block
 };
 
+constexpr int kThreads = 512, kWaves = kThreads / kWave;       // of the kernels that are not tiled
+
 __device__ __forceinline__ bf16x8 zeros8() { return bf16x8{0, 0, 0, 0, 0, 0, 0, 0}; }
 // Adapter of a token; -1 where it has none (an id outside 0 .. n - 1 means that too).
 __device__ __forceinline__ int adapter_of(const AdapterArgs& p, int t) {
@@ -33,13 +35,13 @@ __device__ __forceinline__ int adapter_of(const AdapterArgs& p, int t) {
 // v: a workgroup takes 32 tokens, one piece of K, and of the adapters that occur in the block every lists-th.  Its eight wavefronts split the
 // piece again and are joined through LDS.  Bound by reading A (once per block of 32 tokens that has the adapter).
 template <int RB, int MATS>
-__global__ __launch_bounds__(kMmaThreads) void low_rank_kernel(AdapterArgs p) {
-    __shared__ float part[kMmaWaves][32][RB * 32 + 1];
+__global__ __launch_bounds__(kThreads) void low_rank_kernel(AdapterArgs p) {
+    __shared__ float part[kWaves][32][RB * 32 + 1];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, r = lane & 31, half = lane >> 5;
     const int block = blockIdx.x / (p.lists * p.parts), rest = blockIdx.x % (p.lists * p.parts), list = rest / p.parts, piece = rest % p.parts;
     const int t0 = block * 32, t = t0 + r;
-    const int steps = p.K / 16, each = (steps + p.parts * kMmaWaves - 1) / (p.parts * kMmaWaves);
-    const int s0 = (piece * kMmaWaves + wave) * each, s1 = s0 + each < steps ? s0 + each : steps;
+    const int steps = p.K / 16, each = (steps + p.parts * kWaves - 1) / (p.parts * kWaves);
+    const int s0 = (piece * kWaves + wave) * each, s1 = s0 + each < steps ? s0 + each : steps;
     const int id = adapter_of(p, t);
     unsigned long long left = __ballot(id >= 0) & 0xffffffffull;
     const uint16_t* x = p.x + (size_t)(t < p.T ? t : p.T - 1) * p.K + half * 8;
@@ -63,28 +65,30 @@ __global__ __launch_bounds__(kMmaThreads) void low_rank_kernel(AdapterArgs p) {
                 const int row = b * 32 + r;
                 rows[m][b] = p.a[m] + ((size_t)a * p.rank + (row < p.rank ? row : p.rank - 1)) * p.K + half * 8;
             }
-        auto step = [&](int s, auto count) {
-            constexpr int U = decltype(count)::value;            // steps whose loads are under way at once
+        // U steps' loads are under way at once; those past the end are zeros on both sides
+        constexpr int LOADS = 1 + MATS * RB, U = LOADS <= 3 ? 8 : LOADS <= 5 ? 4 : 2;
+        for (int s = s0; s < s1; s += U) {
             bf16x8 fx[U], fa[U][MATS][RB];
 #pragma unroll
             for (int i = 0; i < U; ++i) {
-                fx[i] = *reinterpret_cast<const bf16x8*>(x + (s + i) * 16);
+                const int at = (s + i < s1 ? s + i : s1 - 1) * 16;
+                fx[i] = *reinterpret_cast<const bf16x8*>(x + at);
 #pragma unroll
                 for (int m = 0; m < MATS; ++m)
 #pragma unroll
-                    for (int b = 0; b < RB; ++b) fa[i][m][b] = *reinterpret_cast<const bf16x8*>(rows[m][b] + (s + i) * 16);
+                    for (int b = 0; b < RB; ++b) fa[i][m][b] = *reinterpret_cast<const bf16x8*>(rows[m][b] + at);
             }
+            __builtin_amdgcn_sched_barrier(0);     // else the compiler waits for each load before it issues the next, to save registers
 #pragma unroll
-            for (int i = 0; i < U; ++i)
+            for (int i = 0; i < U; ++i) {
+                const bool in = s + i < s1;
+                const bf16x8 vx = in ? fx[i] : zeros8();
 #pragma unroll
                 for (int m = 0; m < MATS; ++m)
 #pragma unroll
-                    for (int b = 0; b < RB; ++b) acc[m][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i][m][b], fx[i], acc[m][b], 0, 0, 0);
-        };
-        constexpr int U = MATS * RB >= 4 ? 4 : 8;
-        int s = s0;
-        for (; s + U <= s1; s += U) step(s, std::integral_constant<int, U>{});
-        for (; s < s1; ++s) step(s, std::integral_constant<int, 1>{});
+                    for (int b = 0; b < RB; ++b) acc[m][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(in ? fa[i][m][b] : zeros8(), vx, acc[m][b], 0, 0, 0);
+            }
+        }
         const float scale = p.scale ? p.scale[a] : 1.0f;
         const unsigned here = (unsigned)__ballot(mine);          // the block's tokens with this adapter
 #pragma unroll
@@ -95,12 +99,12 @@ __global__ __launch_bounds__(kMmaThreads) void low_rank_kernel(AdapterArgs p) {
 #pragma unroll
                 for (int q = 0; q < 16; ++q) part[wave][r][b * 32 + (q / 4) * 8 + half * 4 + q % 4] = acc[m][b][q];
             __syncthreads();
-            for (int j = threadIdx.x; j < 32 * p.rank; j += kMmaThreads) {
+            for (int j = threadIdx.x; j < 32 * p.rank; j += kThreads) {
                 const int row = j / p.rank, c = j % p.rank;
                 if (!((here >> row) & 1)) continue;
                 float sum = 0.0f;
 #pragma unroll
-                for (int w = 0; w < kMmaWaves; ++w) sum += part[w][row][c];
+                for (int w = 0; w < kWaves; ++w) sum += part[w][row][c];
                 p.v[(((size_t)piece * MATS + m) * p.T + t0 + row) * p.rank + c] = sum * scale;
             }
         }
@@ -134,9 +138,10 @@ __device__ __forceinline__ float silu(float g) { return g * __builtin_amdgcn_rcp
 
 constexpr int kMaxRank = 128;
 
+
 // Many tokens: tiles of the projection as in ffn_train.hip, then the adapters of the tile's tokens.
 template <class S, int MATS>
-__global__ __launch_bounds__(kMmaThreads) void adapter_rows_kernel(AdapterArgs p) {
+__global__ __launch_bounds__(S::THREADS, 2) void adapter_rows_kernel(AdapterArgs p) {
     constexpr int FB = S::BN / MATS, kRow = kMaxRank * 2 + 16, kV = MATS * S::BM * kRow;     // bytes of a token's v in LDS
     __shared__ __attribute__((aligned(1024))) char lds[(S::kLds > kV ? S::kLds : kV) + S::BM * 4];
     const int tm_n = (p.T + S::BM - 1) / S::BM, tn_n = (p.N + FB - 1) / FB;
@@ -148,93 +153,94 @@ __global__ __launch_bounds__(kMmaThreads) void adapter_rows_kernel(AdapterArgs p
     const int wm = wave / S::WN, wn = wave % S::WN;
     const int t0 = tm * S::BM, rows = p.T - t0 < S::BM ? p.T - t0 : S::BM, n0 = tn * FB, cols = p.N - n0 < FB ? p.N - n0 : FB;
     int32_t* const ids = reinterpret_cast<int32_t*>(lds + (S::kLds > kV ? S::kLds : kV));
-    for (int i = tid; i < S::BM; i += kMmaThreads) ids[i] = adapter_of(p, t0 + i);
-    Acc<S> acc;
-    clear<S>(acc);
-    {
-        const bool second = MATS == 2 && wave >= kMmaWaves / 2;
-        Loader<S::BM, true> la;
-        Loader<S::BN, true> lb;
-        la.init(p.K, wave, lane);
-        lb.init(p.K, wave, lane, second ? FB : 0);
-        const uint16_t* w = second ? p.w[1] : p.w[0];
-        multiply<S, true, true>(acc, Stream<true>::make(p.x + (size_t)t0 * p.K, p.K, rows, 0), Stream<true>::make(w + (size_t)n0 * p.K, p.K, cols, 0),
-                                la, lb, w ? p.K / kMmaK : 0, lds);
-    }
-    // What the rest derives from the thread's number is worked out here, not held in registers through the reduction.
-    int again = threadIdx.x;
-    asm volatile("" : "+v"(again));
-    const int tid2 = again, lane2 = again % kWave;
-    // the tile's v as bf16
-    for (int j = tid2; j < MATS * S::BM * (p.rank / 8); j += kMmaThreads) {
-        const int c = j % (p.rank / 8), row = j / (p.rank / 8) % S::BM, m = j / (p.rank / 8) / S::BM;
-        if (ids[row] >= 0) *reinterpret_cast<bf16x8*>(lds + (m * S::BM + row) * kRow + c * 16) = low_rank8(p, MATS, m, t0 + row, c * 8);
-    }
-    __syncthreads();
-    {
-        const int r = lane2 & 31, half = lane2 >> 5, c0 = wn * S::NB * 32, m2 = MATS == 2 && c0 >= FB ? 1 : 0;
-        int id[S::MB];
-        unsigned left[S::MB], any = 0;
-#pragma unroll
-        for (int m = 0; m < S::MB; ++m) {
-            id[m] = ids[(wm * S::MB + m) * 32 + r];
-            left[m] = (unsigned)__ballot(id[m] >= 0);
-            any |= left[m];
+    for (int i = tid; i < S::BM; i += S::THREADS) ids[i] = adapter_of(p, t0 + i);
+    by_height<S>(rows, [&](auto height) {
+        constexpr int MB = decltype(height)::value;
+        Acc<S, MB> acc;
+        clear<S, MB>(acc);
+        {
+            const bool second = MATS == 2 && wave >= S::WAVES / 2;
+            typename S::template LoadA<true> la;
+            typename S::template LoadB<true> lb;
+            la.init(p.K, wave, lane);
+            lb.init(p.K, wave, lane, second ? FB : 0);
+            const uint16_t* w = second ? p.w[1] : p.w[0];
+            multiply<S, MB, true, true>(acc, Stream<true, S::BK>::make(p.x + (size_t)t0 * p.K, p.K, rows, p.K), Stream<true, S::BK>::make(w + (size_t)n0 * p.K, p.K, cols, p.K),
+                                    la, lb, w ? p.K / S::BK : 0, lds);
         }
-        const uint16_t* brow[S::NB];
-#pragma unroll
-        for (int n = 0; n < S::NB; ++n) {
-            int col = n0 + c0 - m2 * FB + n * 32 + r;
-            brow[n] = p.b[m2] + (size_t)(col < p.N ? col : p.N - 1) * p.rank;
+        // What the rest derives from the thread's number is worked out here, not held in registers through the reduction.
+        const int tid2 = body_thread(), lane2 = tid2 % kWave;
+        // the tile's v as bf16
+        for (int j = tid2; j < MATS * S::BM * (p.rank / 8); j += S::THREADS) {
+            const int c = j % (p.rank / 8), row = j / (p.rank / 8) % S::BM, m = j / (p.rank / 8) / S::BM;
+            if (ids[row] >= 0) *reinterpret_cast<bf16x8*>(lds + (m * S::BM + row) * kRow + c * 16) = low_rank8(p, MATS, m, t0 + row, c * 8);
         }
-        while (any) {
-            int a = -1;
-#pragma unroll
-            for (int m = S::MB - 1; m >= 0; --m)
-                if (left[m]) a = __builtin_amdgcn_readlane(id[m], __builtin_ctz(left[m]));
-            unsigned here[S::MB];
-            any = 0;
-#pragma unroll
-            for (int m = 0; m < S::MB; ++m) {
-                here[m] = (unsigned)__ballot(id[m] == a);
-                left[m] &= ~here[m];
+        __syncthreads();
+        {
+            const int r = lane2 & 31, half = lane2 >> 5, c0 = wn * S::NB * 32, m2 = MATS == 2 && c0 >= FB ? 1 : 0;
+            int id[MB];
+            unsigned left[MB], any = 0;
+    #pragma unroll
+            for (int m = 0; m < MB; ++m) {
+                id[m] = ids[(wm * MB + m) * 32 + r];
+                left[m] = (unsigned)__ballot(id[m] >= 0);
                 any |= left[m];
             }
-            for (int c = 0; c < p.rank; c += 16) {
-                const bool in = c + half * 8 < p.rank;
-                bf16x8 fb[S::NB];
-#pragma unroll
-                for (int n = 0; n < S::NB; ++n)
-                    fb[n] = in ? *reinterpret_cast<const bf16x8*>(brow[n] + (size_t)a * p.N * p.rank + c + half * 8) : zeros8();
-#pragma unroll
-                for (int m = 0; m < S::MB; ++m) {
-                    if (!here[m]) continue;
-                    const bf16x8 fv = in && id[m] == a
-                        ? *reinterpret_cast<const bf16x8*>(lds + (m2 * S::BM + (wm * S::MB + m) * 32 + r) * kRow + (c + half * 8) * 2) : zeros8();
-#pragma unroll
-                    for (int n = 0; n < S::NB; ++n) keep_mine<f32x16>(acc[n][m], __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[n], fv, acc[n][m], 0, 0, 0), id[m] == a);
+            const uint16_t* brow[S::NB];
+    #pragma unroll
+            for (int n = 0; n < S::NB; ++n) {
+                int col = n0 + c0 - m2 * FB + n * 32 + r;
+                brow[n] = p.b[m2] + (size_t)(col < p.N ? col : p.N - 1) * p.rank;
+            }
+            while (any) {
+                int a = -1;
+    #pragma unroll
+                for (int m = MB - 1; m >= 0; --m)
+                    if (left[m]) a = __builtin_amdgcn_readlane(id[m], __builtin_ctz(left[m]));
+                unsigned here[MB];
+                any = 0;
+    #pragma unroll
+                for (int m = 0; m < MB; ++m) {
+                    here[m] = (unsigned)__ballot(id[m] == a);
+                    left[m] &= ~here[m];
+                    any |= left[m];
+                }
+                for (int c = 0; c < p.rank; c += 16) {
+                    const bool in = c + half * 8 < p.rank;
+                    bf16x8 fb[S::NB];
+    #pragma unroll
+                    for (int n = 0; n < S::NB; ++n)
+                        fb[n] = in ? *reinterpret_cast<const bf16x8*>(brow[n] + (size_t)a * p.N * p.rank + c + half * 8) : zeros8();
+    #pragma unroll
+                    for (int m = 0; m < MB; ++m) {
+                        if (!here[m]) continue;
+                        const bf16x8 fv = in && id[m] == a
+                            ? *reinterpret_cast<const bf16x8*>(lds + (m2 * S::BM + (wm * MB + m) * 32 + r) * kRow + (c + half * 8) * 2) : zeros8();
+    #pragma unroll
+                        for (int n = 0; n < S::NB; ++n) keep_mine<f32x16>(acc[n][m], __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[n], fv, acc[n][m], 0, 0, 0), id[m] == a);
+                    }
                 }
             }
         }
-    }
-    __syncthreads();
-    by_rows<S, FB / 8>(acc, lds, [&](int r, int c, const float* row) {
-        if (r >= rows || c * 8 >= cols) return;
-        float v[8];
-        load8(row + c * 8, v);
-        const size_t at = (size_t)(t0 + r) * p.N + n0 + c * 8;
-        if constexpr (MATS == 2) {
-            float u[8];
-            load8(row + FB + c * 8, u);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = silu(v[i]) * u[i];
-        } else if (p.base) {
-            float o[8];
-            unpack8(*reinterpret_cast<const u32x4_t*>(p.base + at), o);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += o[i];
-        }
-        *reinterpret_cast<u32x4_t*>(p.y + at) = pack8(v);
+        __syncthreads();
+        by_rows<S, FB / 8>(acc, lds, [&](int r, int c, const float* row) {
+            if (r >= rows || c * 8 >= cols) return;
+            float v[8];
+            load8(row + c * 8, v);
+            const size_t at = (size_t)(t0 + r) * p.N + n0 + c * 8;
+            if constexpr (MATS == 2) {
+                float u[8];
+                load8(row + FB + c * 8, u);
+    #pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = silu(v[i]) * u[i];
+            } else if (p.base) {
+                float o[8];
+                unpack8(*reinterpret_cast<const u32x4_t*>(p.base + at), o);
+    #pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] += o[i];
+            }
+            *reinterpret_cast<u32x4_t*>(p.y + at) = pack8(v);
+        });
     });
 }
 
@@ -242,8 +248,8 @@ __global__ __launch_bounds__(kMmaThreads) void adapter_rows_kernel(AdapterArgs p
 // eight wavefronts split K, and the adapters that occur, and are joined through LDS.  Weights go from memory to registers: 16x16x32
 // MFMAs, so that four lanes read 64 consecutive bytes of a weight row.
 template <int MB, int NB, int MATS>
-__global__ __launch_bounds__(kMmaThreads) void adapter_few_kernel(AdapterArgs p) {
-    constexpr int kRow = kMaxRank * 2 + 16, kV = MATS * MB * 16 * kRow, kPart = kMmaWaves * MATS * NB * MB * 64 * 16;
+__global__ __launch_bounds__(kThreads, 4) void adapter_few_kernel(AdapterArgs p) {
+    constexpr int kRow = kMaxRank * 2 + 16, kV = MATS * MB * 16 * kRow, kPart = kWaves / 2 * MATS * NB * MB * 64 * 16;
     __shared__ __attribute__((aligned(1024))) char lds[kPart > kV ? kPart : kV];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid % kWave, r = lane & 15, quad = lane >> 4;
     const int n0 = blockIdx.x * (NB * 16);
@@ -254,47 +260,51 @@ __global__ __launch_bounds__(kMmaThreads) void adapter_few_kernel(AdapterArgs p)
         for (int n = 0; n < NB; ++n)
 #pragma unroll
             for (int b = 0; b < MB; ++b) acc[m][n][b] = f32x4{0, 0, 0, 0};
-    const int steps = p.w[0] ? p.K / 32 : 0, each = (steps + kMmaWaves - 1) / kMmaWaves;
+    const int steps = p.w[0] ? p.K / 32 : 0, each = (steps + kWaves - 1) / kWaves;
     const int s0 = wave * each < steps ? wave * each : steps, s1 = s0 + each < steps ? s0 + each : steps;
-    const uint16_t *wrow[MATS][NB], *xrow[MB];
+    // addresses: what is the same for the wavefront (scalar registers), plus a 32-bit offset per lane
+    const uint32_t wlane = (uint32_t)(r * p.K + quad * 8) * 2u;
+    uint32_t xlane[MB];
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-        const int col = n0 + n * 16 + r;
-#pragma unroll
-        for (int m = 0; m < MATS; ++m) wrow[m][n] = p.w[m] + (size_t)(col < p.N ? col : p.N - 1) * p.K + quad * 8;
-    }
-#pragma unroll
-    for (int b = 0; b < MB; ++b) xrow[b] = p.x + (size_t)(b * 16 + r < p.T ? b * 16 + r : p.T - 1) * p.K + quad * 8;
-    auto step = [&](int s, auto count) {
-        constexpr int U = decltype(count)::value;                // steps whose weights are under way at once
+    for (int b = 0; b < MB; ++b) xlane[b] = (uint32_t)((b * 16 + r < p.T ? b * 16 + r : p.T - 1) * p.K + quad * 8) * 2u;
+    auto wpiece = [&](int m, int n, int s) {
+        const char* base = reinterpret_cast<const char*>(p.w[m] + (size_t)(n0 + n * 16) * p.K + s * 32);
+        return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(base + wlane));
+    };
+    auto xpiece = [&](int b, int s) { return *reinterpret_cast<const bf16x8*>(reinterpret_cast<const char*>(p.x + s * 32) + xlane[b]); };
+    // U steps' loads are under way at once, as many as 128 registers hold; weights past the end are zeros, and so are their tokens
+    constexpr int fit = ((128 - 22) / 4 - MATS * NB * MB) / (MATS * NB + MB), U = fit < 1 ? 1 : fit > 8 ? 8 : fit;
+    for (int s = s0; s < s1; s += U) {
         u32x4_t fw[U][MATS][NB];
-#pragma unroll
-        for (int i = 0; i < U; ++i)
-#pragma unroll
-            for (int m = 0; m < MATS; ++m)
-#pragma unroll
-                for (int n = 0; n < NB; ++n) fw[i][m][n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(wrow[m][n] + (s + i) * 32));
+        bf16x8 fx[U][MB];
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            bf16x8 fx[MB];
-#pragma unroll
-            for (int b = 0; b < MB; ++b) fx[b] = *reinterpret_cast<const bf16x8*>(xrow[b] + (s + i) * 32);
+            const int at = s + i < s1 ? s + i : s1 - 1;
 #pragma unroll
             for (int m = 0; m < MATS; ++m)
 #pragma unroll
-                for (int n = 0; n < NB; ++n)
+                for (int n = 0; n < NB; ++n) fw[i][m][n] = wpiece(m, n, at);
 #pragma unroll
-                    for (int b = 0; b < MB; ++b)
-                        acc[m][n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fw[i][m][n]), fx[b], acc[m][n][b], 0, 0, 0);
+            for (int b = 0; b < MB; ++b) fx[i][b] = xpiece(b, at);
         }
-    };
-    constexpr int U = 8 / (MATS * NB);
-    int s = s0;
-    for (; s + U <= s1; s += U) step(s, std::integral_constant<int, U>{});
-    for (; s < s1; ++s) step(s, std::integral_constant<int, 1>{});
+        __builtin_amdgcn_sched_barrier(0);         // else the compiler waits for each load before it issues the next, to save registers
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const bool in = s + i < s1;
+#pragma unroll
+            for (int b = 0; b < MB; ++b) {
+                const bf16x8 vx = in ? fx[i][b] : zeros8();
+#pragma unroll
+                for (int m = 0; m < MATS; ++m)
+#pragma unroll
+                    for (int n = 0; n < NB; ++n)
+                        acc[m][n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(in ? __builtin_bit_cast(bf16x8, fw[i][m][n]) : zeros8(), vx, acc[m][n][b], 0, 0, 0);
+            }
+        }
+    }
     // v of all tokens as bf16
     const int chunks = p.rank / 8;
-    for (int j = tid; j < MATS * MB * 16 * chunks; j += kMmaThreads) {
+    for (int j = tid; j < MATS * MB * 16 * chunks; j += kThreads) {
         const int c = j % chunks, t = j / chunks % (MB * 16), m = j / chunks / (MB * 16);
         if (adapter_of(p, t) >= 0) *reinterpret_cast<bf16x8*>(lds + (m * MB * 16 + t) * kRow + c * 16) = low_rank8(p, MATS, m, t, c * 8);
     }
@@ -303,53 +313,95 @@ __global__ __launch_bounds__(kMmaThreads) void adapter_few_kernel(AdapterArgs p)
     int idb[MB];
 #pragma unroll
     for (int b = 0; b < MB; ++b) idb[b] = __shfl(id, b * 16 + r, kWave);
-    unsigned long long left = __ballot(id >= 0);
-    for (int i = 0; left != 0; ++i) {
-        const int a = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
-        const unsigned long long here = __ballot(id == a);
-        left &= ~here;
-        if (i % kMmaWaves != wave) continue;
-        for (int c = 0; c < p.rank; c += 32) {
-            const bool in = c + quad * 8 < p.rank;
-            bf16x8 fb[MATS][NB];
+    // This wavefront's adapters: every eighth of those that occur, 32 of the rank at a time; the next piece of B is under way meanwhile.
+    unsigned long long left = __ballot(id >= 0), here = 0;
+    int a = -1, c = 0, seen = 0;
+    auto next = [&] {
+        c += 32;
+        if (a >= 0 && c < p.rank) return;
+        a = -1;
+        c = 0;
+        while (left != 0 && a < 0) {
+            const int first = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+            here = __ballot(id == first);
+            left &= ~here;
+            if (seen++ % kWaves == wave) a = first;
+        }
+    };
+    bf16x8 fb[MATS][NB];
+    auto load = [&] {
+        const bool in = c + quad * 8 < p.rank;
 #pragma unroll
-            for (int m = 0; m < MATS; ++m)
+        for (int m = 0; m < MATS; ++m)
 #pragma unroll
-                for (int n = 0; n < NB; ++n) {
-                    const int col = n0 + n * 16 + r;
-                    fb[m][n] = in ? *reinterpret_cast<const bf16x8*>(p.b[m] + ((size_t)a * p.N + (col < p.N ? col : p.N - 1)) * p.rank + c + quad * 8) : zeros8();
-                }
+            for (int n = 0; n < NB; ++n) {
+                const char* base = reinterpret_cast<const char*>(p.b[m] + ((size_t)a * p.N + n0 + n * 16) * p.rank + c);
+                fb[m][n] = in ? *reinterpret_cast<const bf16x8*>(base + (uint32_t)(r * p.rank + quad * 8) * 2u) : zeros8();
+            }
+    };
+    next();
+    if (a >= 0) load();
+    while (a >= 0) {
+        const int a0 = a, c0 = c;
+        const unsigned long long h0 = here;
+        bf16x8 f0[MATS][NB];
 #pragma unroll
-            for (int b = 0; b < MB; ++b) {
-                if (!((here >> (b * 16)) & 0xffff)) continue;
+        for (int m = 0; m < MATS; ++m)
 #pragma unroll
-                for (int m = 0; m < MATS; ++m) {
-                    const bf16x8 fv = in && idb[b] == a ? *reinterpret_cast<const bf16x8*>(lds + (m * MB * 16 + b * 16 + r) * kRow + (c + quad * 8) * 2) : zeros8();
+            for (int n = 0; n < NB; ++n) f0[m][n] = fb[m][n];
+        next();
+        if (a >= 0) load();
+        __builtin_amdgcn_sched_barrier(0);
+        const bool in = c0 + quad * 8 < p.rank;
 #pragma unroll
-                    for (int n = 0; n < NB; ++n)
-                        keep_mine<f32x4>(acc[m][n][b], __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[m][n], fv, acc[m][n][b], 0, 0, 0), idb[b] == a);
-                }
+        for (int b = 0; b < MB; ++b) {
+            if (!((h0 >> (b * 16)) & 0xffff)) continue;
+#pragma unroll
+            for (int m = 0; m < MATS; ++m) {
+                const bf16x8 fv = in && idb[b] == a0 ? *reinterpret_cast<const bf16x8*>(lds + (m * MB * 16 + b * 16 + r) * kRow + (c0 + quad * 8) * 2) : zeros8();
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+                    keep_mine<f32x4>(acc[m][n][b], __builtin_amdgcn_mfma_f32_16x16x32_bf16(f0[m][n], fv, acc[m][n][b], 0, 0, 0), idb[b] == a0);
             }
         }
     }
     __syncthreads();
+    // join: the upper four wavefronts hand theirs to the lower four, whose sums are added by whoever stores (half the LDS, hence two workgroups per CU)
+    constexpr int kJoin = kWaves / 2;
     f32x4* const part = reinterpret_cast<f32x4*>(lds);       // [wave][matrix][n][b][lane]
+    f32x4* const mine = part + (size_t)(wave % kJoin) * MATS * NB * MB * 64 + lane;
+    if (wave >= kJoin) {
 #pragma unroll
-    for (int m = 0; m < MATS; ++m)
+        for (int m = 0; m < MATS; ++m)
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
+            for (int n = 0; n < NB; ++n)
 #pragma unroll
-            for (int b = 0; b < MB; ++b) part[(((wave * MATS + m) * NB + n) * MB + b) * 64 + lane] = acc[m][n][b];
+                for (int b = 0; b < MB; ++b) mine[((m * NB + n) * MB + b) * 64] = acc[m][n][b];
+    }
     __syncthreads();
-    for (int j = tid; j < NB * MB * 64; j += kMmaThreads) {
+    if (wave < kJoin) {
+#pragma unroll
+        for (int m = 0; m < MATS; ++m)
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int b = 0; b < MB; ++b) {
+                    const f32x4 o = mine[((m * NB + n) * MB + b) * 64];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[m][n][b][i] += o[i];
+                    mine[((m * NB + n) * MB + b) * 64] = acc[m][n][b];
+                }
+    }
+    __syncthreads();
+    for (int j = tid; j < NB * MB * 64; j += kThreads) {
         const int l = j % 64, b = j / 64 % MB, n = j / 64 / MB, t = b * 16 + (l & 15), col = n0 + n * 16 + (l >> 4) * 4;
-        if (t >= p.T || col >= p.N) continue;
+        if (t >= p.T) continue;
         f32x4 v[MATS];
 #pragma unroll
         for (int m = 0; m < MATS; ++m) {
             v[m] = part[((m * NB + n) * MB + b) * 64 + l];
 #pragma unroll
-            for (int w = 1; w < kMmaWaves; ++w) {
+            for (int w = 1; w < kJoin; ++w) {
                 const f32x4 o = part[(((w * MATS + m) * NB + n) * MB + b) * 64 + l];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[m][i] += o[i];
@@ -370,40 +422,43 @@ __global__ __launch_bounds__(kMmaThreads) void adapter_few_kernel(AdapterArgs p)
 
 constexpr int kFewTokens = 64;
 
-// Pieces of K and workgroups per block of 32 tokens of low_rank_kernel.  Every occurring adapter of a block can have a workgroup of its own
-// while that keeps the launch within 4096; K is cut until there is a workgroup per CU, into eight pieces at most, which the
-// projection's kernel adds up, and no finer than 64 elements per wavefront.
+// Pieces of K and workgroups per block of 32 tokens of low_rank_kernel, for about 512 workgroups.  In a decode batch a block has up to 32 adapters, each
+// with a workgroup of its own.  In a prompt it has one or two; there K is cut first, into up to eight pieces (which the projection's kernel adds
+// up), no finer than 64 elements per wavefront.
 struct Split {
     int blocks, lists, parts;
 };
 Split split(const moe_adapter_config& c) {
     Split s;
     s.blocks = (c.T + 31) / 32;
-    s.lists = c.adapters < 32 ? c.adapters : 32;
-    if (c.T < s.lists) s.lists = c.T;
-    while (s.lists > 1 && (long long)s.blocks * s.lists > 4096) s.lists = (s.lists + 1) / 2;
+    const int most = c.adapters < 32 ? (c.adapters < c.T ? c.adapters : c.T) : (c.T < 32 ? c.T : 32);
+    const bool decode = c.T <= kFewTokens;
+    s.lists = decode ? most : 1;
     s.parts = 1;
-    while (s.parts < 8 && (long long)s.blocks * s.lists * s.parts < 256 && c.K >= s.parts * 2 * kMmaWaves * 64) s.parts *= 2;
+    while (s.parts < 8 && s.blocks * s.lists * s.parts < (decode ? 256 : 512) && c.K >= s.parts * 2 * kWaves * 64) s.parts *= 2;
+    if (!decode) s.lists = s.blocks * s.parts * 2 <= 512 ? 512 / (s.blocks * s.parts) : 1;
+    if (s.lists > most) s.lists = most;
     return s;
 }
 
 template <int MATS>
 void low_rank(const AdapterArgs& p, unsigned grid, hipStream_t s) {
     const int rb = (p.rank + 31) / 32;
-    if (rb == 1) hipLaunchKernelGGL((low_rank_kernel<1, MATS>), dim3(grid), dim3(kMmaThreads), 0, s, p);
-    else if (rb == 2) hipLaunchKernelGGL((low_rank_kernel<2, MATS>), dim3(grid), dim3(kMmaThreads), 0, s, p);
-    else hipLaunchKernelGGL((low_rank_kernel<4, MATS>), dim3(grid), dim3(kMmaThreads), 0, s, p);
+    if (rb == 1) hipLaunchKernelGGL((low_rank_kernel<1, MATS>), dim3(grid), dim3(kThreads), 0, s, p);
+    else if (rb == 2) hipLaunchKernelGGL((low_rank_kernel<2, MATS>), dim3(grid), dim3(kThreads), 0, s, p);
+    else hipLaunchKernelGGL((low_rank_kernel<4, MATS>), dim3(grid), dim3(kThreads), 0, s, p);
 }
 
 template <int MB, int MATS>
 void few(const AdapterArgs& p, hipStream_t s) {
-    hipLaunchKernelGGL((adapter_few_kernel<MB, 1, MATS>), dim3((p.N + 15) / 16), dim3(kMmaThreads), 0, s, p);
+    if (p.N >= 32 * 256) hipLaunchKernelGGL((adapter_few_kernel<MB, 2, MATS>), dim3(p.N / 32), dim3(kThreads), 0, s, p);
+    else hipLaunchKernelGGL((adapter_few_kernel<MB, 1, MATS>), dim3(p.N / 16), dim3(kThreads), 0, s, p);
 }
 
 template <class S, int MATS>
 void many(const AdapterArgs& p, hipStream_t s) {
     const long long tiles = (long long)((p.T + S::BM - 1) / S::BM) * ((p.N + S::BN / MATS - 1) / (S::BN / MATS));
-    hipLaunchKernelGGL((adapter_rows_kernel<S, MATS>), dim3(xcd_grid(tiles)), dim3(kMmaThreads), 0, s, p);
+    hipLaunchKernelGGL((adapter_rows_kernel<S, MATS>), dim3(xcd_grid(tiles)), dim3(S::THREADS), 0, s, p);
 }
 
 template <int MATS>
@@ -422,8 +477,7 @@ hipError_t launch(AdapterArgs p, const moe_adapter_config& c, hipStream_t s) {
             default: few<4, MATS>(p, s);
         }
     } else {
-        const long long wide = (long long)((p.T + 255) / 256) * ((p.N * MATS + 255) / 256);
-        if (wide >= 256) many<Wide, MATS>(p, s);
+        if (cost<Wide>(p.T, p.N * MATS) <= cost<Half>(p.T, p.N * MATS)) many<Wide, MATS>(p, s);
         else many<Half, MATS>(p, s);
     }
     return hipGetLastError();

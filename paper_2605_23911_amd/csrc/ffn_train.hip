@@ -5,6 +5,9 @@
 //             dWg = dg^T x, dWu = du^T x, dWd = dy^T h, per expert                                  (launch 3)
 // with SiLU(g) = g s, SiLU'(g) = s (1 + g (1 - s)), s = 1 / (1 + exp(-g)).
 #include "mma_tile.hpp"
+#ifndef BIG
+#define BIG Pair
+#endif
 
 namespace moe {
 
@@ -23,33 +26,36 @@ struct GatedArgs {
 // Tile: BM rows x BN / 2 features of both projections: the first half of B's rows are the gate's, the second the up projection's,
 // so that one copy of the token tile in LDS feeds both and the activation needs nothing but the tile.
 template <class S>
-__global__ __launch_bounds__(kMmaThreads) void gated_keep_kernel(GatedArgs a) {
+__global__ __launch_bounds__(S::THREADS, 2) void gated_keep_kernel(GatedArgs a) {
     __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
     constexpr int FB = S::BN / 2;
     RowTile t;
     if (!find_tile(a.offsets, a.E, S::BM, (a.F + FB - 1) / FB, t)) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int f0 = t.n * FB, features = a.F - f0 < FB ? a.F - f0 : FB;
-    const bool up = wave >= kMmaWaves / 2;
-    Loader<S::BM, true> la;
-    Loader<S::BN, true> lb;
+    const bool up = wave >= S::WAVES / 2;
+    typename S::template LoadA<true> la;
+    typename S::template LoadB<true> lb;
     la.init(a.d, wave, lane);
     lb.init(a.d, wave, lane, up ? FB : 0);
-    Acc<S> acc;
-    clear<S>(acc);
-    multiply<S, true, true>(acc, Stream<true>::make(a.x + (size_t)t.row0 * a.d, a.d, t.rows, 0),
-                            Stream<true>::make((up ? a.wu : a.wg) + ((size_t)t.e * a.F + f0) * a.d, a.d, features, 0), la, lb, a.d / kMmaK, lds);
-    by_rows<S, FB / 8>(acc, lds, [&](int r, int c, const float* row) {
-        if (r >= t.rows || c * 8 >= features) return;
-        float g[8], u[8], h[8];
-        load8(row + c * 8, g);
-        load8(row + FB + c * 8, u);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) h[i] = g[i] * sigmoid(g[i]) * u[i];
-        const size_t at = (size_t)(t.row0 + r) * a.F + f0 + c * 8;
-        *reinterpret_cast<u32x4_t*>(a.g + at) = pack8(g);
-        *reinterpret_cast<u32x4_t*>(a.u + at) = pack8(u);
-        *reinterpret_cast<u32x4_t*>(a.h + at) = pack8(h);
+    by_height<S>(t.rows, [&](auto height) {
+        constexpr int MB = decltype(height)::value;
+        Acc<S, MB> acc;
+        clear<S, MB>(acc);
+        multiply<S, MB, true, true>(acc, Stream<true, S::BK>::make(a.x + (size_t)t.row0 * a.d, a.d, t.rows, a.d),
+                                Stream<true, S::BK>::make((up ? a.wu : a.wg) + ((size_t)t.e * a.F + f0) * a.d, a.d, features, a.d), la, lb, a.d / S::BK, lds);
+        by_rows<S, FB / 8>(acc, lds, [&](int r, int c, const float* row) {
+            if (r >= t.rows || c * 8 >= features) return;
+            float g[8], u[8], h[8];
+            load8(row + c * 8, g);
+            load8(row + FB + c * 8, u);
+    #pragma unroll
+            for (int i = 0; i < 8; ++i) h[i] = g[i] * sigmoid(g[i]) * u[i];
+            const size_t at = (size_t)(t.row0 + r) * a.F + f0 + c * 8;
+            *reinterpret_cast<u32x4_t*>(a.g + at) = pack8(g);
+            *reinterpret_cast<u32x4_t*>(a.u + at) = pack8(u);
+            *reinterpret_cast<u32x4_t*>(a.h + at) = pack8(h);
+        });
     });
 }
 
@@ -65,70 +71,76 @@ struct GradArgs {
 // dh = dy Wd, and from the tile's dh and the kept g and u: dg, du and h.  dg and du are rounded to bf16, as the operands that the
 // products of launches 2 and 3 take; g and u are the rounded values that the forward pass kept.
 template <class S>
-__global__ __launch_bounds__(kMmaThreads) void gated_grad_kernel(GradArgs a) {
+__global__ __launch_bounds__(S::THREADS, 2) void gated_grad_kernel(GradArgs a) {
     __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
     RowTile t;
     if (!find_tile(a.offsets, a.E, S::BM, (a.F + S::BN - 1) / S::BN, t)) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int f0 = t.n * S::BN;
-    Loader<S::BM, true> la;
-    Loader<S::BN, false> lb;
+    typename S::template LoadA<true> la;
+    typename S::template LoadB<false> lb;
     la.init(a.d, wave, lane);
     lb.init(a.F, wave, lane);
-    Acc<S> acc;
-    clear<S>(acc);
-    multiply<S, true, false>(acc, Stream<true>::make(a.dy + (size_t)t.row0 * a.d, a.d, t.rows, 0),
-                             Stream<false>::make(a.wd + (size_t)t.e * a.d * a.F, a.F, f0, a.d), la, lb, a.d / kMmaK, lds);
-    by_rows<S, S::BN / 8>(acc, lds, [&](int r, int c, const float* row) {
-        if (r >= t.rows || f0 + c * 8 >= a.F) return;
-        const size_t at = (size_t)(t.row0 + r) * a.F + f0 + c * 8;
-        float dh[8], g[8], u[8], dg[8], du[8], h[8];
-        unpack8(*reinterpret_cast<const u32x4_t*>(a.g + at), g);
-        unpack8(*reinterpret_cast<const u32x4_t*>(a.u + at), u);
-        load8(row + c * 8, dh);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float s = sigmoid(g[i]), act = g[i] * s;
-            dg[i] = dh[i] * u[i] * (s + act * (1.0f - s));
-            du[i] = dh[i] * act;
-            h[i] = act * u[i];
-        }
-        *reinterpret_cast<u32x4_t*>(a.dg + at) = pack8(dg);
-        *reinterpret_cast<u32x4_t*>(a.du + at) = pack8(du);
-        *reinterpret_cast<u32x4_t*>(a.h + at) = pack8(h);
+    by_height<S>(t.rows, [&](auto height) {
+        constexpr int MB = decltype(height)::value;
+        Acc<S, MB> acc;
+        clear<S, MB>(acc);
+        multiply<S, MB, true, false>(acc, Stream<true, S::BK>::make(a.dy + (size_t)t.row0 * a.d, a.d, t.rows, a.d),
+                                 Stream<false, S::BK>::make(a.wd + (size_t)t.e * a.d * a.F, a.F, f0, a.d), la, lb, a.d / S::BK, lds);
+        by_rows<S, S::BN / 8>(acc, lds, [&](int r, int c, const float* row) {
+            if (r >= t.rows || f0 + c * 8 >= a.F) return;
+            const size_t at = (size_t)(t.row0 + r) * a.F + f0 + c * 8;
+            float dh[8], g[8], u[8], dg[8], du[8], h[8];
+            unpack8(*reinterpret_cast<const u32x4_t*>(a.g + at), g);
+            unpack8(*reinterpret_cast<const u32x4_t*>(a.u + at), u);
+            load8(row + c * 8, dh);
+    #pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float s = sigmoid(g[i]), act = g[i] * s;
+                dg[i] = dh[i] * u[i] * (s + act * (1.0f - s));
+                du[i] = dh[i] * act;
+                h[i] = act * u[i];
+            }
+            *reinterpret_cast<u32x4_t*>(a.dg + at) = pack8(dg);
+            *reinterpret_cast<u32x4_t*>(a.du + at) = pack8(du);
+            *reinterpret_cast<u32x4_t*>(a.h + at) = pack8(h);
+        });
     });
 }
 
 // dx = dg Wg + du Wu: one sum over 2 F.
 template <class S>
-__global__ __launch_bounds__(kMmaThreads) void rows_grad_kernel(GradArgs a) {
+__global__ __launch_bounds__(S::THREADS, 2) void rows_grad_kernel(GradArgs a) {
     __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
     RowTile t;
     if (!find_tile(a.offsets, a.E, S::BM, (a.d + S::BN - 1) / S::BN, t)) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int n0 = t.n * S::BN;
-    Loader<S::BM, true> la;
-    Loader<S::BN, false> lb;
+    typename S::template LoadA<true> la;
+    typename S::template LoadB<false> lb;
     la.init(a.F, wave, lane);
     lb.init(a.d, wave, lane);
-    Acc<S> acc;
-    clear<S>(acc);
-#pragma unroll 1
-    for (int m = 0; m < 2; ++m)
-        multiply<S, true, false>(acc, Stream<true>::make((m ? a.du : a.dg) + (size_t)t.row0 * a.F, a.F, t.rows, 0),
-                                 Stream<false>::make((m ? a.wu : a.wg) + (size_t)t.e * a.F * a.d, a.d, n0, a.F), la, lb, a.F / kMmaK, lds);
-    by_rows<S, S::BN / 8>(acc, lds, [&](int r, int c, const float* row) {
-        if (r >= t.rows || n0 + c * 8 >= a.d) return;
-        float v[8];
-        load8(row + c * 8, v);
-        *reinterpret_cast<u32x4_t*>(a.dx + (size_t)(t.row0 + r) * a.d + n0 + c * 8) = pack8(v);
+    by_height<S>(t.rows, [&](auto height) {
+        constexpr int MB = decltype(height)::value;
+        Acc<S, MB> acc;
+        clear<S, MB>(acc);
+    #pragma unroll 1
+        for (int m = 0; m < 2; ++m)
+            multiply<S, MB, true, false>(acc, Stream<true, S::BK>::make((m ? a.du : a.dg) + (size_t)t.row0 * a.F, a.F, t.rows, a.F),
+                                     Stream<false, S::BK>::make((m ? a.wu : a.wg) + (size_t)t.e * a.F * a.d, a.d, n0, a.F), la, lb, a.F / S::BK, lds);
+        by_rows<S, S::BN / 8>(acc, lds, [&](int r, int c, const float* row) {
+            if (r >= t.rows || n0 + c * 8 >= a.d) return;
+            float v[8];
+            load8(row + c * 8, v);
+            *reinterpret_cast<u32x4_t*>(a.dx + (size_t)(t.row0 + r) * a.d + n0 + c * 8) = pack8(v);
+        });
     });
 }
 
 // dW[m, n] = sum over the expert's rows of P[row, m] Q[row, n] for the three matrices in one launch (the tails of three would add
 // up): tiles [expert][matrix][patch].  An expert without rows gets zeros.
 template <class S>
-__global__ __launch_bounds__(kMmaThreads) void weights_grad_kernel(GradArgs a) {
+__global__ __launch_bounds__(S::THREADS, 2) void weights_grad_kernel(GradArgs a) {
     __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
     const int tm_f = (a.F + S::BM - 1) / S::BM, tn_d = (a.d + S::BN - 1) / S::BN;     // gate, up: [F, d]
     const int tm_d = (a.d + S::BM - 1) / S::BM, tn_f = (a.F + S::BN - 1) / S::BN;     // down: [d, F]
@@ -146,40 +158,43 @@ __global__ __launch_bounds__(kMmaThreads) void weights_grad_kernel(GradArgs a) {
     const uint16_t* Q = which < 2 ? a.x : a.h;
     const int row0 = a.offsets[e], rows = a.offsets[e + 1] - row0;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-    Loader<S::BM, false> la;
-    Loader<S::BN, false> lb;
+    typename S::template LoadA<false> la;
+    typename S::template LoadB<false> lb;
     la.init(M, wave, lane);
     lb.init(N, wave, lane);
-    Acc<S> acc;
-    clear<S>(acc);
-    multiply<S, false, false>(acc, Stream<false>::make(P + (size_t)row0 * M, M, m0, rows), Stream<false>::make(Q + (size_t)row0 * N, N, n0, rows),
-                              la, lb, (rows + kMmaK - 1) / kMmaK, lds);
-    void* const out = which == 0 ? a.dwg : which == 1 ? a.dwu : a.dwd;
-    by_rows<S, S::BN / 8>(acc, lds, [&](int r, int c, const float* row) {
-        if (m0 + r >= M || n0 + c * 8 >= N) return;
-        const size_t at = ((size_t)e * M + m0 + r) * N + n0 + c * 8;
-        float v[8];
-        load8(row + c * 8, v);
-        if (a.f32) {
-            float* dst = reinterpret_cast<float*>(out) + at;
-            if (a.add) {
-                float o[8];
-                load8(dst, o);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] += o[i];
+    by_height<S>(M - m0, [&](auto height) {
+        constexpr int MB = decltype(height)::value;
+        Acc<S, MB> acc;
+        clear<S, MB>(acc);
+        multiply<S, MB, false, false>(acc, Stream<false, S::BK>::make(P + (size_t)row0 * M, M, m0, rows), Stream<false, S::BK>::make(Q + (size_t)row0 * N, N, n0, rows),
+                                  la, lb, (rows + S::BK - 1) / S::BK, lds);
+        void* const out = which == 0 ? a.dwg : which == 1 ? a.dwu : a.dwd;
+        by_rows<S, S::BN / 8>(acc, lds, [&](int r, int c, const float* row) {
+            if (m0 + r >= M || n0 + c * 8 >= N) return;
+            const size_t at = ((size_t)e * M + m0 + r) * N + n0 + c * 8;
+            float v[8];
+            load8(row + c * 8, v);
+            if (a.f32) {
+                float* dst = reinterpret_cast<float*>(out) + at;
+                if (a.add) {
+                    float o[8];
+                    load8(dst, o);
+    #pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] += o[i];
+                }
+                *reinterpret_cast<f32x4*>(dst) = f32x4{v[0], v[1], v[2], v[3]};
+                *reinterpret_cast<f32x4*>(dst + 4) = f32x4{v[4], v[5], v[6], v[7]};
+            } else {
+                u32x4_t* dst = reinterpret_cast<u32x4_t*>(reinterpret_cast<uint16_t*>(out) + at);
+                if (a.add) {
+                    float o[8];
+                    unpack8(*dst, o);
+    #pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] += o[i];
+                }
+                *dst = pack8(v);
             }
-            *reinterpret_cast<f32x4*>(dst) = f32x4{v[0], v[1], v[2], v[3]};
-            *reinterpret_cast<f32x4*>(dst + 4) = f32x4{v[4], v[5], v[6], v[7]};
-        } else {
-            u32x4_t* dst = reinterpret_cast<u32x4_t*>(reinterpret_cast<uint16_t*>(out) + at);
-            if (a.add) {
-                float o[8];
-                unpack8(*dst, o);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] += o[i];
-            }
-            *dst = pack8(v);
-        }
+        });
     });
 }
 
@@ -190,20 +205,20 @@ __global__ __launch_bounds__(256) void zero_kernel(u32x4_t* p, size_t n) {
 template <class S>
 void go_keep(const GatedArgs& a, const moe_config& c, hipStream_t s) {
     const long long tiles = most_blocks(c, S::BM) * ((a.F + S::BN / 2 - 1) / (S::BN / 2));
-    hipLaunchKernelGGL(gated_keep_kernel<S>, dim3(xcd_grid(tiles)), dim3(kMmaThreads), 0, s, a);
+    hipLaunchKernelGGL(gated_keep_kernel<S>, dim3(xcd_grid(tiles)), dim3(S::THREADS), 0, s, a);
 }
 template <class S>
 void go_gated_grad(const GradArgs& a, const moe_config& c, hipStream_t s) {
-    hipLaunchKernelGGL(gated_grad_kernel<S>, dim3(xcd_grid(most_blocks(c, S::BM) * ((a.F + S::BN - 1) / S::BN))), dim3(kMmaThreads), 0, s, a);
+    hipLaunchKernelGGL(gated_grad_kernel<S>, dim3(xcd_grid(most_blocks(c, S::BM) * ((a.F + S::BN - 1) / S::BN))), dim3(S::THREADS), 0, s, a);
 }
 template <class S>
 void go_rows_grad(const GradArgs& a, const moe_config& c, hipStream_t s) {
-    hipLaunchKernelGGL(rows_grad_kernel<S>, dim3(xcd_grid(most_blocks(c, S::BM) * ((a.d + S::BN - 1) / S::BN))), dim3(kMmaThreads), 0, s, a);
+    hipLaunchKernelGGL(rows_grad_kernel<S>, dim3(xcd_grid(most_blocks(c, S::BM) * ((a.d + S::BN - 1) / S::BN))), dim3(S::THREADS), 0, s, a);
 }
 template <class S>
 void go_weights_grad(const GradArgs& a, hipStream_t s) {
     const long long fd = (long long)((a.F + S::BM - 1) / S::BM) * ((a.d + S::BN - 1) / S::BN), df = (long long)((a.d + S::BM - 1) / S::BM) * ((a.F + S::BN - 1) / S::BN);
-    hipLaunchKernelGGL(weights_grad_kernel<S>, dim3(xcd_grid(a.E * ((a.dwg ? fd : 0) + (a.dwu ? fd : 0) + (a.dwd ? df : 0)))), dim3(kMmaThreads), 0, s, a);
+    hipLaunchKernelGGL(weights_grad_kernel<S>, dim3(xcd_grid(a.E * ((a.dwg ? fd : 0) + (a.dwu ? fd : 0) + (a.dwd ? df : 0)))), dim3(S::THREADS), 0, s, a);
 }
 
 }  // namespace
@@ -212,7 +227,7 @@ hipError_t launch_gated_keep(const moe_config& c, const uint16_t* x_rows, const 
                              uint16_t* g, uint16_t* u, uint16_t* h, hipStream_t s) {
     const GatedArgs a{x_rows, wg, wu, offsets, g, u, h, c.E, c.d, c.F};
     if ((long long)c.T * c.k <= 128ll * c.E) go_keep<Half>(a, c, s);
-    else go_keep<Wide>(a, c, s);
+    else go_keep<BIG>(a, c, s);
     return hipGetLastError();
 }
 
@@ -226,14 +241,14 @@ hipError_t launch_ffn_backward(const moe_config& c, const FfnGrad& p, hipStream_
     }
     const bool few = (long long)c.T * c.k <= 128ll * c.E;
     if (few) go_gated_grad<Half>(a, c, s);
-    else go_gated_grad<Wide>(a, c, s);
+    else go_gated_grad<BIG>(a, c, s);
     if (p.dx) {
         if (few) go_rows_grad<Half>(a, c, s);
-        else go_rows_grad<Wide>(a, c, s);
+        else go_rows_grad<BIG>(a, c, s);
     }
     if (p.dwg || p.dwu || p.dwd) {
         if (few) go_weights_grad<Half>(a, s);
-        else go_weights_grad<Wide>(a, s);
+        else go_weights_grad<BIG>(a, s);
     }
     return hipGetLastError();
 }

@@ -2,8 +2,7 @@
 // the reduction dimension contiguous: gradients with respect to rows (the weights' rows run along k), gradients with respect to
 // weights (both operands' rows run along k), and the projections with row-major weights beside them.
 //
-// Eight wavefronts share the tile.  Both operands go global -> LDS by DMA from buffer descriptors, 64 of k per step into two
-// buffers, one step ahead; a descriptor's range is the tile's own rows, so what lies beyond a ragged end (rows of the next
+// Both operands go global -> LDS by DMA from buffer descriptors, BK of k per step into a ring of buffers; a descriptor's range is the tile's own rows, so what lies beyond a ragged end (rows of the next
 // expert, whatever they hold) arrives as zeros and needs no mask.
 //   operand stored with k contiguous:   LDS rows of 64 k (128 bytes), one ds_read_b128 per MFMA fragment.  Position p of row r
 //       holds 16-byte chunk p ^ ((r >> 1) & 7): sixteen lanes that read one chunk column of sixteen rows hit all 64 banks once.
@@ -24,13 +23,17 @@ namespace moe {
 
 namespace {
 
-constexpr int kMmaThreads = 512;
-constexpr int kMmaWaves = kMmaThreads / kWave;
-constexpr int kMmaK = 64;                          // reduction elements per step
-
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+// The thread's number at the start of a body.  Opaque to the compiler, which would work out what all bodies of a kernel derive from it once, in
+// front of them, and hold it in registers that the tallest body does not have.
+__device__ __forceinline__ int body_thread() {
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    return tid;
+}
 
 // A buffer descriptor's parts; everything in it is the same for all lanes.
 struct Panel {
@@ -42,29 +45,29 @@ struct Panel {
     }
 };
 
-// An operand on its way through the reduction: where the next step's panel starts, and how far it reaches.
-//   k contiguous: `rows` rows of `ld` elements; a step advances 64 elements along them.
-//   m contiguous: a step is 64 rows (k) of `ld` elements; `left` rows are still to come, the last step may hold fewer than 64.
-template <bool KC>
+// An operand on its way through the reduction, a step of BK elements at a time: the next step's panel.
+//   k contiguous: `rows` rows of `ld` elements; a step advances BK elements along them.
+//   m contiguous: a step is BK rows (k) of `ld` elements; the last one may hold fewer.
+// Past the last step panels are empty (range 0): loads from them leave zeros and fetch nothing.
+template <bool KC, int BK>
 struct Stream {
     uint64_t base;
     uint32_t range;       // KC: bytes from base to the end of the tile's last row
     uint32_t row_bytes;
     uint32_t skip;        // !KC: bytes of the row in front of the tile
-    int left;             // !KC: rows still to come
-    __device__ static __forceinline__ Stream make(const uint16_t* p, int ld, int rows_or_m0, int k_rows) {
+    int left;             // elements of k still to come
+    __device__ static __forceinline__ Stream make(const uint16_t* p, int ld, int rows_or_m0, int k) {
         Stream s;
         s.row_bytes = (uint32_t)ld * 2u;
+        s.left = k;
         if constexpr (KC) {
             s.base = (uint64_t)(uintptr_t)p;
             s.range = (uint32_t)rows_or_m0 * s.row_bytes;
             s.skip = 0;
-            s.left = 0;
         } else {
             s.skip = (uint32_t)rows_or_m0 * 2u;
             s.base = (uint64_t)(uintptr_t)p + s.skip;
             s.range = 0;
-            s.left = k_rows;
         }
         return s;
     }
@@ -72,23 +75,30 @@ struct Stream {
         Panel p;
         p.base = base;
         if constexpr (KC) {
-            p.range = range;
-            base += kMmaK * 2;
-            range -= kMmaK * 2;
+            p.range = left > 0 ? range : 0;
+            base += BK * 2;
+            range -= BK * 2;
         } else {
-            const int n = left < kMmaK ? left : kMmaK;
-            p.range = (uint32_t)n * row_bytes - skip;
-            base += (uint64_t)kMmaK * row_bytes;
-            left -= kMmaK;
+            const int n = left < BK ? left : BK;
+            p.range = left > 0 ? (uint32_t)n * row_bytes - skip : 0;
+            base += (uint64_t)BK * row_bytes;
         }
+        left -= BK;
         return p;
     }
 };
 
-// What a wavefront loads of an operand's panel: N KiB of its MN x 64 elements, and the lanes' byte offsets from the panel's start.
-template <int MN, bool KC>
+// Permutation of a row's chunks (k contiguous) or pieces, by the row's number in the panel.
+template <int MN, bool KC, int BK>
+__device__ __forceinline__ int swizzle(int r) {
+    if constexpr (KC) return BK == 64 ? (r >> 1) & 7 : (r >> 2) & 3;
+    else return MN >= 128 ? 2 * (r & 3) : (r & 2);
+}
+
+// What a wavefront loads of an operand's panel: N KiB of its MN x BK elements, and the lanes' byte offsets from the panel's start.
+template <int MN, bool KC, int BK, int WAVES>
 struct Loader {
-    static constexpr int N = MN / 64;              // KiB per wavefront: MN * 64 * 2 / 8 wavefronts
+    static constexpr int N = MN * BK / (512 * WAVES);
     uint32_t off[N];
     // first: KC only, the tile's row that the panel starts with (operands of two matrices: half of the rows each)
     __device__ __forceinline__ void init(int ld, int wave, int lane, int first = 0) {
@@ -96,45 +106,42 @@ struct Loader {
         for (int j = 0; j < N; ++j) {
             const int u = wave * N + j;
             if constexpr (KC) {
-                const int row = u * 8 + (lane >> 3), chunk = (lane & 7) ^ ((row >> 1) & 7);
+                constexpr int C = BK / 8;          // 16-byte chunks of a row
+                const int row = u * (64 / C) + lane / C, chunk = (lane % C) ^ swizzle<MN, KC, BK>(row);
                 off[j] = (uint32_t)(row - first) * (uint32_t)ld * 2u + chunk * 16;
             } else {
                 constexpr int W = MN * 2;          // bytes of an LDS row
                 const int byte = u * 1024 + lane * 16, k = byte / W, piece = (byte % W) >> 5;
-                off[j] = (uint32_t)k * (uint32_t)ld * 2u + (piece ^ swz(k)) * 32 + (byte & 16);
+                off[j] = (uint32_t)k * (uint32_t)ld * 2u + (piece ^ swizzle<MN, KC, BK>(k)) * 32 + (byte & 16);
             }
         }
     }
-    __device__ static __forceinline__ int swz(int k) { return MN >= 128 ? 2 * (k & 3) : (k & 2); }
     __device__ __forceinline__ void issue(const Panel& p, uint32_t lds, int wave) const { buffer_dma<N>(off, p.desc(), lds + wave * (N * 1024)); }
 };
 
 // What a lane reads: fragments of 32 rows (m or n) x 16 k, slot s of the step: element i of lane l is k = 16 s + 8 (l / 32) + i.
-template <int MN, bool KC, int BLOCKS>
+template <int MN, bool KC, int BK, int BLOCKS>
 struct Reader {
-    uint32_t at[KC ? 4 : BLOCKS];
-    uint32_t first;
+    uint32_t at[KC ? BK / 16 : BLOCKS];
     __device__ __forceinline__ void init(int row0, int lane) {
         const int half = lane >> 5;
-        first = 0;
         if constexpr (KC) {
             const int r = lane & 31;
-            first = (uint32_t)(row0 + r) * 128u;
 #pragma unroll
-            for (int s = 0; s < 4; ++s) at[s] = first + (uint32_t)(((2 * s + half) ^ ((r >> 1) & 7)) * 16);
+            for (int s = 0; s < BK / 16; ++s) at[s] = (uint32_t)((row0 + r) * BK * 2 + ((2 * s + half) ^ swizzle<MN, KC, BK>(r)) * 16);
         } else {
             constexpr int W = MN * 2;
             const int k = 8 * half + ((lane & 15) >> 2);
 #pragma unroll
             for (int b = 0; b < BLOCKS; ++b) {
                 const int piece = (row0 + b * 32) / 16 + ((lane >> 4) & 1);
-                at[b] = (uint32_t)(k * W + (piece ^ Loader<MN, KC>::swz(k)) * 32 + (lane & 3) * 8);
+                at[b] = (uint32_t)(k * W + (piece ^ swizzle<MN, KC, BK>(k)) * 32 + (lane & 3) * 8);
             }
         }
     }
     __device__ __forceinline__ bf16x8 read(const char* lds, int b, int s) const {
         if constexpr (KC) {
-            return *reinterpret_cast<const bf16x8*>(lds + at[s] + b * 4096);
+            return *reinterpret_cast<const bf16x8*>(lds + at[s] + b * (64 * BK));
         } else {
             typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
             constexpr int W = MN * 2;
@@ -146,84 +153,127 @@ struct Reader {
     }
 };
 
-// BM x BN tile by WM x WN wavefronts.
-template <int BM_, int BN_, int WM_, int WN_>
+// BM x BN tile by WM x WN wavefronts, BK elements of k per step, a ring of STAGES steps.
+template <int BM_, int BN_, int WM_, int WN_, int BK_, int STAGES_, int PER_, int RATE_>
 struct Shape {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+    static constexpr int PER = PER_, RATE = RATE_;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = BK_, STAGES = STAGES_;
+    static constexpr int WAVES = WM * WN, THREADS = WAVES * kWave;
     static constexpr int MB = BM / WM / 32, NB = BN / WN / 32;   // 32x32 blocks per wavefront
-    static constexpr int kBufA = BM * kMmaK * 2, kBuf = (BM + BN) * kMmaK * 2, kRing = 2 * kBuf;
+    static constexpr int kBufA = BM * BK * 2, kBuf = (BM + BN) * BK * 2, kRing = STAGES * kBuf;
     static constexpr int LD = BN + 4;                            // floats per staged row: 16 bytes more, which spreads the rows over the banks
-    static constexpr int kPassRows = WM * 32;                    // rows staged at a time: one block of every wavefront row ...
-    static constexpr int kPasses = MB;
+    static constexpr int kPassRows = WM * 32;                    // rows staged at a time: one block of every wavefront row
     static constexpr int kStage = kPassRows * LD * 4;
     static constexpr int kLds = kRing > kStage ? kRing : kStage;
-    static_assert(WM * WN == kMmaWaves && MB >= 1 && NB >= 1, "eight wavefronts");
+    template <bool KC> using LoadA = Loader<BM, KC, BK, WAVES>;
+    template <bool KC> using LoadB = Loader<BN, KC, BK, WAVES>;
+    static_assert(MB >= 1 && MB <= 4 && NB >= 1, "blocks");
 };
-typedef Shape<256, 256, 2, 4> Wide;
-typedef Shape<128, 128, 2, 4> Half;
-typedef Shape<64, 128, 2, 4> Flat;
 
-template <class S>
-using Acc = f32x16[S::NB][S::MB];
+typedef Shape<256, 256, 2, 4, 64, 2, 1, 100> Wide;
+typedef Shape<128, 256, 1, 4, 32, 3, 2, 95> Pair;
+typedef Shape<128, 128, 2, 4, 64, 2, 2, 75> Half;
 
-template <class S>
-__device__ __forceinline__ void clear(Acc<S>& acc) {
+// A wavefront's results: MB blocks of 32 rows (up to the shape's: a tile of few rows takes a body with fewer), NB of 32 columns.
+template <class S, int MB>
+using Acc = f32x16[S::NB][MB];
+
+template <class S, int MB>
+__device__ __forceinline__ void clear(f32x16 (&acc)[S::NB][MB]) {
 #pragma unroll
     for (int n = 0; n < S::NB; ++n)
 #pragma unroll
-        for (int m = 0; m < S::MB; ++m)
+        for (int m = 0; m < MB; ++m)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[n][m][i] = 0.0f;
 }
 
+// Calls body(integral_constant<MB>) with the fewest blocks per wavefront that hold `rows` rows: a ragged expert's last tile does not multiply
+// rows that it does not have.
+template <class S, class F>
+__device__ __forceinline__ void by_height(int rows, F&& body) {
+    using std::integral_constant;
+    const int need = (rows + S::WM * 32 - 1) / (S::WM * 32);
+    if constexpr (S::MB >= 4) if (need >= 4) return body(integral_constant<int, 4>{});
+    if constexpr (S::MB >= 3) if (need == 3) return body(integral_constant<int, 3>{});
+    if constexpr (S::MB >= 2) if (need == 2 || (S::MB == 2 && need > 2)) return body(integral_constant<int, 2>{});
+    body(integral_constant<int, 1>{});
+}
+
 // acc += the tile's product over `steps` steps.  a, b: the operands' streams, loaders with the offsets set.
-// B2: B's second half of rows is another matrix with the same row length (the gate's rows, then the up projection's).
+// The ring is always full: STAGES - 1 steps are under way while one is read.  The fragments of a slot are read while the slot before is
+// multiplied; a step's barrier stands in front of its last slot's multiplications, which cover the first reads of the next step.
 // Ends with every wavefront past its last LDS read and nothing on its way into LDS.
-template <class S, bool AKC, bool BKC>
-__device__ __forceinline__ void multiply(Acc<S>& acc, Stream<AKC> a, Stream<BKC> b, const Loader<S::BM, AKC>& la, const Loader<S::BN, BKC>& lb,
-                                         int steps, char* lds) {
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid % kWave;
+template <class S, int MB, bool AKC, bool BKC>
+__device__ __forceinline__ void multiply(f32x16 (&acc)[S::NB][MB], Stream<AKC, S::BK> a, Stream<BKC, S::BK> b, const typename S::template LoadA<AKC>& la,
+                                         const typename S::template LoadB<BKC>& lb, int steps, char* lds) {
+    constexpr int SLOTS = S::BK / 16, LOADS = S::template LoadA<AKC>::N + S::template LoadB<BKC>::N;     // loads per step and wavefront
+    constexpr int READS = (AKC ? 1 : 2) * MB + (BKC ? 1 : 2) * S::NB, MFMAS = MB * S::NB;
+    const int tid = body_thread(), wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid % kWave;
     const int wm = wave / S::WN, wn = wave % S::WN;
-    Reader<S::BM, AKC, S::MB> ra;
-    Reader<S::BN, BKC, S::NB> rb;
-    ra.init(wm * S::MB * 32, lane);
+    Reader<S::BM, AKC, S::BK, MB> ra;
+    Reader<S::BN, BKC, S::BK, S::NB> rb;
+    ra.init(wm * MB * 32, lane);
     rb.init(wn * S::NB * 32, lane);
     const uint32_t at = (uint32_t)(uintptr_t)lds;
-    auto load = [&](int buf) {
-        la.issue(a.next(), at + buf * S::kBuf, wave);
-        lb.issue(b.next(), at + buf * S::kBuf + S::kBufA, wave);
+    uint32_t buf = 0;                                            // byte offset of the step that is read
+    bf16x8 fa[2][MB], fb[2][S::NB];
+    auto load = [&](uint32_t to) {
+        la.issue(a.next(), at + to, wave);
+        lb.issue(b.next(), at + to + S::kBufA, wave);
     };
-    if (steps > 0) load(0);
+    auto read = [&](uint32_t from, int s, int set) {
+#pragma unroll
+        for (int n = 0; n < S::NB; ++n) fb[set][n] = rb.read(lds + from + S::kBufA, n, s);
+#pragma unroll
+        for (int m = 0; m < MB; ++m) fa[set][m] = ra.read(lds + from, m, s);
+    };
+    auto landed = [&] {       // the oldest step under way has landed, and no wavefront reads what it has read any more
+        wait_vmcnt<(S::STAGES - 2) * LOADS>();
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    };
+    if (steps <= 0) return;
+#pragma unroll
+    for (int i = 0; i < S::STAGES; ++i) {
+        if (i + 1 == S::STAGES) landed();
+        load(i * S::kBuf);
+    }
+    read(0, 0, 0);
     for (int i = 0; i < steps; ++i) {
-        // this step's panels have landed (the only loads under way), and nobody reads the other buffer any more
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (i + 1 < steps) load((i + 1) & 1);
-        const char* pa = lds + (i & 1) * S::kBuf;
-        const char* pb = pa + S::kBufA;
+        const uint32_t next = buf + S::kBuf == S::kRing ? 0 : buf + S::kBuf;
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            bf16x8 fb[S::NB], fa[S::MB];
+        for (int s = 0; s < SLOTS; ++s) {
+            if (s + 1 < SLOTS) {
+                read(buf, s + 1, (s + 1) & 1);
+            } else {
+                landed();
+                read(next, 0, 0);
+                load(buf);
+            }
 #pragma unroll
-            for (int n = 0; n < S::NB; ++n) fb[n] = rb.read(pb, n, s);
+            for (int m = 0; m < MB; ++m)
 #pragma unroll
-            for (int m = 0; m < S::MB; ++m) fa[m] = ra.read(pa, m, s);
+                for (int n = 0; n < S::NB; ++n) acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[s & 1][n], fa[s & 1][m], acc[n][m], 0, 0, 0);
+            // one multiplication, then as many of the next slot's reads as keep the reads in front of the end
 #pragma unroll
-            for (int m = 0; m < S::MB; ++m)
-#pragma unroll
-                for (int n = 0; n < S::NB; ++n) acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[n], fa[m], acc[n][m], 0, 0, 0);
+            for (int j = 0; j < MFMAS; ++j) {
+                __builtin_amdgcn_sched_group_barrier(0x100, (READS + MFMAS - 1) / MFMAS, 0);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+            }
         }
+        buf = next;
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-// Hands the tile's fp32 results out by rows: f(row in the tile, float* of the row in LDS, which is n = 0 .. BN).  Staged through LDS, one
-// 32-row block of every wavefront at a time, so that what f stores are whole rows.  PER: results per call and thread, GROUPS of them in a row.
-template <class S, int GROUPS, class F>
-__device__ __forceinline__ void by_rows(const Acc<S>& acc, char* lds, F&& f) {
-    const int tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
+// Hands the tile's fp32 results out by rows: f(row in the tile, group, the row's BN floats in LDS) for GROUPS groups of columns per row.  Staged
+// through LDS, one 32-row block of every wavefront row at a time, so that what f stores are whole rows.
+template <class S, int GROUPS, int MB, class F>
+__device__ __forceinline__ void by_rows(const f32x16 (&acc)[S::NB][MB], char* lds, F&& f) {
+    const int tid = body_thread(), wave = tid / kWave, lane = tid % kWave;
     const int wm = wave / S::WN, wn = wave % S::WN;
 #pragma unroll
-    for (int p = 0; p < S::kPasses; ++p) {
+    for (int p = 0; p < MB; ++p) {
         float* row = reinterpret_cast<float*>(lds) + (size_t)(wm * 32 + (lane & 31)) * S::LD + wn * S::NB * 32 + (lane >> 5) * 4;
 #pragma unroll
         for (int n = 0; n < S::NB; ++n)
@@ -231,11 +281,12 @@ __device__ __forceinline__ void by_rows(const Acc<S>& acc, char* lds, F&& f) {
             for (int q = 0; q < 4; ++q)
                 *reinterpret_cast<f32x4*>(row + n * 32 + q * 8) = f32x4{acc[n][p][q * 4], acc[n][p][q * 4 + 1], acc[n][p][q * 4 + 2], acc[n][p][q * 4 + 3]};
         __syncthreads();
-        for (int j = tid; j < S::kPassRows * GROUPS; j += kMmaThreads) {
+#pragma unroll 4
+        for (int j = tid; j < S::kPassRows * GROUPS; j += S::THREADS) {
             const int r = j / GROUPS, g = j % GROUPS;
-            f((r / 32) * (S::MB * 32) + p * 32 + (r & 31), g, reinterpret_cast<const float*>(lds) + (size_t)r * S::LD);
+            f((r / 32) * (MB * 32) + p * 32 + (r & 31), g, reinterpret_cast<const float*>(lds) + (size_t)r * S::LD);
         }
-        if (p + 1 < S::kPasses) __syncthreads();
+        if (p + 1 < MB) __syncthreads();
     }
 }
 
@@ -260,6 +311,14 @@ __device__ __forceinline__ int xcd_tile(int total) {
     return i < per && t < total ? t : -1;
 }
 inline unsigned xcd_grid(long long total) { return (unsigned)((total + 7) / 8 * 8); }
+
+// What a launch of M x N results takes by rounds of tiles, in units of a result: rounds times what a CU works on at a time.  PER: workgroups per CU;
+// RATE: how fast the shape multiplies where rounds are full, in percent of Wide.
+template <class S>
+inline long long cost(long long M, long long N) {
+    const long long tiles = ((M + S::BM - 1) / S::BM) * ((N + S::BN - 1) / S::BN);
+    return (tiles + 256 * S::PER - 1) / (256 * S::PER) * S::PER * S::BM * S::BN * 100 / S::RATE;
+}
 
 // Order inside a rectangle of tiles: columns of up to G row tiles, so that what an XCD runs at one time is a square-ish patch.
 __device__ __forceinline__ void patch(int t, int rows, int cols, int& m, int& n) {
