@@ -141,11 +141,11 @@ constexpr int kMaxRank = 128;
 
 // Many tokens: tiles of the projection as in ffn_train.hip, then the adapters of the tile's tokens.
 template <class S, int MATS>
-__global__ __launch_bounds__(S::THREADS, 2) void adapter_rows_kernel(AdapterArgs p) {
+__global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void adapter_rows_kernel(AdapterArgs p) {
     constexpr int FB = S::BN / MATS, kRow = kMaxRank * 2 + 16, kV = MATS * S::BM * kRow;     // bytes of a token's v in LDS
     __shared__ __attribute__((aligned(1024))) char lds[(S::kLds > kV ? S::kLds : kV) + S::BM * 4];
     const int tm_n = (p.T + S::BM - 1) / S::BM, tn_n = (p.N + FB - 1) / FB;
-    const int t = xcd_tile(tm_n * tn_n);
+    const int t = xcd_tile(blockIdx.x, tm_n * tn_n);
     if (t < 0) return;
     int tm, tn;
     patch(t, tm_n, tn_n, tm, tn);
@@ -223,7 +223,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void adapter_rows_kernel(AdapterArgs
             }
         }
         __syncthreads();
-        by_rows<S, FB / 8>(acc, lds, [&](int r, int c, const float* row) {
+        by_rows<S, FB / 8>(acc, lds, AheadNothing{}, [&](int r, int c, const float* row, Nothing) {
             if (r >= rows || c * 8 >= cols) return;
             float v[8];
             load8(row + c * 8, v);
@@ -477,8 +477,8 @@ hipError_t launch(AdapterArgs p, const moe_adapter_config& c, hipStream_t s) {
             default: few<4, MATS>(p, s);
         }
     } else {
-        if (cost<Wide>(p.T, p.N * MATS) <= cost<Half>(p.T, p.N * MATS)) many<Wide, MATS>(p, s);
-        else many<Half, MATS>(p, s);
+        if (cost<Small>(1, p.T, (long long)p.N * MATS) < cost<Wide>(1, p.T, (long long)p.N * MATS)) many<Small, MATS>(p, s);
+        else many<Wide, MATS>(p, s);
     }
     return hipGetLastError();
 }

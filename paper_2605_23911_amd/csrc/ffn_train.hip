@@ -5,9 +5,6 @@
 //             dWg = dg^T x, dWu = du^T x, dWd = dy^T h, per expert                                  (launch 3)
 // with SiLU(g) = g s, SiLU'(g) = s (1 + g (1 - s)), s = 1 / (1 + exp(-g)).
 #include "mma_tile.hpp"
-#ifndef BIG
-#define BIG Pair
-#endif
 
 namespace moe {
 
@@ -26,7 +23,7 @@ struct GatedArgs {
 // Tile: BM rows x BN / 2 features of both projections: the first half of B's rows are the gate's, the second the up projection's,
 // so that one copy of the token tile in LDS feeds both and the activation needs nothing but the tile.
 template <class S>
-__global__ __launch_bounds__(S::THREADS, 2) void gated_keep_kernel(GatedArgs a) {
+__global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void gated_keep_kernel(GatedArgs a) {
     __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
     constexpr int FB = S::BN / 2;
     RowTile t;
@@ -44,7 +41,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void gated_keep_kernel(GatedArgs a) 
         clear<S, MB>(acc);
         multiply<S, MB, true, true>(acc, Stream<true, S::BK>::make(a.x + (size_t)t.row0 * a.d, a.d, t.rows, a.d),
                                 Stream<true, S::BK>::make((up ? a.wu : a.wg) + ((size_t)t.e * a.F + f0) * a.d, a.d, features, a.d), la, lb, a.d / S::BK, lds);
-        by_rows<S, FB / 8>(acc, lds, [&](int r, int c, const float* row) {
+        by_rows<S, FB / 8>(acc, lds, AheadNothing{}, [&](int r, int c, const float* row, Nothing) {
             if (r >= t.rows || c * 8 >= features) return;
             float g[8], u[8], h[8];
             load8(row + c * 8, g);
@@ -71,7 +68,7 @@ struct GradArgs {
 // dh = dy Wd, and from the tile's dh and the kept g and u: dg, du and h.  dg and du are rounded to bf16, as the operands that the
 // products of launches 2 and 3 take; g and u are the rounded values that the forward pass kept.
 template <class S>
-__global__ __launch_bounds__(S::THREADS, 2) void gated_grad_kernel(GradArgs a) {
+__global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void gated_grad_kernel(GradArgs a) {
     __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
     RowTile t;
     if (!find_tile(a.offsets, a.E, S::BM, (a.F + S::BN - 1) / S::BN, t)) return;
@@ -87,14 +84,21 @@ __global__ __launch_bounds__(S::THREADS, 2) void gated_grad_kernel(GradArgs a) {
         clear<S, MB>(acc);
         multiply<S, MB, true, false>(acc, Stream<true, S::BK>::make(a.dy + (size_t)t.row0 * a.d, a.d, t.rows, a.d),
                                  Stream<false, S::BK>::make(a.wd + (size_t)t.e * a.d * a.F, a.F, f0, a.d), la, lb, a.d / S::BK, lds);
-        by_rows<S, S::BN / 8>(acc, lds, [&](int r, int c, const float* row) {
+        struct Kept {
+            u32x4_t g, u;
+        };
+        auto kept = [&](int r, int c) {
+            const size_t at = (size_t)(t.row0 + (r < t.rows ? r : 0)) * a.F + (f0 + c * 8 < a.F ? f0 + c * 8 : f0);
+            return Kept{*reinterpret_cast<const u32x4_t*>(a.g + at), *reinterpret_cast<const u32x4_t*>(a.u + at)};
+        };
+        by_rows<S, S::BN / 8>(acc, lds, kept, [&](int r, int c, const float* row, const Kept& k) {
             if (r >= t.rows || f0 + c * 8 >= a.F) return;
             const size_t at = (size_t)(t.row0 + r) * a.F + f0 + c * 8;
             float dh[8], g[8], u[8], dg[8], du[8], h[8];
-            unpack8(*reinterpret_cast<const u32x4_t*>(a.g + at), g);
-            unpack8(*reinterpret_cast<const u32x4_t*>(a.u + at), u);
+            unpack8(k.g, g);
+            unpack8(k.u, u);
             load8(row + c * 8, dh);
-    #pragma unroll
+#pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float s = sigmoid(g[i]), act = g[i] * s;
                 dg[i] = dh[i] * u[i] * (s + act * (1.0f - s));
@@ -110,7 +114,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void gated_grad_kernel(GradArgs a) {
 
 // dx = dg Wg + du Wu: one sum over 2 F.
 template <class S>
-__global__ __launch_bounds__(S::THREADS, 2) void rows_grad_kernel(GradArgs a) {
+__global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void rows_grad_kernel(GradArgs a) {
     __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
     RowTile t;
     if (!find_tile(a.offsets, a.E, S::BM, (a.d + S::BN - 1) / S::BN, t)) return;
@@ -128,11 +132,8 @@ __global__ __launch_bounds__(S::THREADS, 2) void rows_grad_kernel(GradArgs a) {
         for (int m = 0; m < 2; ++m)
             multiply<S, MB, true, false>(acc, Stream<true, S::BK>::make((m ? a.du : a.dg) + (size_t)t.row0 * a.F, a.F, t.rows, a.F),
                                      Stream<false, S::BK>::make((m ? a.wu : a.wg) + (size_t)t.e * a.F * a.d, a.d, n0, a.F), la, lb, a.F / S::BK, lds);
-        by_rows<S, S::BN / 8>(acc, lds, [&](int r, int c, const float* row) {
-            if (r >= t.rows || n0 + c * 8 >= a.d) return;
-            float v[8];
-            load8(row + c * 8, v);
-            *reinterpret_cast<u32x4_t*>(a.dx + (size_t)(t.row0 + r) * a.d + n0 + c * 8) = pack8(v);
+        by_rows_bf16<S, MB>(acc, lds, [&](int r, int c, u32x4_t v) {
+            if (r < t.rows && n0 + c * 8 < a.d) *reinterpret_cast<u32x4_t*>(a.dx + (size_t)(t.row0 + r) * a.d + n0 + c * 8) = v;
         });
     });
 }
@@ -140,12 +141,12 @@ __global__ __launch_bounds__(S::THREADS, 2) void rows_grad_kernel(GradArgs a) {
 // dW[m, n] = sum over the expert's rows of P[row, m] Q[row, n] for the three matrices in one launch (the tails of three would add
 // up): tiles [expert][matrix][patch].  An expert without rows gets zeros.
 template <class S>
-__global__ __launch_bounds__(S::THREADS, 2) void weights_grad_kernel(GradArgs a) {
+__global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void weights_grad_kernel(GradArgs a) {
     __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
     const int tm_f = (a.F + S::BM - 1) / S::BM, tn_d = (a.d + S::BN - 1) / S::BN;     // gate, up: [F, d]
     const int tm_d = (a.d + S::BM - 1) / S::BM, tn_f = (a.F + S::BN - 1) / S::BN;     // down: [d, F]
     const int n_g = a.dwg ? tm_f * tn_d : 0, n_u = a.dwu ? tm_f * tn_d : 0, n_d = a.dwd ? tm_d * tn_f : 0, each = n_g + n_u + n_d;
-    int t = xcd_tile(a.E * each);
+    int t = xcd_run_tile(blockIdx.x, a.E * each);
     if (t < 0) return;
     const int e = t / each;
     t -= e * each;
@@ -169,7 +170,15 @@ __global__ __launch_bounds__(S::THREADS, 2) void weights_grad_kernel(GradArgs a)
         multiply<S, MB, false, false>(acc, Stream<false, S::BK>::make(P + (size_t)row0 * M, M, m0, rows), Stream<false, S::BK>::make(Q + (size_t)row0 * N, N, n0, rows),
                                   la, lb, (rows + S::BK - 1) / S::BK, lds);
         void* const out = which == 0 ? a.dwg : which == 1 ? a.dwu : a.dwd;
-        by_rows<S, S::BN / 8>(acc, lds, [&](int r, int c, const float* row) {
+        if (!a.f32 && !a.add) {
+            by_rows_bf16<S, MB>(acc, lds, [&](int r, int c, u32x4_t v) {
+                if (m0 + r >= M || n0 + c * 8 >= N) return;
+                u32x4_t* dst = reinterpret_cast<u32x4_t*>(reinterpret_cast<uint16_t*>(out) + ((size_t)e * M + m0 + r) * N + n0 + c * 8);
+                __builtin_nontemporal_store(v, dst);
+            });
+            return;
+        }
+        by_rows<S, S::BN / 8>(acc, lds, AheadNothing{}, [&](int r, int c, const float* row, Nothing) {
             if (m0 + r >= M || n0 + c * 8 >= N) return;
             const size_t at = ((size_t)e * M + m0 + r) * N + n0 + c * 8;
             float v[8];
@@ -205,20 +214,27 @@ __global__ __launch_bounds__(256) void zero_kernel(u32x4_t* p, size_t n) {
 template <class S>
 void go_keep(const GatedArgs& a, const moe_config& c, hipStream_t s) {
     const long long tiles = most_blocks(c, S::BM) * ((a.F + S::BN / 2 - 1) / (S::BN / 2));
-    hipLaunchKernelGGL(gated_keep_kernel<S>, dim3(xcd_grid(tiles)), dim3(S::THREADS), 0, s, a);
+    hipLaunchKernelGGL(gated_keep_kernel<S>, dim3(16 + xcd_grid(tiles)), dim3(S::THREADS), 0, s, a);
 }
 template <class S>
 void go_gated_grad(const GradArgs& a, const moe_config& c, hipStream_t s) {
-    hipLaunchKernelGGL(gated_grad_kernel<S>, dim3(xcd_grid(most_blocks(c, S::BM) * ((a.F + S::BN - 1) / S::BN))), dim3(S::THREADS), 0, s, a);
+    hipLaunchKernelGGL(gated_grad_kernel<S>, dim3(16 + xcd_grid(most_blocks(c, S::BM) * ((a.F + S::BN - 1) / S::BN))), dim3(S::THREADS), 0, s, a);
 }
 template <class S>
 void go_rows_grad(const GradArgs& a, const moe_config& c, hipStream_t s) {
-    hipLaunchKernelGGL(rows_grad_kernel<S>, dim3(xcd_grid(most_blocks(c, S::BM) * ((a.d + S::BN - 1) / S::BN))), dim3(S::THREADS), 0, s, a);
+    hipLaunchKernelGGL(rows_grad_kernel<S>, dim3(16 + xcd_grid(most_blocks(c, S::BM) * ((a.d + S::BN - 1) / S::BN))), dim3(S::THREADS), 0, s, a);
 }
 template <class S>
 void go_weights_grad(const GradArgs& a, hipStream_t s) {
     const long long fd = (long long)((a.F + S::BM - 1) / S::BM) * ((a.d + S::BN - 1) / S::BN), df = (long long)((a.d + S::BM - 1) / S::BM) * ((a.F + S::BN - 1) / S::BN);
-    hipLaunchKernelGGL(weights_grad_kernel<S>, dim3(xcd_grid(a.E * ((a.dwg ? fd : 0) + (a.dwu ? fd : 0) + (a.dwd ? df : 0)))), dim3(S::THREADS), 0, s, a);
+    hipLaunchKernelGGL(weights_grad_kernel<S>, dim3(xcd_run_grid(a.E * ((a.dwg ? fd : 0) + (a.dwu ? fd : 0) + (a.dwd ? df : 0)))), dim3(S::THREADS), 0, s, a);
+}
+
+// Whether the small tiles are faster for rows x N results, from the mean number of rows per expert: the host does not know more.
+template <class S>
+bool small(const moe_config& c, long long N) {
+    const long long R = (long long)c.T * c.k, active = R < c.E ? R : c.E, rows = (R + active - 1) / active;
+    return cost<Small>(active, rows, N) < cost<S>(active, rows, N);
 }
 
 }  // namespace
@@ -226,8 +242,8 @@ void go_weights_grad(const GradArgs& a, hipStream_t s) {
 hipError_t launch_gated_keep(const moe_config& c, const uint16_t* x_rows, const int32_t* offsets, const uint16_t* wg, const uint16_t* wu,
                              uint16_t* g, uint16_t* u, uint16_t* h, hipStream_t s) {
     const GatedArgs a{x_rows, wg, wu, offsets, g, u, h, c.E, c.d, c.F};
-    if ((long long)c.T * c.k <= 128ll * c.E) go_keep<Half>(a, c, s);
-    else go_keep<BIG>(a, c, s);
+    if (small<Wide>(c, 2ll * c.F)) go_keep<Small>(a, c, s);
+    else go_keep<Wide>(a, c, s);
     return hipGetLastError();
 }
 
@@ -239,16 +255,16 @@ hipError_t launch_ffn_backward(const moe_config& c, const FfnGrad& p, hipStream_
             if (w && !p.add) hipLaunchKernelGGL(zero_kernel, dim3((unsigned)(n / 256 + 1 < 4096 ? n / 256 + 1 : 4096)), dim3(256), 0, s, (u32x4_t*)w, n);
         return hipGetLastError();
     }
-    const bool few = (long long)c.T * c.k <= 128ll * c.E;
-    if (few) go_gated_grad<Half>(a, c, s);
-    else go_gated_grad<BIG>(a, c, s);
+    if (small<Deep>(c, c.F)) go_gated_grad<Small>(a, c, s);
+    else go_gated_grad<Deep>(a, c, s);
     if (p.dx) {
-        if (few) go_rows_grad<Half>(a, c, s);
-        else go_rows_grad<BIG>(a, c, s);
+        if (small<Deep>(c, c.d)) go_rows_grad<Small>(a, c, s);
+        else go_rows_grad<Deep>(a, c, s);
     }
     if (p.dwg || p.dwu || p.dwd) {
-        if (few) go_weights_grad<Half>(a, s);
-        else go_weights_grad<BIG>(a, s);
+        const int n = (p.dwg != nullptr) + (p.dwu != nullptr) + (p.dwd != nullptr);
+        if (cost<Small>((long long)n * c.E, c.F, c.d) < cost<Pair>((long long)n * c.E, c.F, c.d)) go_weights_grad<Small>(a, s);
+        else go_weights_grad<Pair>(a, s);
     }
     return hipGetLastError();
 }

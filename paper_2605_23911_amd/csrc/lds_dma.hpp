@@ -52,27 +52,12 @@ __device__ __forceinline__ void lds_dma16_at(const void* base, uint32_t lane_off
 
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-// N consecutive KiB of LDS from a buffer descriptor (in scalar registers) and 32-bit lane offsets; lanes beyond the descriptor's range leave zeros.
-// The waits are those of lds_dma16_at: five states in front of the first load (the M0 write is one, s_nop 4 the others and one to spare) also
-// cover a descriptor that a vector instruction wrote last.
+// 1 KiB of LDS from a buffer descriptor (in scalar registers) and 32-bit lane offsets; lanes beyond the descriptor's range leave zeros.
+// The M0 write and s_nop 4 make six states in front of the load, which also cover a descriptor that a vector instruction wrote last.
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-template <int N>
-__device__ __forceinline__ void buffer_dma(const uint32_t (&off)[N], i32x4 desc, uint32_t lds_addr) {
-    static_assert(N == 1 || N == 2 || N == 4, "KiB per wavefront");
+__device__ __forceinline__ void buffer_dma(uint32_t off, i32x4 desc, uint32_t lds_addr) {
     const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_addr);
-    if constexpr (N == 1) {
-        asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off[0]), "s"(desc), "s"(dst) : "memory", "m0");
-    } else if constexpr (N == 2) {
-        asm volatile("s_mov_b32 m0, %3\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %2, 0 offen lds\n\t"
-                     "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                     ::"v"(off[0]), "v"(off[1]), "s"(desc), "s"(dst) : "memory", "m0", "scc");
-    } else {
-        asm volatile("s_mov_b32 m0, %5\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %4, 0 offen lds\n\t"
-                     "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %4, 0 offen lds\n\t"
-                     "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %4, 0 offen lds\n\t"
-                     "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %4, 0 offen lds"
-                     ::"v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(desc), "s"(dst) : "memory", "m0", "scc");
-    }
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(desc), "s"(dst) : "memory", "m0");
 }
 #pragma clang diagnostic pop
 

@@ -16,6 +16,9 @@
 #include <type_traits>
 #include <utility>
 
+#ifndef SMALL_RATE
+#define SMALL_RATE 60
+#endif
 #include "lds_dma.hpp"
 #include "moe_internal.hpp"
 
@@ -33,6 +36,16 @@ __device__ __forceinline__ int body_thread() {
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));
     return tid;
+}
+
+template <int... Is, class F>
+__device__ __forceinline__ void static_for_impl(std::integer_sequence<int, Is...>, F&& f) {
+    (f(std::integral_constant<int, Is>{}), ...);
+}
+// f(integral_constant<0>) ... f(integral_constant<N - 1>)
+template <int N, class F>
+__device__ __forceinline__ void static_for(F&& f) {
+    static_for_impl(std::make_integer_sequence<int, N>{}, f);
 }
 
 // A buffer descriptor's parts; everything in it is the same for all lanes.
@@ -116,7 +129,9 @@ struct Loader {
             }
         }
     }
-    __device__ __forceinline__ void issue(const Panel& p, uint32_t lds, int wave) const { buffer_dma<N>(off, p.desc(), lds + wave * (N * 1024)); }
+    // the wavefront's J-th KiB
+    template <int J>
+    __device__ __forceinline__ void one(i32x4 desc, uint32_t lds, int wave) const { buffer_dma(off[J], desc, lds + wave * (N * 1024) + J * 1024); }
 };
 
 // What a lane reads: fragments of 32 rows (m or n) x 16 k, slot s of the step: element i of lane l is k = 16 s + 8 (l / 32) + i.
@@ -157,6 +172,7 @@ struct Reader {
 template <int BM_, int BN_, int WM_, int WN_, int BK_, int STAGES_, int PER_, int RATE_>
 struct Shape {
     static constexpr int PER = PER_, RATE = RATE_;
+    static constexpr int SIMD_WAVES = PER_ * WM_ * WN_ / 4;
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = BK_, STAGES = STAGES_;
     static constexpr int WAVES = WM * WN, THREADS = WAVES * kWave;
     static constexpr int MB = BM / WM / 32, NB = BN / WN / 32;   // 32x32 blocks per wavefront
@@ -164,15 +180,22 @@ struct Shape {
     static constexpr int LD = BN + 4;                            // floats per staged row: 16 bytes more, which spreads the rows over the banks
     static constexpr int kPassRows = WM * 32;                    // rows staged at a time: one block of every wavefront row
     static constexpr int kStage = kPassRows * LD * 4;
-    static constexpr int kLds = kRing > kStage ? kRing : kStage;
+    static constexpr int kTile = BM * (BN * 2 + 16);             // the whole tile as bf16
+    static constexpr int kMost = kRing > kStage ? kRing : kStage, kLds = kMost > kTile ? kMost : kTile;
     template <bool KC> using LoadA = Loader<BM, KC, BK, WAVES>;
     template <bool KC> using LoadB = Loader<BN, KC, BK, WAVES>;
     static_assert(MB >= 1 && MB <= 4 && NB >= 1, "blocks");
 };
 
+// Both operands with k contiguous: rows of 128 bytes, whole lines.  Else four short steps, three of them under way (8192 rows, 28672 -> 4096, four
+// steps of 32 / two of 64: 1840 / 2100 us; with k contiguous in both 2050 / 2010).
 typedef Shape<256, 256, 2, 4, 64, 2, 1, 100> Wide;
+typedef Shape<256, 256, 2, 4, 32, 4, 1, 100> Deep;
+// Two workgroups per CU, one of which stores while the other multiplies: weight gradients, where a tile's reduction is as short as an expert
+// has rows (250 rows of 64 experts, 2560 x 3584: 1470 us, Deep 1500, Wide 1560).
 typedef Shape<128, 256, 1, 4, 32, 3, 2, 95> Pair;
-typedef Shape<128, 128, 2, 4, 64, 2, 2, 75> Half;
+// Few tiles: a quarter of the work each and three steps under way.
+typedef Shape<128, 128, 2, 4, 64, 4, 1, SMALL_RATE> Small;
 
 // A wavefront's results: MB blocks of 32 rows (up to the shape's: a tile of few rows takes a body with fewer), NB of 32 columns.
 template <class S, int MB>
@@ -201,14 +224,19 @@ __device__ __forceinline__ void by_height(int rows, F&& body) {
 }
 
 // acc += the tile's product over `steps` steps.  a, b: the operands' streams, loaders with the offsets set.
-// The ring is always full: STAGES - 1 steps are under way while one is read.  The fragments of a slot are read while the slot before is
-// multiplied; a step's barrier stands in front of its last slot's multiplications, which cover the first reads of the next step.
+// Everything is put in its place by hand: a slot (16 of k) is MB x NB multiplications, and between them go the reads of the next slot's fragments,
+// one or two after each, and the next step's loads, one after each from the last slot on.  In a burst the loads of all wavefronts
+// queue up for longer than a slot takes, and the multiplications behind them wait.  A step's barrier stands in front of its last slot, whose
+// multiplications cover the first reads of the next step.
 // Ends with every wavefront past its last LDS read and nothing on its way into LDS.
 template <class S, int MB, bool AKC, bool BKC>
 __device__ __forceinline__ void multiply(f32x16 (&acc)[S::NB][MB], Stream<AKC, S::BK> a, Stream<BKC, S::BK> b, const typename S::template LoadA<AKC>& la,
                                          const typename S::template LoadB<BKC>& lb, int steps, char* lds) {
-    constexpr int SLOTS = S::BK / 16, LOADS = S::template LoadA<AKC>::N + S::template LoadB<BKC>::N;     // loads per step and wavefront
-    constexpr int READS = (AKC ? 1 : 2) * MB + (BKC ? 1 : 2) * S::NB, MFMAS = MB * S::NB;
+    constexpr int SLOTS = S::BK / 16, NA = S::template LoadA<AKC>::N, LOADS = NA + S::template LoadB<BKC>::N;     // loads per step and wavefront
+    constexpr int READS = MB + S::NB, MFMAS = MB * S::NB, PER = (READS + MFMAS - 1) / MFMAS;
+    // loads that go with the last slot (of the step after next), the rest with the first slots of the next step
+    constexpr int SPREAD = S::STAGES > 2 ? SLOTS : SLOTS - 1;    // slots that loads are spread over
+    constexpr int EACH = (LOADS + SPREAD - 1) / SPREAD;
     const int tid = body_thread(), wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid % kWave;
     const int wm = wave / S::WN, wn = wave % S::WN;
     Reader<S::BM, AKC, S::BK, MB> ra;
@@ -216,78 +244,63 @@ __device__ __forceinline__ void multiply(f32x16 (&acc)[S::NB][MB], Stream<AKC, S
     ra.init(wm * MB * 32, lane);
     rb.init(wn * S::NB * 32, lane);
     const uint32_t at = (uint32_t)(uintptr_t)lds;
-    uint32_t buf = 0;                                            // byte offset of the step that is read
     bf16x8 fa[2][MB], fb[2][S::NB];
-    auto load = [&](uint32_t to) {
-        la.issue(a.next(), at + to, wave);
-        lb.issue(b.next(), at + to + S::kBufA, wave);
+    i32x4 da, db;                                                // the step that is being loaded: descriptors, and where it goes
+    uint32_t to = 0;
+    auto begin = [&](uint32_t where) {
+        da = a.next().desc();
+        db = b.next().desc();
+        to = at + where;
     };
-    auto read = [&](uint32_t from, int s, int set) {
-#pragma unroll
-        for (int n = 0; n < S::NB; ++n) fb[set][n] = rb.read(lds + from + S::kBufA, n, s);
-#pragma unroll
-        for (int m = 0; m < MB; ++m) fa[set][m] = ra.read(lds + from, m, s);
+    auto load = [&](auto piece) {
+        constexpr int p = decltype(piece)::value;
+        if constexpr (p < NA) la.template one<p>(da, to, wave);
+        else if constexpr (p < LOADS) lb.template one<p - NA>(db, to + S::kBufA, wave);
     };
-    auto landed = [&] {       // the oldest step under way has landed, and no wavefront reads what it has read any more
-        wait_vmcnt<(S::STAGES - 2) * LOADS>();
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    auto read = [&](uint32_t from, int s, int set, int which) {
+        if (which < S::NB) fb[set][which] = rb.read(lds + from + S::kBufA, which, s);
+        else if (which < READS) fa[set][which - S::NB] = ra.read(lds + from, which - S::NB, s);
     };
     if (steps <= 0) return;
+    // Steps 0 .. STAGES - 2 whole, and of the next one what the last slot of a step loads.
+    begin(0);
+    static_for<LOADS>(load);
 #pragma unroll
-    for (int i = 0; i < S::STAGES; ++i) {
-        if (i + 1 == S::STAGES) landed();
-        load(i * S::kBuf);
+    for (int i = 1; i < S::STAGES - 1; ++i) {
+        begin(i * S::kBuf);
+        static_for<LOADS>(load);
     }
-    read(0, 0, 0);
+    wait_vmcnt<(S::STAGES - 2) * LOADS>();
+    asm volatile("s_barrier" ::: "memory");
+    begin((S::STAGES - 1) * S::kBuf);
+    static_for<EACH>(load);
+#pragma unroll
+    for (int w = 0; w < READS; ++w) read(0, 0, 0, w);
+    uint32_t buf = 0;                                            // byte offset of the step that is read
     for (int i = 0; i < steps; ++i) {
         const uint32_t next = buf + S::kBuf == S::kRing ? 0 : buf + S::kBuf;
-#pragma unroll
-        for (int s = 0; s < SLOTS; ++s) {
-            if (s + 1 < SLOTS) {
-                read(buf, s + 1, (s + 1) & 1);
-            } else {
-                landed();
-                read(next, 0, 0);
-                load(buf);
+        static_for<SLOTS>([&](auto slot) {
+            constexpr int s = decltype(slot)::value;
+            constexpr bool last = s + 1 == SLOTS;
+            if constexpr (last) {   // the next step has landed, and no wavefront reads this one any more
+                wait_vmcnt<(S::STAGES - 2) * LOADS>();
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                begin(buf);
             }
+            constexpr int first = last ? 0 : (s + 1) * EACH;     // of the step's loads, those of this slot
+            static_for<MFMAS>([&](auto mfma) {
+                constexpr int j = decltype(mfma)::value, m = j / S::NB, n = j % S::NB;
 #pragma unroll
-            for (int m = 0; m < MB; ++m)
-#pragma unroll
-                for (int n = 0; n < S::NB; ++n) acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[s & 1][n], fa[s & 1][m], acc[n][m], 0, 0, 0);
-            // one multiplication, then as many of the next slot's reads as keep the reads in front of the end
-#pragma unroll
-            for (int j = 0; j < MFMAS; ++j) {
-                __builtin_amdgcn_sched_group_barrier(0x100, (READS + MFMAS - 1) / MFMAS, 0);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-            }
-        }
+                for (int q = 0; q < PER; ++q) read(last ? next : buf, last ? 0 : s + 1, (s + 1) & 1, j * PER + q);
+                acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[s & 1][n], fa[s & 1][m], acc[n][m], 0, 0, 0);
+                if constexpr (j < EACH) load(std::integral_constant<int, first + j>{});
+                if constexpr (j + 1 == MFMAS) static_for<(EACH > MFMAS ? EACH - MFMAS : 0)>([&](auto more) { load(std::integral_constant<int, first + MFMAS + decltype(more)::value>{}); });
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
         buf = next;
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-}
-
-// Hands the tile's fp32 results out by rows: f(row in the tile, group, the row's BN floats in LDS) for GROUPS groups of columns per row.  Staged
-// through LDS, one 32-row block of every wavefront row at a time, so that what f stores are whole rows.
-template <class S, int GROUPS, int MB, class F>
-__device__ __forceinline__ void by_rows(const f32x16 (&acc)[S::NB][MB], char* lds, F&& f) {
-    const int tid = body_thread(), wave = tid / kWave, lane = tid % kWave;
-    const int wm = wave / S::WN, wn = wave % S::WN;
-#pragma unroll
-    for (int p = 0; p < MB; ++p) {
-        float* row = reinterpret_cast<float*>(lds) + (size_t)(wm * 32 + (lane & 31)) * S::LD + wn * S::NB * 32 + (lane >> 5) * 4;
-#pragma unroll
-        for (int n = 0; n < S::NB; ++n)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                *reinterpret_cast<f32x4*>(row + n * 32 + q * 8) = f32x4{acc[n][p][q * 4], acc[n][p][q * 4 + 1], acc[n][p][q * 4 + 2], acc[n][p][q * 4 + 3]};
-        __syncthreads();
-#pragma unroll 4
-        for (int j = tid; j < S::kPassRows * GROUPS; j += S::THREADS) {
-            const int r = j / GROUPS, g = j % GROUPS;
-            f((r / 32) * (MB * 32) + p * 32 + (r & 31), g, reinterpret_cast<const float*>(lds) + (size_t)r * S::LD);
-        }
-        if (p + 1 < MB) __syncthreads();
-    }
 }
 
 __device__ __forceinline__ u32x4_t pack8(const float (&v)[8]) {
@@ -303,21 +316,94 @@ __device__ __forceinline__ void unpack8(u32x4_t p, float (&v)[8]) {
     for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(p[i] << 16), v[2 * i + 1] = __uint_as_float(p[i] & 0xffff0000u);
 }
 
-// Which of a launch's `total` tiles a workgroup takes: the hardware deals workgroups to the eight XCDs in turn, and here every XCD gets
-// one run of consecutive tiles, so that tiles which share operands share an L2.  -1: none.
-__device__ __forceinline__ int xcd_tile(int total) {
-    const int per = (total + 7) / 8, x = blockIdx.x & 7, i = blockIdx.x >> 3;
-    const int t = x * per + i;
-    return i < per && t < total ? t : -1;
+// Hands the tile's fp32 results out by rows: f(row in the tile, group, the row's BN floats in LDS, what `ahead` gave) for GROUPS groups of columns per
+// row.  Staged through LDS, one 32-row block of every wavefront row at a time, so that what f stores are whole rows.  ahead(row, group) loads what f
+// needs beside them and is called a block earlier.
+template <class S, int GROUPS, int MB, class A, class F>
+__device__ __forceinline__ void by_rows(const f32x16 (&acc)[S::NB][MB], char* lds, A&& ahead, F&& f) {
+    constexpr int ITEMS = S::kPassRows * GROUPS / S::THREADS;
+    static_assert(S::kPassRows * GROUPS % S::THREADS == 0, "whole items");
+    const int tid = body_thread(), wave = tid / kWave, lane = tid % kWave;
+    const int wm = wave / S::WN, wn = wave % S::WN;
+    auto row_of = [&](int item, int p) {
+        const int r = (tid + item * S::THREADS) / GROUPS;
+        return (r / 32) * (MB * 32) + p * 32 + (r & 31);
+    };
+    decltype(ahead(0, 0)) held[2][ITEMS];
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) held[0][i] = ahead(row_of(i, 0), (tid + i * S::THREADS) % GROUPS);
+#pragma unroll
+    for (int p = 0; p < MB; ++p) {
+        if (p + 1 < MB) {
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) held[(p + 1) & 1][i] = ahead(row_of(i, p + 1), (tid + i * S::THREADS) % GROUPS);
+        }
+        float* row = reinterpret_cast<float*>(lds) + (size_t)(wm * 32 + (lane & 31)) * S::LD + wn * S::NB * 32 + (lane >> 5) * 4;
+#pragma unroll
+        for (int n = 0; n < S::NB; ++n)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<f32x4*>(row + n * 32 + q * 8) = f32x4{acc[n][p][q * 4], acc[n][p][q * 4 + 1], acc[n][p][q * 4 + 2], acc[n][p][q * 4 + 3]};
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int j = tid + i * S::THREADS;
+            f(row_of(i, p), j % GROUPS, reinterpret_cast<const float*>(lds) + (size_t)(j / GROUPS) * S::LD, held[p & 1][i]);
+        }
+        if (p + 1 < MB) __syncthreads();
+    }
+}
+struct Nothing {};
+struct AheadNothing {
+    __device__ __forceinline__ Nothing operator()(int, int) const { return {}; }
+};
+
+// The same for results that need nothing but their rounding to bf16: the whole tile is staged at once, f(row, group of 8 columns, the eight values).
+template <class S, int MB, class F>
+__device__ __forceinline__ void by_rows_bf16(const f32x16 (&acc)[S::NB][MB], char* lds, F&& f) {
+    constexpr int LD = S::BN * 2 + 16, GROUPS = S::BN / 8;
+    static_assert(S::BM * LD <= S::kLds, "the tile fits");
+    const int tid = body_thread(), wave = tid / kWave, lane = tid % kWave;
+    const int wm = wave / S::WN, wn = wave % S::WN;
+#pragma unroll
+    for (int p = 0; p < MB; ++p) {
+        char* row = lds + (wm * MB * 32 + p * 32 + (lane & 31)) * LD + wn * S::NB * 64 + (lane >> 5) * 8;
+#pragma unroll
+        for (int n = 0; n < S::NB; ++n)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<uint2*>(row + n * 64 + q * 16) =
+                    make_uint2(pack2_bf16(acc[n][p][q * 4], acc[n][p][q * 4 + 1]), pack2_bf16(acc[n][p][q * 4 + 2], acc[n][p][q * 4 + 3]));
+    }
+    __syncthreads();
+#pragma unroll 4
+    for (int j = tid; j < S::WM * MB * 32 * GROUPS; j += S::THREADS) {
+        const int r = j / GROUPS, g = j % GROUPS;
+        f(r, g, *reinterpret_cast<const u32x4_t*>(lds + r * LD + g * 16));
+    }
+}
+
+// Which of a launch's tiles a workgroup takes.  The hardware deals workgroups to the eight XCDs in turn.
+// One run of consecutive tiles per XCD, so that tiles which share operands share an L2: for tiles that take the same time.
+__device__ __forceinline__ int xcd_tile(int id, int total) {
+    const int per = (total + 7) / 8, t = (id & 7) * per + (id >> 3);
+    return (id >> 3) < per && t < total ? t : -1;
+}
+// Runs of 32 (what an XCD works on at a time) dealt to the XCDs in turn: for tiles of unequal length.
+__device__ __forceinline__ int xcd_run_tile(int id, int total) {
+    const int t = ((id >> 8) * 8 + (id & 7)) * 32 + ((id >> 3) & 31);
+    return t < total ? t : -1;
 }
 inline unsigned xcd_grid(long long total) { return (unsigned)((total + 7) / 8 * 8); }
+inline unsigned xcd_run_grid(long long total) { return (unsigned)((total + 255) / 256 * 256); }
 
-// What a launch of M x N results takes by rounds of tiles, in units of a result: rounds times what a CU works on at a time.  PER: workgroups per CU;
-// RATE: how fast the shape multiplies where rounds are full, in percent of Wide.
+// What a launch of `groups` times M x N results takes: rounds of tiles times a tile's area, at the shape's RATE (percent of the large ones').  A tile
+// of few rows takes a body of its height, but no less than half of the large ones' for what it loads of B.
 template <class S>
-inline long long cost(long long M, long long N) {
-    const long long tiles = ((M + S::BM - 1) / S::BM) * ((N + S::BN - 1) / S::BN);
-    return (tiles + 256 * S::PER - 1) / (256 * S::PER) * S::PER * S::BM * S::BN * 100 / S::RATE;
+inline long long cost(long long groups, long long M, long long N) {
+    const long long tiles = groups * ((M + S::BM - 1) / S::BM) * ((N + S::BN - 1) / S::BN), rows = (M + 63) / 64 * 64;
+    const long long height = rows < S::BM ? (rows > 128 ? rows : S::BM < 128 ? S::BM : 128) : S::BM;
+    return (tiles + 256 * S::PER - 1) / (256 * S::PER) * S::PER * height * S::BN * 100 / S::RATE;
 }
 
 // Order inside a rectangle of tiles: columns of up to G row tiles, so that what an XCD runs at one time is a square-ish patch.
@@ -330,37 +416,64 @@ __device__ __forceinline__ void patch(int t, int rows, int cols, int& m, int& n)
 
 // Rows of expert-contiguous storage cut into blocks of BM per expert (Alg. 1), each with `cols` column tiles: the workgroup's tile, found from
 // the offsets by every wavefront for itself (up to 256 experts: four per lane).  No list in memory, hence no launch that writes one.
+// Whole blocks come first, then what is left of the experts, the taller ones (more than half a block) before the others: a launch then ends
+// with its short tiles, where it would otherwise start another round of whole ones.  Where whole blocks are the rule the rest is dealt to
+// the XCDs tile by tile, else (many experts of less than a block) in runs like the whole ones.
+// 8 experts, 8192 rows, 14336 -> 4096: 448 whole tiles of 256 x 256, 64 nearly whole, two rounds, and 64 of a few rows.
 struct RowTile {
     int e, row0, rows, n;      // expert, first row, rows in the tile, column tile
 };
+__device__ __forceinline__ int wave_sums(int v, int lane) {
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+        const int up = __shfl_up(v, o, kWave);
+        if (lane >= o) v += up;
+    }
+    return v;
+}
 __device__ __forceinline__ bool find_tile(const int32_t* offsets, int E, int BM, int cols, RowTile& out) {
     const int lane = threadIdx.x % kWave;
-    int start[5], nb[4], sum = 0;
+    int start[5], count[3][4], sum[3] = {0, 0, 0}, inc[3], total[3];
 #pragma unroll
     for (int i = 0; i < 5; ++i) {
         const int e = lane * 4 + i;
         start[i] = offsets[e < E ? e : E];
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sum += nb[i] = (start[i + 1] - start[i] + BM - 1) / BM;
-    int inc = sum;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-        const int up = __shfl_up(inc, o, kWave);
-        if (lane >= o) inc += up;
+    for (int i = 0; i < 4; ++i) {
+        const int n = start[i + 1] - start[i], rest = n % BM;
+        sum[0] += count[0][i] = n / BM;
+        sum[1] += count[1][i] = rest > BM / 2;
+        sum[2] += count[2][i] = rest > 0 && rest <= BM / 2;
     }
-    const int total = __shfl(inc, kWave - 1, kWave) * cols;
-    const int t = xcd_tile(total);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        inc[k] = wave_sums(sum[k], lane);
+        total[k] = __builtin_amdgcn_readlane(inc[k], kWave - 1);
+    }
+    // which class, and the place in it
+    const bool deal = total[0] > total[1] + total[2];
+    int id = blockIdx.x, k = -1, t = -1;
+#pragma unroll
+    for (int c = 0; c < 3; ++c) {
+        const int n = total[c] * cols, ids = (n + 7) / 8 * 8;
+        if (k < 0 && id < ids) {
+            k = c;
+            t = c > 0 && deal ? (id < n ? id : -1) : xcd_tile(id, n);
+        }
+        if (k < 0) id -= ids;
+    }
     if (t < 0) return false;
     const int block = t / cols;                    // some block of the same expert
-    const unsigned long long hit = __ballot(inc > block);
-    const int owner = __builtin_ctzll(hit);
-    int before = inc - sum, e = 0, s = 0, n_e = 0, blocks = 0;
+    const int upto = k == 0 ? inc[0] : k == 1 ? inc[1] : inc[2];
+    const int owner = __builtin_ctzll(__ballot(upto > block));
+    int before = upto - (k == 0 ? sum[0] : k == 1 ? sum[1] : sum[2]), e = 0, s = 0, n_e = 0, blocks = 0;
     bool found = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if (!found && block < before + nb[i]) found = true, e = lane * 4 + i, s = start[i], n_e = start[i + 1] - start[i], blocks = nb[i];
-        if (!found) before += nb[i];
+        const int nb = k == 0 ? count[0][i] : k == 1 ? count[1][i] : count[2][i];
+        if (!found && block < before + nb) found = true, e = lane * 4 + i, s = start[i], n_e = start[i + 1] - start[i], blocks = nb;
+        if (!found) before += nb;
     }
     e = __builtin_amdgcn_readlane(e, owner);
     s = __builtin_amdgcn_readlane(s, owner);
@@ -369,6 +482,7 @@ __device__ __forceinline__ bool find_tile(const int32_t* offsets, int E, int BM,
     before = __builtin_amdgcn_readlane(before, owner);
     int m, n;
     patch(t - before * cols, blocks, cols, m, n);
+    if (k > 0) m = n_e / BM;
     out.e = e;
     out.row0 = s + m * BM;
     out.rows = n_e - m * BM < BM ? n_e - m * BM : BM;
