@@ -290,32 +290,44 @@ class _Call:
     """Arguments of one call of the training and adapter entry points: sizes and types are checked here (the C ABI sees addresses only), all
     tensors have to be on one GPU, and the call runs with that GPU current, on `stream` or that GPU's current stream."""
 
+    __slots__ = ("index", "stream")
+
     def __init__(self, stream=None):
-        self.device, self.stream = None, stream
+        self.index, self.stream = -1, stream
 
     def __call__(self, name, t, shape, dtype, optional=False):
         if t is None:
             if optional:
                 return None
             raise ValueError(f"{name} is required")
-        if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        if t.dtype != dtype or t.shape != shape:
             raise ValueError(f"{name} has to be {dtype} {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
         return self.raw(name, t)
 
     def raw(self, name, t):
-        p = _ptr(t)
-        if self.device is None:
-            self.device = t.device
-        if t.device != self.device:
-            raise ValueError(f"{name} is on {t.device}, the other tensors on {self.device}")
-        return p
+        index = t.get_device()
+        if index != self.index:
+            if index < 0:
+                raise ValueError("tensors handed to the MoE library must be contiguous GPU tensors")
+            if self.index >= 0:
+                raise ValueError(f"{name} is on cuda:{index}, the other tensors on cuda:{self.index}")
+            self.index = index
+        if not t.is_contiguous():
+            raise ValueError("tensors handed to the MoE library must be contiguous GPU tensors")
+        return t.data_ptr()
 
     def run(self, where, fn, *args):
-        with torch.cuda.device(self.device):
-            s = self.stream if self.stream is not None else torch.cuda.current_stream()
-            if s.device != self.device:
-                raise ValueError(f"{where}: the stream is on {s.device}, the tensors on {self.device}")
-            _check(fn(*args, C.c_void_p(s.cuda_stream)), where)
+        s = self.stream
+        if s is None:
+            s = torch.cuda.current_stream(self.index)
+        elif s.device_index != self.index:
+            raise ValueError(f"{where}: the stream is on cuda:{s.device_index}, the tensors on cuda:{self.index}")
+        if torch.cuda.current_device() == self.index:
+            status = fn(*args, s.cuda_stream)
+        else:
+            with torch.cuda.device(self.index):
+                status = fn(*args, s.cuda_stream)
+        _check(status, where)
 
 
 def ffn_backward_workspace_size(cfg) -> int:

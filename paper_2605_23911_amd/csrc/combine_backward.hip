@@ -12,7 +12,7 @@ constexpr int kWaves = kThreads / kWave;
 // p and dp may be one buffer.  One token per workgroup, up to eight slots at a time: dy's piece is read once for all of them, their rows' pieces are requested
 // before the first is used.  Every dp row belongs to one slot, so nothing is added in memory; the dot products are summed in fp32 per
 // thread (d / 2048 pieces of eight), over the wavefront and over the four wavefronts, always in the same order.
-template <int N>
+template <int N, bool STREAM>
 __device__ __forceinline__ void slots(const uint16_t* __restrict__ dy, const uint16_t* p, const int32_t* __restrict__ rows,
                                       const float* __restrict__ w, int d, uint16_t* dp, float* __restrict__ dw, float (*part)[8]) {
     size_t at[N];
@@ -24,7 +24,10 @@ __device__ __forceinline__ void slots(const uint16_t* __restrict__ dy, const uin
         u32x4_t row[N];
         const u32x4_t g = *reinterpret_cast<const u32x4_t*>(dy + c);
 #pragma unroll
-        for (int i = 0; i < N; ++i) row[i] = *reinterpret_cast<const u32x4_t*>(p + at[i] + c);
+        for (int i = 0; i < N; ++i) {
+            const u32x4_t* from = reinterpret_cast<const u32x4_t*>(p + at[i] + c);
+            row[i] = STREAM ? __builtin_nontemporal_load(from) : *from;
+        }
         unpack8(g, v);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -35,7 +38,9 @@ __device__ __forceinline__ void slots(const uint16_t* __restrict__ dy, const uin
                 dot[i] = fmaf(v[j], q[j], dot[i]);
                 o[j] = wi[i] * v[j];
             }
-            *reinterpret_cast<u32x4_t*>(dp + at[i] + c) = pack8(o);
+            u32x4_t* to = reinterpret_cast<u32x4_t*>(dp + at[i] + c);
+            if constexpr (STREAM) __builtin_nontemporal_store(pack8(o), to);
+            else *to = pack8(o);
         }
     }
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
@@ -55,7 +60,7 @@ __device__ __forceinline__ void slots(const uint16_t* __restrict__ dy, const uin
     __syncthreads();
 }
 
-template <int K>
+template <int K, bool STREAM>
 __global__ __launch_bounds__(kThreads) void combine_backward_kernel(const uint16_t* __restrict__ dy, const uint16_t* p,
                                                                    const int32_t* __restrict__ row_of, const float* __restrict__ topk_w, int k, int d,
                                                                    uint16_t* dp, float* __restrict__ dw) {
@@ -66,13 +71,13 @@ __global__ __launch_bounds__(kThreads) void combine_backward_kernel(const uint16
     topk_w += t * (K ? K : k);
     dw += t * (K ? K : k);
     if constexpr (K > 0) {
-        slots<K>(dy, p, row_of, topk_w, d, dp, dw, part);
+        slots<K, STREAM>(dy, p, row_of, topk_w, d, dp, dw, part);
     } else {
         int i = 0;
-        for (; i + 8 <= k; i += 8) slots<8>(dy, p, row_of + i, topk_w + i, d, dp, dw + i, part);
-        if (k & 4) slots<4>(dy, p, row_of + i, topk_w + i, d, dp, dw + i, part), i += 4;
-        if (k & 2) slots<2>(dy, p, row_of + i, topk_w + i, d, dp, dw + i, part), i += 2;
-        if (k & 1) slots<1>(dy, p, row_of + i, topk_w + i, d, dp, dw + i, part);
+        for (; i + 8 <= k; i += 8) slots<8, STREAM>(dy, p, row_of + i, topk_w + i, d, dp, dw + i, part);
+        if (k & 4) slots<4, STREAM>(dy, p, row_of + i, topk_w + i, d, dp, dw + i, part), i += 4;
+        if (k & 2) slots<2, STREAM>(dy, p, row_of + i, topk_w + i, d, dp, dw + i, part), i += 2;
+        if (k & 1) slots<1, STREAM>(dy, p, row_of + i, topk_w + i, d, dp, dw + i, part);
     }
 }
 
@@ -80,8 +85,10 @@ __global__ __launch_bounds__(kThreads) void combine_backward_kernel(const uint16
 
 hipError_t launch_combine_backward(const moe_config& c, const uint16_t* dy, const uint16_t* y_perm, const int32_t* row_of, const float* topk_w,
                                    uint16_t* dy_perm, float* d_topk_w, hipStream_t s) {
+    const bool stream = (long long)c.T * c.k * c.d >= (1ll << 26);
     auto go = [&](auto k) {
-        hipLaunchKernelGGL(combine_backward_kernel<decltype(k)::value>, dim3(c.T), dim3(kThreads), 0, s, dy, y_perm, row_of, topk_w, c.k, c.d, dy_perm, d_topk_w);
+        constexpr int K = decltype(k)::value;
+        hipLaunchKernelGGL((stream ? combine_backward_kernel<K, true> : combine_backward_kernel<K, false>), dim3(c.T), dim3(kThreads), 0, s, dy, y_perm, row_of, topk_w, c.k, c.d, dy_perm, d_topk_w);
     };
     using std::integral_constant;
     switch (c.k) {

@@ -49,8 +49,8 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void gated_keep_kernel(G
     #pragma unroll
             for (int i = 0; i < 8; ++i) h[i] = g[i] * sigmoid(g[i]) * u[i];
             const size_t at = (size_t)(t.row0 + r) * a.F + f0 + c * 8;
-            *reinterpret_cast<u32x4_t*>(a.g + at) = pack8(g);
-            *reinterpret_cast<u32x4_t*>(a.u + at) = pack8(u);
+            __builtin_nontemporal_store(pack8(g), reinterpret_cast<u32x4_t*>(a.g + at));
+            __builtin_nontemporal_store(pack8(u), reinterpret_cast<u32x4_t*>(a.u + at));
             *reinterpret_cast<u32x4_t*>(a.h + at) = pack8(h);
         });
     });
@@ -128,10 +128,10 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void rows_grad_kernel(Gr
         constexpr int MB = decltype(height)::value;
         Acc<S, MB> acc;
         clear<S, MB>(acc);
-    #pragma unroll 1
+#pragma unroll 1
         for (int m = 0; m < 2; ++m)
             multiply<S, MB, true, false>(acc, Stream<true, S::BK>::make((m ? a.du : a.dg) + (size_t)t.row0 * a.F, a.F, t.rows, a.F),
-                                     Stream<false, S::BK>::make((m ? a.wu : a.wg) + (size_t)t.e * a.F * a.d, a.d, n0, a.F), la, lb, a.F / S::BK, lds);
+                                         Stream<false, S::BK>::make((m ? a.wu : a.wg) + (size_t)t.e * a.F * a.d, a.d, n0, a.F), la, lb, a.F / S::BK, lds);
         by_rows_bf16<S, MB>(acc, lds, [&](int r, int c, u32x4_t v) {
             if (r < t.rows && n0 + c * 8 < a.d) *reinterpret_cast<u32x4_t*>(a.dx + (size_t)(t.row0 + r) * a.d + n0 + c * 8) = v;
         });

@@ -16,9 +16,6 @@
 #include <type_traits>
 #include <utility>
 
-#ifndef SMALL_RATE
-#define SMALL_RATE 60
-#endif
 #include "lds_dma.hpp"
 #include "moe_internal.hpp"
 
@@ -195,7 +192,7 @@ typedef Shape<256, 256, 2, 4, 32, 4, 1, 100> Deep;
 // has rows (250 rows of 64 experts, 2560 x 3584: 1470 us, Deep 1500, Wide 1560).
 typedef Shape<128, 256, 1, 4, 32, 3, 2, 95> Pair;
 // Few tiles: a quarter of the work each and three steps under way.
-typedef Shape<128, 128, 2, 4, 64, 4, 1, SMALL_RATE> Small;
+typedef Shape<128, 128, 2, 4, 64, 4, 1, 60> Small;
 
 // A wavefront's results: MB blocks of 32 rows (up to the shape's: a tile of few rows takes a body with fewer), NB of 32 columns.
 template <class S, int MB>
@@ -283,9 +280,9 @@ __device__ __forceinline__ void multiply(f32x16 (&acc)[S::NB][MB], Stream<AKC, S
             constexpr int s = decltype(slot)::value;
             constexpr bool last = s + 1 == SLOTS;
             if constexpr (last) {   // the next step has landed, and no wavefront reads this one any more
+                begin(buf);
                 wait_vmcnt<(S::STAGES - 2) * LOADS>();
                 asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-                begin(buf);
             }
             constexpr int first = last ? 0 : (s + 1) * EACH;     // of the step's loads, those of this slot
             static_for<MFMAS>([&](auto mfma) {
