@@ -18,6 +18,8 @@ struct AdapterArgs {
     const int32_t* of;                // [T]
     const uint16_t* base;             // [T, N] or null
     float* v;                         // [parts][matrices][T][rank] partial sums over K
+    float* sums;                      // [splits][matrices][T][N] the projection's, where its launch has too few tiles (adapter_part_kernel)
+    int splits;
     uint16_t* y;                      // [T, N]
     int T, N, K, n, rank;
     int parts, lists;                 // low_rank_kernel: pieces of K, workgroups per token block
@@ -179,12 +181,11 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void adapter_rows_kernel
         {
             const int r = lane2 & 31, half = lane2 >> 5, c0 = wn * S::NB * 32, m2 = MATS == 2 && c0 >= FB ? 1 : 0;
             int id[MB];
-            unsigned left[MB], any = 0;
+            unsigned left[MB];
     #pragma unroll
             for (int m = 0; m < MB; ++m) {
                 id[m] = ids[(wm * MB + m) * 32 + r];
                 left[m] = (unsigned)__ballot(id[m] >= 0);
-                any |= left[m];
             }
             const uint16_t* brow[S::NB];
     #pragma unroll
@@ -192,32 +193,58 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void adapter_rows_kernel
                 int col = n0 + c0 - m2 * FB + n * 32 + r;
                 brow[n] = p.b[m2] + (size_t)(col < p.N ? col : p.N - 1) * p.rank;
             }
-            while (any) {
-                int a = -1;
-    #pragma unroll
+            // The next piece (64 of the rank of an adapter) of B is under way while one is multiplied.
+            int a = -1, c = 0;
+            unsigned here[MB];
+            bf16x8 fb[4][S::NB];
+            auto next = [&] {
+                c += 64;
+                if (a >= 0 && c < p.rank) return;
+                a = -1;
+                c = 0;
+#pragma unroll
                 for (int m = MB - 1; m >= 0; --m)
                     if (left[m]) a = __builtin_amdgcn_readlane(id[m], __builtin_ctz(left[m]));
-                unsigned here[MB];
-                any = 0;
-    #pragma unroll
+                if (a < 0) return;
+#pragma unroll
                 for (int m = 0; m < MB; ++m) {
                     here[m] = (unsigned)__ballot(id[m] == a);
                     left[m] &= ~here[m];
-                    any |= left[m];
                 }
-                for (int c = 0; c < p.rank; c += 16) {
-                    const bool in = c + half * 8 < p.rank;
-                    bf16x8 fb[S::NB];
-    #pragma unroll
+            };
+            auto load = [&] {
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
                     for (int n = 0; n < S::NB; ++n)
-                        fb[n] = in ? *reinterpret_cast<const bf16x8*>(brow[n] + (size_t)a * p.N * p.rank + c + half * 8) : zeros8();
-    #pragma unroll
+                        fb[q][n] = c + q * 16 + half * 8 < p.rank ? *reinterpret_cast<const bf16x8*>(brow[n] + (size_t)a * p.N * p.rank + c + q * 16 + half * 8) : zeros8();
+            };
+            next();
+            if (a >= 0) load();
+            while (a >= 0) {
+                const int a0 = a, c0 = c;
+                unsigned h0[MB];
+                bf16x8 f0[4][S::NB];
+#pragma unroll
+                for (int m = 0; m < MB; ++m) h0[m] = here[m];
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int n = 0; n < S::NB; ++n) f0[q][n] = fb[q][n];
+                next();
+                if (a >= 0) load();
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int at = c0 + q * 16 + half * 8;
+                    if (c0 + q * 16 >= p.rank) break;
+#pragma unroll
                     for (int m = 0; m < MB; ++m) {
-                        if (!here[m]) continue;
-                        const bf16x8 fv = in && id[m] == a
-                            ? *reinterpret_cast<const bf16x8*>(lds + (m2 * S::BM + (wm * MB + m) * 32 + r) * kRow + (c + half * 8) * 2) : zeros8();
-    #pragma unroll
-                        for (int n = 0; n < S::NB; ++n) keep_mine<f32x16>(acc[n][m], __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[n], fv, acc[n][m], 0, 0, 0), id[m] == a);
+                        if (!h0[m]) continue;
+                        const bf16x8 fv = at < p.rank && id[m] == a0
+                            ? *reinterpret_cast<const bf16x8*>(lds + (m2 * S::BM + (wm * MB + m) * 32 + r) * kRow + at * 2) : zeros8();
+#pragma unroll
+                        for (int n = 0; n < S::NB; ++n) keep_mine<f32x16>(acc[n][m], __builtin_amdgcn_mfma_f32_32x32x16_bf16(f0[q][n], fv, acc[n][m], 0, 0, 0), id[m] == a0);
                     }
                 }
             }
@@ -244,15 +271,82 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void adapter_rows_kernel
     });
 }
 
-// Up to 64 tokens: bound by streaming W.  A workgroup takes NB blocks of 16 features (of each matrix) and all tokens (MB blocks of 16); its
-// eight wavefronts split K, and the adapters that occur, and are joined through LDS.  Weights go from memory to registers: 16x16x32
-// MFMAs, so that four lanes read 64 consecutive bytes of a weight row.
+// The j-th adapter, counted from 0, that occurs among up to 128 tokens from t0; -1: fewer occur.
+__device__ __forceinline__ int occurring(const AdapterArgs& p, int t0, int rows, int j, int lane) {
+    const int a0 = lane < rows ? adapter_of(p, t0 + lane) : -1, a1 = lane + kWave < rows ? adapter_of(p, t0 + lane + kWave) : -1;
+    unsigned long long left0 = __ballot(a0 >= 0), left1 = __ballot(a1 >= 0);
+    for (;;) {
+        if ((left0 | left1) == 0) return -1;
+        const int a = left0 ? __builtin_amdgcn_readlane(a0, __builtin_ctzll(left0)) : __builtin_amdgcn_readlane(a1, __builtin_ctzll(left1));
+        if (j-- == 0) return a;
+        left0 &= ~__ballot(a0 == a);
+        left1 &= ~__ballot(a1 == a);
+    }
+}
+
+// Decode batches, and projections with too few tiles for the CUs: the fp32 sums of x W^T over one of `splits` pieces of K, and in the same launch
+// v, one tile per adapter that occurs (its A takes W's place, the rows that have it are kept).  Bound by streaming W and A, of which every
+// workgroup has three steps (48 KiB) under way: 14336 -> 4096 for one token 18 us, 6.5 TB/s.
+template <class S, int MATS>
+__global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void adapter_part_kernel(AdapterArgs p) {
+    constexpr int FB = S::BN / MATS;
+    static_assert(S::BM <= 2 * kWave, "occurring");
+    __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
+    const int tn_n = p.w[0] ? (p.N + FB - 1) / FB : 0, tn_r = (p.rank + FB - 1) / FB, low = p.lists * tn_r, per = low + tn_n;
+    const int piece = blockIdx.x % p.splits, t = blockIdx.x / p.splits, tm = t / per;
+    int tn = t - tm * per;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    const int t0 = tm * S::BM, rows = p.T - t0 < S::BM ? p.T - t0 : S::BM;
+    const bool second = MATS == 2 && wave >= S::WAVES / 2;
+    const uint16_t* w = second ? p.w[1] : p.w[0];
+    int a = -1, N = p.N;
+    float* out = p.sums;
+    float scale = 1.0f;
+    if (tn < low) {                    // an adapter's tile
+        a = occurring(p, t0, rows, tn / tn_r, lane);
+        if (a < 0) return;
+        tn %= tn_r;
+        N = p.rank;
+        w = (second ? p.a[1] : p.a[0]) + (size_t)a * p.rank * p.K;
+        out = p.v;
+        if (p.scale) scale = p.scale[a];
+    } else {
+        tn -= low;
+    }
+    const int n0 = tn * FB, cols = N - n0 < FB ? N - n0 : FB;
+    const int all = p.K / S::BK, each = (all + p.splits - 1) / p.splits, s0 = piece * each < all ? piece * each : all, steps = all - s0 < each ? all - s0 : each;
+    by_height<S>(rows, [&](auto height) {
+        constexpr int MB = decltype(height)::value;
+        Acc<S, MB> acc;
+        clear<S, MB>(acc);
+        typename S::template LoadA<true> la;
+        typename S::template LoadB<true> lb;
+        la.init(p.K, wave, lane);
+        lb.init(p.K, wave, lane, second ? FB : 0);
+        const int k0 = s0 * S::BK;      // the panels start at k0; their rows still end where the tile's do
+        multiply<S, MB, true, true>(acc, Stream<true, S::BK>::make(p.x + (size_t)t0 * p.K + k0, p.K, rows, steps * S::BK, k0),
+                                    Stream<true, S::BK>::make(w + (size_t)n0 * p.K + k0, p.K, cols, steps * S::BK, k0), la, lb, steps, lds);
+        by_rows<S, S::BN / 8>(acc, lds, AheadNothing{}, [&](int r, int c, const float* row, Nothing) {
+            const int m = MATS == 2 && c * 8 >= FB ? 1 : 0, col = c * 8 - m * FB;
+            if (r >= rows || col >= cols) return;
+            if (a >= 0 && adapter_of(p, t0 + r) != a) return;
+            float* to = out + (((size_t)piece * MATS + m) * p.T + t0 + r) * N + n0 + col;
+            float v[8];
+            load8(row + c * 8, v);
+            *reinterpret_cast<f32x4*>(to) = f32x4{v[0] * scale, v[1] * scale, v[2] * scale, v[3] * scale};
+            *reinterpret_cast<f32x4*>(to + 4) = f32x4{v[4] * scale, v[5] * scale, v[6] * scale, v[7] * scale};
+        });
+    });
+}
+
+// Adds adapter_part_kernel's sums and the adapters' part.  A workgroup takes up to 64 tokens (MB blocks of 16) and NB blocks of 16 features (of each
+// matrix); its eight wavefronts share the adapters that occur and are joined through LDS.  Bound by reading B.
 template <int MB, int NB, int MATS>
-__global__ __launch_bounds__(kThreads, 4) void adapter_few_kernel(AdapterArgs p) {
+__global__ __launch_bounds__(kThreads, 4) void adapter_join_kernel(AdapterArgs p) {
     constexpr int kRow = kMaxRank * 2 + 16, kV = MATS * MB * 16 * kRow, kPart = kWaves / 2 * MATS * NB * MB * 64 * 16;
     __shared__ __attribute__((aligned(1024))) char lds[kPart > kV ? kPart : kV];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid % kWave, r = lane & 15, quad = lane >> 4;
-    const int n0 = blockIdx.x * (NB * 16);
+    const int n0 = blockIdx.x * (NB * 16), t0 = blockIdx.y * (MB * 16);
     f32x4 acc[MATS][NB][MB];
 #pragma unroll
     for (int m = 0; m < MATS; ++m)
@@ -260,56 +354,14 @@ __global__ __launch_bounds__(kThreads, 4) void adapter_few_kernel(AdapterArgs p)
         for (int n = 0; n < NB; ++n)
 #pragma unroll
             for (int b = 0; b < MB; ++b) acc[m][n][b] = f32x4{0, 0, 0, 0};
-    const int steps = p.w[0] ? p.K / 32 : 0, each = (steps + kWaves - 1) / kWaves;
-    const int s0 = wave * each < steps ? wave * each : steps, s1 = s0 + each < steps ? s0 + each : steps;
-    // addresses: what is the same for the wavefront (scalar registers), plus a 32-bit offset per lane
-    const uint32_t wlane = (uint32_t)(r * p.K + quad * 8) * 2u;
-    uint32_t xlane[MB];
-#pragma unroll
-    for (int b = 0; b < MB; ++b) xlane[b] = (uint32_t)((b * 16 + r < p.T ? b * 16 + r : p.T - 1) * p.K + quad * 8) * 2u;
-    auto wpiece = [&](int m, int n, int s) {
-        const char* base = reinterpret_cast<const char*>(p.w[m] + (size_t)(n0 + n * 16) * p.K + s * 32);
-        return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(base + wlane));
-    };
-    auto xpiece = [&](int b, int s) { return *reinterpret_cast<const bf16x8*>(reinterpret_cast<const char*>(p.x + s * 32) + xlane[b]); };
-    // U steps' loads are under way at once, as many as 128 registers hold; weights past the end are zeros, and so are their tokens
-    constexpr int fit = ((128 - 22) / 4 - MATS * NB * MB) / (MATS * NB + MB), U = fit < 1 ? 1 : fit > 8 ? 8 : fit;
-    for (int s = s0; s < s1; s += U) {
-        u32x4_t fw[U][MATS][NB];
-        bf16x8 fx[U][MB];
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const int at = s + i < s1 ? s + i : s1 - 1;
-#pragma unroll
-            for (int m = 0; m < MATS; ++m)
-#pragma unroll
-                for (int n = 0; n < NB; ++n) fw[i][m][n] = wpiece(m, n, at);
-#pragma unroll
-            for (int b = 0; b < MB; ++b) fx[i][b] = xpiece(b, at);
-        }
-        __builtin_amdgcn_sched_barrier(0);         // else the compiler waits for each load before it issues the next, to save registers
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const bool in = s + i < s1;
-#pragma unroll
-            for (int b = 0; b < MB; ++b) {
-                const bf16x8 vx = in ? fx[i][b] : zeros8();
-#pragma unroll
-                for (int m = 0; m < MATS; ++m)
-#pragma unroll
-                    for (int n = 0; n < NB; ++n)
-                        acc[m][n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(in ? __builtin_bit_cast(bf16x8, fw[i][m][n]) : zeros8(), vx, acc[m][n][b], 0, 0, 0);
-            }
-        }
-    }
     // v of all tokens as bf16
     const int chunks = p.rank / 8;
     for (int j = tid; j < MATS * MB * 16 * chunks; j += kThreads) {
         const int c = j % chunks, t = j / chunks % (MB * 16), m = j / chunks / (MB * 16);
-        if (adapter_of(p, t) >= 0) *reinterpret_cast<bf16x8*>(lds + (m * MB * 16 + t) * kRow + c * 16) = low_rank8(p, MATS, m, t, c * 8);
+        if (adapter_of(p, t0 + t) >= 0) *reinterpret_cast<bf16x8*>(lds + (m * MB * 16 + t) * kRow + c * 16) = low_rank8(p, MATS, m, t0 + t, c * 8);
     }
     __syncthreads();
-    const int id = adapter_of(p, lane);
+    const int id = lane < MB * 16 ? adapter_of(p, t0 + lane) : -1;
     int idb[MB];
 #pragma unroll
     for (int b = 0; b < MB; ++b) idb[b] = __shfl(id, b * 16 + r, kWave);
@@ -394,7 +446,7 @@ __global__ __launch_bounds__(kThreads, 4) void adapter_few_kernel(AdapterArgs p)
     }
     __syncthreads();
     for (int j = tid; j < NB * MB * 64; j += kThreads) {
-        const int l = j % 64, b = j / 64 % MB, n = j / 64 / MB, t = b * 16 + (l & 15), col = n0 + n * 16 + (l >> 4) * 4;
+        const int l = j % 64, b = j / 64 % MB, n = j / 64 / MB, t = t0 + b * 16 + (l & 15), col = n0 + n * 16 + (l >> 4) * 4;
         if (t >= p.T) continue;
         f32x4 v[MATS];
 #pragma unroll
@@ -408,6 +460,13 @@ __global__ __launch_bounds__(kThreads, 4) void adapter_few_kernel(AdapterArgs p)
             }
         }
         const size_t at = (size_t)t * p.N + col;
+        for (int q = 0; q < (p.w[0] ? p.splits : 0); ++q)
+#pragma unroll
+            for (int m = 0; m < MATS; ++m) {
+                const f32x4 o = *reinterpret_cast<const f32x4*>(p.sums + ((size_t)q * MATS + m) * p.T * p.N + at);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[m][i] += o[i];
+            }
         if constexpr (MATS == 2) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[0][i] = silu(v[0][i]) * v[1][i];
@@ -420,23 +479,18 @@ __global__ __launch_bounds__(kThreads, 4) void adapter_few_kernel(AdapterArgs p)
     }
 }
 
-constexpr int kFewTokens = 64;
-
-// Pieces of K and workgroups per block of 32 tokens of low_rank_kernel, for about 512 workgroups.  In a decode batch a block has up to 32 adapters, each
-// with a workgroup of its own.  In a prompt it has one or two; there K is cut first, into up to eight pieces (which the projection's kernel adds
-// up), no finer than 64 elements per wavefront.
+// Pieces of K and workgroups per block of 32 tokens of low_rank_kernel, for about 512 workgroups.  In a prompt a block has one or two adapters: K is
+// cut first, into up to eight pieces (which the projection's kernel adds up), no finer than 64 elements per wavefront.
 struct Split {
     int blocks, lists, parts;
 };
 Split split(const moe_adapter_config& c) {
     Split s;
     s.blocks = (c.T + 31) / 32;
-    const int most = c.adapters < 32 ? (c.adapters < c.T ? c.adapters : c.T) : (c.T < 32 ? c.T : 32);
-    const bool decode = c.T <= kFewTokens;
-    s.lists = decode ? most : 1;
+    const int most = c.adapters < 32 ? c.adapters : 32;
     s.parts = 1;
-    while (s.parts < 8 && s.blocks * s.lists * s.parts < (decode ? 256 : 512) && c.K >= s.parts * 2 * kWaves * 64) s.parts *= 2;
-    if (!decode) s.lists = s.blocks * s.parts * 2 <= 512 ? 512 / (s.blocks * s.parts) : 1;
+    while (s.parts < 8 && s.blocks * s.parts < 512 && c.K >= s.parts * 2 * kWaves * 64) s.parts *= 2;
+    s.lists = s.blocks * s.parts * 2 <= 512 ? 512 / (s.blocks * s.parts) : 1;
     if (s.lists > most) s.lists = most;
     return s;
 }
@@ -450,9 +504,43 @@ void low_rank(const AdapterArgs& p, unsigned grid, hipStream_t s) {
 }
 
 template <int MB, int MATS>
-void few(const AdapterArgs& p, hipStream_t s) {
-    if (p.N >= 32 * 256) hipLaunchKernelGGL((adapter_few_kernel<MB, 2, MATS>), dim3(p.N / 32), dim3(kThreads), 0, s, p);
-    else hipLaunchKernelGGL((adapter_few_kernel<MB, 1, MATS>), dim3(p.N / 16), dim3(kThreads), 0, s, p);
+void join(const AdapterArgs& p, hipStream_t s) {
+    hipLaunchKernelGGL((adapter_join_kernel<MB, 2, MATS>), dim3(p.N / 32, (p.T + MB * 16 - 1) / (MB * 16)), dim3(kThreads), 0, s, p);
+}
+
+// adapter_part_kernel's workgroups per piece of K: the projection's tiles and, per block of tokens, at most so many of adapters.
+struct PartGrid {
+    long long blocks, main, low;
+    int lists, slots;            // adapters per block of tokens at most; workgroups that run at once
+};
+template <class S>
+PartGrid part_grid(const moe_adapter_config& c, int mats) {
+    const int FB = S::BN / mats, block = c.T < S::BM ? c.T : S::BM;
+    PartGrid g;
+    g.blocks = (c.T + S::BM - 1) / S::BM;
+    g.main = g.blocks * ((c.N + FB - 1) / FB);
+    g.lists = c.adapters < block ? c.adapters : block;
+    g.low = g.blocks * g.lists * ((c.rank + FB - 1) / FB);
+    g.slots = 256 * S::PER;
+    return g;
+}
+PartGrid part_grid(const moe_adapter_config& c, int mats) { return c.T <= Flat::BM ? part_grid<Flat>(c, mats) : part_grid<Half>(c, mats); }
+// Pieces of K for adapter_part_kernel; 0: one launch does the projection and the adapters (adapter_rows_kernel).  The former for up to 128 tokens, whose
+// adapters its launch and the join take side by side (4096 -> 2 x 14336, 48 tokens with adapters of rank 64 of their own 122 us in the latter,
+// 110 in the former), and where there are tiles for fewer than half of the CUs (14336 -> 4096, 512 tokens).
+int splits(const moe_adapter_config& c, int mats) {
+    const PartGrid g = part_grid(c, mats);
+    if (c.T > Half::BM && g.main >= 128) return 0;
+    long long n = g.slots / (g.main + g.low), most = c.K / 64 / 4;       // no fewer than four steps each
+    if (n > 8) n = 8;
+    if (n > most) n = most;
+    return n < 1 ? 1 : (int)n;
+}
+template <class S, int MATS>
+void part(const AdapterArgs& p, hipStream_t s) {
+    constexpr int FB = S::BN / MATS;
+    const long long per = (long long)p.lists * ((p.rank + FB - 1) / FB) + (p.w[0] ? (p.N + FB - 1) / FB : 0);
+    hipLaunchKernelGGL((adapter_part_kernel<S, MATS>), dim3((unsigned)((p.T + S::BM - 1) / S::BM * per * p.splits)), dim3(S::THREADS), 0, s, p);
 }
 
 template <class S, int MATS>
@@ -463,36 +551,55 @@ void many(const AdapterArgs& p, hipStream_t s) {
 
 template <int MATS>
 hipError_t launch(AdapterArgs p, const moe_adapter_config& c, hipStream_t s) {
+    p.splits = splits(c, MATS);
+    if (p.splits > 0) {
+        p.parts = p.splits;
+        p.lists = part_grid(c, MATS).lists;
+        if (p.T <= Flat::BM) part<Flat, MATS>(p, s);
+        else part<Half, MATS>(p, s);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        switch (p.T > 48 ? 4 : (p.T + 15) / 16) {
+            case 1: join<1, MATS>(p, s); break;
+            case 2: join<2, MATS>(p, s); break;
+            case 3: join<3, MATS>(p, s); break;
+            default: join<4, MATS>(p, s);
+        }
+        return hipGetLastError();
+    }
     const Split sp = split(c);
     p.parts = sp.parts;
     p.lists = sp.lists;
     low_rank<MATS>(p, (unsigned)(sp.blocks * sp.lists * sp.parts), s);
-    hipError_t e = hipGetLastError();
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (p.T <= kFewTokens) {
-        switch ((p.T + 15) / 16) {
-            case 1: few<1, MATS>(p, s); break;
-            case 2: few<2, MATS>(p, s); break;
-            case 3: few<3, MATS>(p, s); break;
-            default: few<4, MATS>(p, s);
-        }
-    } else {
-        if (cost<Small>(1, p.T, (long long)p.N * MATS) < cost<Wide>(1, p.T, (long long)p.N * MATS)) many<Small, MATS>(p, s);
-        else many<Wide, MATS>(p, s);
-    }
+    if (cost<Small>(1, p.T, (long long)p.N * MATS) < cost<Wide>(1, p.T, (long long)p.N * MATS)) many<Small, MATS>(p, s);
+    else many<Wide, MATS>(p, s);
     return hipGetLastError();
+}
+
+// v: as many pieces as the path of either entry point has
+size_t low_rank_bytes(const moe_adapter_config& c) {
+    int pieces = 1;
+    for (int mats = 1; mats <= 2; ++mats) {
+        const int n = splits(c, mats) > 0 ? splits(c, mats) : split(c).parts;
+        if (n > pieces) pieces = n;
+    }
+    return ((size_t)pieces * 2 * c.T * c.rank * sizeof(float) + 255) / 256 * 256;
 }
 
 }  // namespace
 
 size_t adapter_workspace_bytes(const moe_adapter_config& c) {
-    return (size_t)split(c).parts * 2 * c.T * c.rank * sizeof(float);
+    if (c.T == 0) return 0;
+    const int one = splits(c, 1), two = splits(c, 2);
+    return low_rank_bytes(c) + (size_t)(one > 2 * two ? one : 2 * two) * c.T * c.N * sizeof(float);
 }
 
 hipError_t launch_adapter(const moe_adapter_config& c, int mats, const uint16_t* x, const uint16_t* const w[2], const uint16_t* const a[2],
                           const uint16_t* const b[2], const float* scale, const int32_t* adapter_of, const uint16_t* base, uint16_t* y, float* v,
                           hipStream_t s) {
-    const AdapterArgs p{x, {w[0], w[1]}, {a[0], a[1]}, {b[0], b[1]}, scale, adapter_of, base, v, y, c.T, c.N, c.K, c.adapters, c.rank, 0, 0};
+    const AdapterArgs p{x, {w[0], w[1]}, {a[0], a[1]}, {b[0], b[1]}, scale, adapter_of, base, v, (float*)((char*)v + low_rank_bytes(c)), 0, y, c.T, c.N, c.K, c.adapters, c.rank, 0, 0};
     return mats == 2 ? launch<2>(p, c, s) : launch<1>(p, c, s);
 }
 

@@ -66,13 +66,14 @@ struct Stream {
     uint32_t row_bytes;
     uint32_t skip;        // !KC: bytes of the row in front of the tile
     int left;             // elements of k still to come
-    __device__ static __forceinline__ Stream make(const uint16_t* p, int ld, int rows_or_m0, int k) {
+    // k0: KC, p is that many elements into the rows
+    __device__ static __forceinline__ Stream make(const uint16_t* p, int ld, int rows_or_m0, int k, int k0 = 0) {
         Stream s;
         s.row_bytes = (uint32_t)ld * 2u;
         s.left = k;
         if constexpr (KC) {
             s.base = (uint64_t)(uintptr_t)p;
-            s.range = (uint32_t)rows_or_m0 * s.row_bytes;
+            s.range = (uint32_t)rows_or_m0 * s.row_bytes - (uint32_t)k0 * 2u;
             s.skip = 0;
         } else {
             s.skip = (uint32_t)rows_or_m0 * 2u;
@@ -193,6 +194,10 @@ typedef Shape<256, 256, 2, 4, 32, 4, 1, 100> Deep;
 typedef Shape<128, 256, 1, 4, 32, 3, 2, 95> Pair;
 // Few tiles: a quarter of the work each and three steps under way.
 typedef Shape<128, 128, 2, 4, 64, 4, 1, 60> Small;
+
+// Streaming weights past few rows: three (two) workgroups per CU, 96 (64) KiB under way.
+typedef Shape<64, 64, 2, 2, 64, 3, 3, 60> Flat;
+typedef Shape<128, 128, 2, 4, 64, 2, 2, 60> Half;
 
 // A wavefront's results: MB blocks of 32 rows (up to the shape's: a tile of few rows takes a body with fewer), NB of 32 columns.
 template <class S, int MB>
