@@ -282,7 +282,7 @@ moe_status moe_combine_backward(const moe_config* cfg, const void* dy, const voi
  * Tokens in any order and number per adapter; an id outside 0 .. adapters-1 (by convention -1) is a token without one.
  * Stored [out, in] as everywhere: W [N,K], A [adapters, rank, K], B [adapters, N, rank], bf16.  Adapters of a smaller rank are
  * padded with rows (columns) of zeros.  scale [adapters] fp32 or NULL (1).
- * x A^T is summed and scaled in fp32 and rounded to bf16 before the product with B; the sum of all parts is rounded once.
+ * x A^T is summed and scaled in fp32 and enters the product with B as two bf16 numbers (16 bits); the sum of all parts is rounded once.
  * Limits: N % 64 == 0, K % 64 == 0, N, K <= 2^20, rank % 8 == 0, 8 <= rank <= 128, adapters <= 65536, T*max(N,K)*2 bytes below
  * 4 GiB, else MOE_ERR_UNSUPPORTED.  T == 0 returns MOE_OK and enqueues nothing.  Every pointer 16-byte aligned but adapter_of and scale.
  * workspace: moe_adapter_workspace_size(cfg) bytes.  No atomics: results are bit-reproducible. */

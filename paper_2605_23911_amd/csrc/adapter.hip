@@ -121,10 +121,13 @@ __device__ __forceinline__ void keep_mine(V& acc, V with, bool mine) {
     for (int i = 0; i < (int)(sizeof(V) / 4); ++i) acc[i] = mine ? with[i] : acc[i];
 }
 
-// Eight elements of a token's v: the pieces' sum, rounded to bf16 as the operand that B is multiplied with (as h is for the down
-// projection: its error, 2^-8 of the adapter's part at most per element and of random sign, is below that of rounding y).
-__device__ __forceinline__ bf16x8 low_rank8(const AdapterArgs& p, int mats, int m, int t, int c) {
-    float sum[8];
+// Eight elements of a token's v, the pieces' sum, as two bf16 numbers each: rounded once, v would add 2^-8 of the adapter's part to the error, as much as
+// the result's own rounding; with what the first leaves it is 2^-16, for one more multiplication per `rank` elements of the reduction.
+struct Pair8 {
+    u32x4_t hi, lo;
+};
+__device__ __forceinline__ Pair8 low_rank8(const AdapterArgs& p, int mats, int m, int t, int c) {
+    float sum[8], hi[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
     for (int q = 0; q < p.parts; ++q) {
@@ -133,18 +136,24 @@ __device__ __forceinline__ bf16x8 low_rank8(const AdapterArgs& p, int mats, int 
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[i] += v[i];
     }
-    return __builtin_bit_cast(bf16x8, pack8(sum));
+    Pair8 r;
+    r.hi = pack8(sum);
+    unpack8(r.hi, hi);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = fabsf(hi[i]) < INFINITY ? sum[i] - hi[i] : 0.0f;     // an infinity stays one
+    r.lo = pack8(sum);
+    return r;
 }
 
 __device__ __forceinline__ float silu(float g) { return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
 
-constexpr int kMaxRank = 128;
+constexpr int kMaxRank = 128, kPiece = 64;         // of the rank, at a time
 
 
 // Many tokens: tiles of the projection as in ffn_train.hip, then the adapters of the tile's tokens.
 template <class S, int MATS>
 __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void adapter_rows_kernel(AdapterArgs p) {
-    constexpr int FB = S::BN / MATS, kRow = kMaxRank * 2 + 16, kV = MATS * S::BM * kRow;     // bytes of a token's v in LDS
+    constexpr int FB = S::BN / MATS, kRow = 2 * kPiece * 2 + 16, kV = MATS * S::BM * kRow;   // bytes of a token's v in LDS: a piece of the rank
     __shared__ __attribute__((aligned(1024))) char lds[(S::kLds > kV ? S::kLds : kV) + S::BM * 4];
     const int tm_n = (p.T + S::BM - 1) / S::BM, tn_n = (p.N + FB - 1) / FB;
     const int t = xcd_tile(blockIdx.x, tm_n * tn_n);
@@ -172,36 +181,38 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void adapter_rows_kernel
         }
         // What the rest derives from the thread's number is worked out here, not held in registers through the reduction.
         const int tid2 = body_thread(), lane2 = tid2 % kWave;
-        // the tile's v as bf16
-        for (int j = tid2; j < MATS * S::BM * (p.rank / 8); j += S::THREADS) {
-            const int c = j % (p.rank / 8), row = j / (p.rank / 8) % S::BM, m = j / (p.rank / 8) / S::BM;
-            if (ids[row] >= 0) *reinterpret_cast<bf16x8*>(lds + (m * S::BM + row) * kRow + c * 16) = low_rank8(p, MATS, m, t0 + row, c * 8);
+        const int r = lane2 & 31, half = lane2 >> 5, c0 = wn * S::NB * 32, m2 = MATS == 2 && c0 >= FB ? 1 : 0;
+        int id[MB];
+#pragma unroll
+        for (int m = 0; m < MB; ++m) id[m] = ids[(wm * MB + m) * 32 + r];
+        uint32_t brow[S::NB];              // byte offset of the lane's row of B
+#pragma unroll
+        for (int n = 0; n < S::NB; ++n) {
+            const int col = n0 + c0 - m2 * FB + n * 32 + r;
+            brow[n] = (uint32_t)((col < p.N ? col : p.N - 1) * p.rank + half * 8) * 2u;
         }
-        __syncthreads();
-        {
-            const int r = lane2 & 31, half = lane2 >> 5, c0 = wn * S::NB * 32, m2 = MATS == 2 && c0 >= FB ? 1 : 0;
-            int id[MB];
-            unsigned left[MB];
-    #pragma unroll
-            for (int m = 0; m < MB; ++m) {
-                id[m] = ids[(wm * MB + m) * 32 + r];
-                left[m] = (unsigned)__ballot(id[m] >= 0);
+#pragma unroll 1
+        for (int base = 0; base < p.rank; base += kPiece) {
+            // the tile's v, this piece of the rank
+            const int chunks = (p.rank - base < kPiece ? p.rank - base : kPiece) / 8;
+            for (int j = tid2; j < MATS * S::BM * chunks; j += S::THREADS) {
+                const int c = j % chunks, row = j / chunks % S::BM, m = j / chunks / S::BM;
+                if (ids[row] >= 0) {
+                    const Pair8 v = low_rank8(p, MATS, m, t0 + row, base + c * 8);
+                    char* to = lds + (m * S::BM + row) * kRow + c * 16;
+                    *reinterpret_cast<u32x4_t*>(to) = v.hi;
+                    *reinterpret_cast<u32x4_t*>(to + kPiece * 2) = v.lo;
+                }
             }
-            const uint16_t* brow[S::NB];
-    #pragma unroll
-            for (int n = 0; n < S::NB; ++n) {
-                int col = n0 + c0 - m2 * FB + n * 32 + r;
-                brow[n] = p.b[m2] + (size_t)(col < p.N ? col : p.N - 1) * p.rank;
-            }
-            // The next piece (64 of the rank of an adapter) of B is under way while one is multiplied.
-            int a = -1, c = 0;
-            unsigned here[MB];
-            bf16x8 fb[4][S::NB];
+            __syncthreads();
+            // The adapters of the wavefront's tokens; the next one's piece of B is under way while one is multiplied.
+            unsigned left[MB], here[MB];
+#pragma unroll
+            for (int m = 0; m < MB; ++m) left[m] = (unsigned)__ballot(id[m] >= 0);
+            int a = -1;
+            bf16x8 fb[kPiece / 16][S::NB];
             auto next = [&] {
-                c += 64;
-                if (a >= 0 && c < p.rank) return;
                 a = -1;
-                c = 0;
 #pragma unroll
                 for (int m = MB - 1; m >= 0; --m)
                     if (left[m]) a = __builtin_amdgcn_readlane(id[m], __builtin_ctz(left[m]));
@@ -211,45 +222,46 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void adapter_rows_kernel
                     here[m] = (unsigned)__ballot(id[m] == a);
                     left[m] &= ~here[m];
                 }
-            };
-            auto load = [&] {
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
+                for (int q = 0; q < kPiece / 16; ++q)
 #pragma unroll
                     for (int n = 0; n < S::NB; ++n)
-                        fb[q][n] = c + q * 16 + half * 8 < p.rank ? *reinterpret_cast<const bf16x8*>(brow[n] + (size_t)a * p.N * p.rank + c + q * 16 + half * 8) : zeros8();
+                        fb[q][n] = base + q * 16 + half * 8 < p.rank ? *reinterpret_cast<const bf16x8*>(reinterpret_cast<const char*>(p.b[m2] + (size_t)a * p.N * p.rank + base + q * 16) + brow[n]) : zeros8();
             };
             next();
-            if (a >= 0) load();
             while (a >= 0) {
-                const int a0 = a, c0 = c;
+                const int a0 = a;
                 unsigned h0[MB];
-                bf16x8 f0[4][S::NB];
+                bf16x8 f0[kPiece / 16][S::NB];
 #pragma unroll
                 for (int m = 0; m < MB; ++m) h0[m] = here[m];
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
+                for (int q = 0; q < kPiece / 16; ++q)
 #pragma unroll
                     for (int n = 0; n < S::NB; ++n) f0[q][n] = fb[q][n];
                 next();
-                if (a >= 0) load();
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int at = c0 + q * 16 + half * 8;
-                    if (c0 + q * 16 >= p.rank) break;
+                for (int q = 0; q < kPiece / 16; ++q) {
+                    if (base + q * 16 >= p.rank) break;
+                    const bool in = base + q * 16 + half * 8 < p.rank;
 #pragma unroll
                     for (int m = 0; m < MB; ++m) {
                         if (!h0[m]) continue;
-                        const bf16x8 fv = at < p.rank && id[m] == a0
-                            ? *reinterpret_cast<const bf16x8*>(lds + (m2 * S::BM + (wm * MB + m) * 32 + r) * kRow + at * 2) : zeros8();
+                        const bool mine = id[m] == a0;
+                        const char* from = lds + (m2 * S::BM + (wm * MB + m) * 32 + r) * kRow + (q * 16 + half * 8) * 2;
+                        const bf16x8 hi = in && mine ? *reinterpret_cast<const bf16x8*>(from) : zeros8();
+                        const bf16x8 lo = in && mine ? *reinterpret_cast<const bf16x8*>(from + kPiece * 2) : zeros8();
 #pragma unroll
-                        for (int n = 0; n < S::NB; ++n) keep_mine<f32x16>(acc[n][m], __builtin_amdgcn_mfma_f32_32x32x16_bf16(f0[q][n], fv, acc[n][m], 0, 0, 0), id[m] == a0);
+                        for (int n = 0; n < S::NB; ++n) {
+                            const f32x16 some = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f0[q][n], lo, acc[n][m], 0, 0, 0);
+                            keep_mine<f32x16>(acc[n][m], __builtin_amdgcn_mfma_f32_32x32x16_bf16(f0[q][n], hi, some, 0, 0, 0), mine);
+                        }
                     }
                 }
             }
+            __syncthreads();
         }
-        __syncthreads();
         by_rows<S, FB / 8>(acc, lds, AheadNothing{}, [&](int r, int c, const float* row, Nothing) {
             if (r >= rows || c * 8 >= cols) return;
             float v[8];
@@ -343,7 +355,7 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void adapter_part_kernel
 // matrix); its eight wavefronts share the adapters that occur and are joined through LDS.  Bound by reading B.
 template <int MB, int NB, int MATS>
 __global__ __launch_bounds__(kThreads, 4) void adapter_join_kernel(AdapterArgs p) {
-    constexpr int kRow = kMaxRank * 2 + 16, kV = MATS * MB * 16 * kRow, kPart = kWaves / 2 * MATS * NB * MB * 64 * 16;
+    constexpr int kRow = kMaxRank * 4 + 16, kV = MATS * MB * 16 * kRow, kPart = kWaves / 2 * MATS * NB * MB * 64 * 16;
     __shared__ __attribute__((aligned(1024))) char lds[kPart > kV ? kPart : kV];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid % kWave, r = lane & 15, quad = lane >> 4;
     const int n0 = blockIdx.x * (NB * 16), t0 = blockIdx.y * (MB * 16);
@@ -358,7 +370,12 @@ __global__ __launch_bounds__(kThreads, 4) void adapter_join_kernel(AdapterArgs p
     const int chunks = p.rank / 8;
     for (int j = tid; j < MATS * MB * 16 * chunks; j += kThreads) {
         const int c = j % chunks, t = j / chunks % (MB * 16), m = j / chunks / (MB * 16);
-        if (adapter_of(p, t0 + t) >= 0) *reinterpret_cast<bf16x8*>(lds + (m * MB * 16 + t) * kRow + c * 16) = low_rank8(p, MATS, m, t0 + t, c * 8);
+        if (adapter_of(p, t0 + t) >= 0) {
+            const Pair8 v = low_rank8(p, MATS, m, t0 + t, c * 8);
+            char* to = lds + (m * MB * 16 + t) * kRow + c * 16;
+            *reinterpret_cast<u32x4_t*>(to) = v.hi;
+            *reinterpret_cast<u32x4_t*>(to + kMaxRank * 2) = v.lo;
+        }
     }
     __syncthreads();
     const int id = lane < MB * 16 ? adapter_of(p, t0 + lane) : -1;
@@ -410,10 +427,15 @@ __global__ __launch_bounds__(kThreads, 4) void adapter_join_kernel(AdapterArgs p
             if (!((h0 >> (b * 16)) & 0xffff)) continue;
 #pragma unroll
             for (int m = 0; m < MATS; ++m) {
-                const bf16x8 fv = in && idb[b] == a0 ? *reinterpret_cast<const bf16x8*>(lds + (m * MB * 16 + b * 16 + r) * kRow + (c0 + quad * 8) * 2) : zeros8();
+                const bool mine = idb[b] == a0;
+                const char* from = lds + (m * MB * 16 + b * 16 + r) * kRow + (c0 + quad * 8) * 2;
+                const bf16x8 hi = in && mine ? *reinterpret_cast<const bf16x8*>(from) : zeros8();
+                const bf16x8 lo = in && mine ? *reinterpret_cast<const bf16x8*>(from + kMaxRank * 2) : zeros8();
 #pragma unroll
-                for (int n = 0; n < NB; ++n)
-                    keep_mine<f32x4>(acc[m][n][b], __builtin_amdgcn_mfma_f32_16x16x32_bf16(f0[m][n], fv, acc[m][n][b], 0, 0, 0), idb[b] == a0);
+                for (int n = 0; n < NB; ++n) {
+                    const f32x4 some = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f0[m][n], lo, acc[m][n][b], 0, 0, 0);
+                    keep_mine<f32x4>(acc[m][n][b], __builtin_amdgcn_mfma_f32_16x16x32_bf16(f0[m][n], hi, some, 0, 0, 0), mine);
+                }
             }
         }
     }

@@ -3,8 +3,8 @@
 Bounds, element by element (b = 2^-8 for bf16, f = 2^-24 for fp32), on y = base + x W^T + scale B (A x):
   rounding of y                b |y|
   fp32 sum of W's part         K f |x||W|
-  v = scale A x in fp32        (K + 9) f scale |A||x|  (sum, up to eight pieces, scale), then rounded: b |v|;  both times |B|
-  fp32 sum with B's part       (K + rank) f scale |B||v|
+  v = scale A x in fp32        (K + 9) f scale |A||x|  (sum, up to eight pieces, scale), then two bf16 numbers: b^2 |v|;  both times |B|
+  fp32 sum with B's part       (K + 2 rank) f scale |B||v|
 The gated pair: |d(silu(g) u)| <= 1.1 |u| dg + |silu(g)| du, and 16 f for the sigmoid in fp32.  Second order terms: a factor 1 + 2^-6."""
 import os
 import sys
@@ -97,8 +97,8 @@ class Case:
         for t, i in enumerate(self.ids):
             if 0 <= i < self.n:
                 v = np.abs(s[i] * (a[i] @ x[t]))
-                ev = (self.K + 9) * F32 * np.abs(s[i]) * (np.abs(a[i]) @ np.abs(x[t])) + B * v
-                e[t] += np.abs(b[i]) @ (ev + (self.K + self.rank) * F32 * v)
+                ev = (self.K + 9) * F32 * np.abs(s[i]) * (np.abs(a[i]) @ np.abs(x[t])) + B * B * v
+                e[t] += np.abs(b[i]) @ (ev + (self.K + 2 * self.rank) * F32 * v)
         return y, e
 
 
