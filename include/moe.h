@@ -242,7 +242,7 @@ moe_status moe_forward_staged(const moe_config* cfg, const void* x, const void* 
  *   moe_combine(dx_perm, row_of, weights of 1).  d_topk_w is what the router's gradient starts from.
  * offsets are trusted as in moe_grouped_ffn: ascending, offsets[E] <= R.  Rows from offsets[E] on are
  * not written.  Where T == 0 the tensors of rows may be NULL.
- * Beyond the limits above: d, F <= 2^20, else MOE_ERR_UNSUPPORTED.  No atomics: results are bit-reproducible. */
+ * Beyond the limits above: d, F <= 2^20 and E*d*F <= 2^36, else MOE_ERR_UNSUPPORTED.  No atomics: results are bit-reproducible. */
 
 /* moe_grouped_ffn that keeps the two projections: g = x W_gate^T, u = x W_up^T [R,F] bf16 (rounded once from fp32),
  * h [R,F] = SiLU(g) (.) u from the fp32 values, y_perm [R,d] = h W_down^T.  h is not needed by the backward pass.
@@ -261,7 +261,8 @@ moe_status moe_grouped_ffn_train(const moe_config* cfg, const void* x_perm, cons
  *   dW_gate, dW_up [E,F,d] = dg^T x, du^T x;  dW_down [E,d,F] = dy^T h, over each expert's rows
  * dg, du and h = SiLU(g) (.) u (formed again) are rounded to bf16, the operands of the products that follow; all sums are fp32.
  * dx_perm and each dW may be NULL: it is then not computed.  An expert without rows (and T == 0) has weight
- * gradients of zero, which are written unless MOE_GRAD_ACCUMULATE is set.  Outputs must not overlap inputs.
+ * gradients of zero, which are written unless MOE_GRAD_ACCUMULATE is set.  Outputs must not overlap inputs; calls that may run at
+ * the same time need a workspace each.
  * workspace: moe_ffn_backward_workspace_size(cfg) bytes (dg, du, h: 6*R*F), 256-byte aligned. */
 size_t moe_ffn_backward_workspace_size(const moe_config* cfg);
 moe_status moe_grouped_ffn_backward(const moe_config* cfg, const void* x_perm, const int32_t* offsets,
@@ -285,7 +286,8 @@ moe_status moe_combine_backward(const moe_config* cfg, const void* dy, const voi
  * x A^T is summed and scaled in fp32 and enters the product with B as two bf16 numbers (16 bits); the sum of all parts is rounded once.
  * Limits: N % 64 == 0, K % 64 == 0, N, K <= 2^20, rank % 8 == 0, 8 <= rank <= 128, adapters <= 65536, T*max(N,K)*2 bytes below
  * 4 GiB, else MOE_ERR_UNSUPPORTED.  T == 0 returns MOE_OK and enqueues nothing.  Every pointer 16-byte aligned but adapter_of and scale.
- * workspace: moe_adapter_workspace_size(cfg) bytes.  No atomics: results are bit-reproducible. */
+ * workspace: moe_adapter_workspace_size(cfg) bytes; calls that may run at the same time (other streams, graphs replayed side by side) need
+ * one each.  y (h) must not overlap the inputs, but for base.  No atomics: results are bit-reproducible. */
 typedef struct {
     int32_t T, N, K;           /* tokens, output and input features */
     int32_t adapters, rank;

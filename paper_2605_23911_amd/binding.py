@@ -293,7 +293,7 @@ class _Call:
     __slots__ = ("index", "stream")
 
     def __init__(self, stream=None):
-        self.index, self.stream = -1, stream
+        self.index, self.stream = None, stream
 
     def __call__(self, name, t, shape, dtype, optional=False):
         if t is None:
@@ -309,7 +309,7 @@ class _Call:
         if index != self.index:
             if index < 0:
                 raise ValueError("tensors handed to the MoE library must be contiguous GPU tensors")
-            if self.index >= 0:
+            if self.index is not None:
                 raise ValueError(f"{name} is on cuda:{index}, the other tensors on cuda:{self.index}")
             self.index = index
         if not t.is_contiguous():

@@ -165,6 +165,7 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void adapter_rows_kernel
     const int t0 = tm * S::BM, rows = p.T - t0 < S::BM ? p.T - t0 : S::BM, n0 = tn * FB, cols = p.N - n0 < FB ? p.N - n0 : FB;
     int32_t* const ids = reinterpret_cast<int32_t*>(lds + (S::kLds > kV ? S::kLds : kV));
     for (int i = tid; i < S::BM; i += S::THREADS) ids[i] = adapter_of(p, t0 + i);
+    __syncthreads();           // without a shared projection nothing else stands between this and the reads
     by_height<S>(rows, [&](auto height) {
         constexpr int MB = decltype(height)::value;
         Acc<S, MB> acc;

@@ -60,7 +60,9 @@ constexpr int kMaxWidth = 1 << 20;
 moe_status check_train(const moe_config* c) {
     const moe_status st = check_config(c);
     if (st != MOE_OK) return st;
-    return c->d > kMaxWidth || c->F > kMaxWidth ? MOE_ERR_UNSUPPORTED : MOE_OK;
+    if (c->d > kMaxWidth || c->F > kMaxWidth) return MOE_ERR_UNSUPPORTED;
+    // 2^36 elements per weight tensor (128 GiB): the weight gradients' tiles are counted in 32 bits
+    return (unsigned long long)c->E * c->d * c->F > (1ull << 36) ? MOE_ERR_UNSUPPORTED : MOE_OK;
 }
 
 moe_status check_adapter(const moe_adapter_config* c) {

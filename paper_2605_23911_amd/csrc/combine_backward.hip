@@ -88,7 +88,12 @@ hipError_t launch_combine_backward(const moe_config& c, const uint16_t* dy, cons
     const bool stream = (long long)c.T * c.k * c.d >= (1ll << 26);
     auto go = [&](auto k) {
         constexpr int K = decltype(k)::value;
-        hipLaunchKernelGGL((stream ? combine_backward_kernel<K, true> : combine_backward_kernel<K, false>), dim3(c.T), dim3(kThreads), 0, s, dy, y_perm, row_of, topk_w, c.k, c.d, dy_perm, d_topk_w);
+        constexpr int kMost = 1 << 23;         // a launch has less than 2^32 threads
+        for (int t = 0; t < c.T; t += kMost) {
+            const size_t at = (size_t)t * c.k;
+            hipLaunchKernelGGL((stream ? combine_backward_kernel<K, true> : combine_backward_kernel<K, false>), dim3(c.T - t < kMost ? c.T - t : kMost), dim3(kThreads), 0, s,
+                               dy + (size_t)t * c.d, y_perm, row_of + at, topk_w + at, c.k, c.d, dy_perm, d_topk_w + at);
+        }
     };
     using std::integral_constant;
     switch (c.k) {

@@ -249,6 +249,8 @@ hipError_t launch_gated_keep(const moe_config& c, const uint16_t* x_rows, const 
 
 hipError_t launch_ffn_backward(const moe_config& c, const FfnGrad& p, hipStream_t s) {
     const GradArgs a{p.x, p.wg, p.wu, p.wd, p.g, p.u, p.dy, p.offsets, p.dg, p.du, p.h, p.dx, p.dwg, p.dwu, p.dwd, c.E, c.d, c.F, p.f32, p.add};
+    const bool weights = p.dwg || p.dwu || p.dwd;
+    if (!(weights && !(c.T == 0 && p.add)) && !(p.dx && c.T > 0)) return hipSuccess;      // nothing is wanted
     if (c.T == 0) {            // no rows: weight gradients of zero, unless they are added to
         const size_t n = (size_t)c.E * c.d * c.F * (p.f32 ? 4 : 2) / 16;
         for (void* w : {p.dwg, p.dwu, p.dwd})
@@ -261,7 +263,7 @@ hipError_t launch_ffn_backward(const moe_config& c, const FfnGrad& p, hipStream_
         if (small<Deep>(c, c.d)) go_rows_grad<Small>(a, c, s);
         else go_rows_grad<Deep>(a, c, s);
     }
-    if (p.dwg || p.dwu || p.dwd) {
+    if (weights) {
         const int n = (p.dwg != nullptr) + (p.dwu != nullptr) + (p.dwd != nullptr);
         if (cost<Small>((long long)n * c.E, c.F, c.d) < cost<Pair>((long long)n * c.E, c.F, c.d)) go_weights_grad<Small>(a, s);
         else go_weights_grad<Pair>(a, s);

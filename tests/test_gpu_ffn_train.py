@@ -117,7 +117,11 @@ SHAPES = [
 ]
 
 
-@pytest.mark.parametrize("counts,d,F", SHAPES)
+# enough results for the large tiles: of both projections, of dh (wide F) and of dx (wide d), with whole and ragged blocks and an expert without rows
+LARGE = [([500, 0, 1000, 13], 512, 8192), ([700, 259, 512], 8192, 448)]
+
+
+@pytest.mark.parametrize("counts,d,F", SHAPES + LARGE)
 def test_forward_keeps_the_projections(moe, counts, d, F):
     print("forward", counts, d, F, flush=True)
     b = Block(counts, d, F).to_gpu(moe)
@@ -138,7 +142,7 @@ def test_forward_keeps_the_projections(moe, counts, d, F):
     _close(o["y"], y, ey + B * np.abs(y), "y")
 
 
-@pytest.mark.parametrize("counts,d,F", SHAPES)
+@pytest.mark.parametrize("counts,d,F", SHAPES + LARGE)
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_backward(moe, counts, d, F, dtype):
     print("backward", counts, d, F, dtype, flush=True)
@@ -169,9 +173,10 @@ def test_weight_gradients_are_added(moe, dtype):
     assert (both["dwg"][1] == 0.5).all()
 
 
-def test_rows_of_one_expert_do_not_reach_another(moe):
+@pytest.mark.parametrize("counts,d,F", [([65, 3, 130], 192, 320), ([65, 3, 1430], 512, 8192), ([65, 3, 1430], 8192, 512)])
+def test_rows_of_one_expert_do_not_reach_another(moe, counts, d, F):
     """Rows that hold NaN: only their own expert's results have any, although tiles and steps end inside its neighbours."""
-    b = Block([65, 3, 130], 192, 320, seed=3)
+    b = Block(counts, d, F, seed=3)
     for n in ("x", "g", "u", "dy"):
         b.host[n][65:68] = float("nan")
     b.to_gpu(moe)
