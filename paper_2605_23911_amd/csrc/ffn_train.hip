@@ -230,11 +230,16 @@ void go_weights_grad(const GradArgs& a, hipStream_t s) {
     hipLaunchKernelGGL(weights_grad_kernel<S>, dim3(xcd_run_grid(a.E * ((a.dwg ? fd : 0) + (a.dwu ? fd : 0) + (a.dwd ? df : 0)))), dim3(S::THREADS), 0, s, a);
 }
 
-// Whether the small tiles are faster for rows x N results, from the mean number of rows per expert: the host does not know more.
+// Which tiles for rows x N results, from the mean number of rows per expert (the host does not know more): 0 the large ones, 1 Tall, 2 Small.
+// Tall where an expert may have more than one block of 128 rows: Mixtral shape, backward, us, with / without it: 512 tokens (128 +- 11 rows per expert) 1454 /
+// 1649, 1024 2160 / 2335; at 16 rows per expert it gains nothing (8 experts of 256 x 512, 64 tokens 25.3 / 22.5).
 template <class S>
-bool small(const moe_config& c, long long N) {
+int tiles_for(const moe_config& c, long long N) {
     const long long R = (long long)c.T * c.k, active = R < c.E ? R : c.E, rows = (R + active - 1) / active;
-    return cost<Small>(active, rows, N) < cost<S>(active, rows, N);
+    const bool even = active == 1;
+    const long long large = cost<S>(active, rows, N, even), tall = cost<Tall>(active, rows, N, even), small = cost<Small>(active, rows, N, even);
+    if (large <= small && (large <= tall || rows <= 64)) return 0;
+    return rows > 64 && tall <= small ? 1 : 2;
 }
 
 }  // namespace
@@ -242,8 +247,11 @@ bool small(const moe_config& c, long long N) {
 hipError_t launch_gated_keep(const moe_config& c, const uint16_t* x_rows, const int32_t* offsets, const uint16_t* wg, const uint16_t* wu,
                              uint16_t* g, uint16_t* u, uint16_t* h, hipStream_t s) {
     const GatedArgs a{x_rows, wg, wu, offsets, g, u, h, c.E, c.d, c.F};
-    if (small<Wide>(c, 2ll * c.F)) go_keep<Small>(a, c, s);
-    else go_keep<Wide>(a, c, s);
+    switch (tiles_for<Wide>(c, 2ll * c.F)) {
+        case 0: go_keep<Wide>(a, c, s); break;
+        case 1: go_keep<Tall>(a, c, s); break;
+        default: go_keep<Small>(a, c, s);
+    }
     return hipGetLastError();
 }
 
@@ -257,11 +265,17 @@ hipError_t launch_ffn_backward(const moe_config& c, const FfnGrad& p, hipStream_
             if (w && !p.add) hipLaunchKernelGGL(zero_kernel, dim3((unsigned)(n / 256 + 1 < 4096 ? n / 256 + 1 : 4096)), dim3(256), 0, s, (u32x4_t*)w, n);
         return hipGetLastError();
     }
-    if (small<Deep>(c, c.F)) go_gated_grad<Small>(a, c, s);
-    else go_gated_grad<Deep>(a, c, s);
+    switch (tiles_for<Deep>(c, c.F)) {
+        case 0: go_gated_grad<Deep>(a, c, s); break;
+        case 1: go_gated_grad<Tall>(a, c, s); break;
+        default: go_gated_grad<Small>(a, c, s);
+    }
     if (p.dx) {
-        if (small<Deep>(c, c.d)) go_rows_grad<Small>(a, c, s);
-        else go_rows_grad<Deep>(a, c, s);
+        switch (tiles_for<Deep>(c, c.d)) {
+            case 0: go_rows_grad<Deep>(a, c, s); break;
+            case 1: go_rows_grad<Tall>(a, c, s); break;
+            default: go_rows_grad<Small>(a, c, s);
+        }
     }
     if (weights) {
         const int n = (p.dwg != nullptr) + (p.dwu != nullptr) + (p.dwd != nullptr);

@@ -195,6 +195,8 @@ typedef Shape<128, 256, 1, 4, 32, 3, 2, 95> Pair;
 // Few tiles: a quarter of the work each and three steps under way.
 typedef Shape<128, 128, 2, 4, 64, 4, 1, 60> Small;
 
+// Weights past up to 256 rows per expert in one block: half as wide as Deep, so twice as many tiles (tiles_for in ffn_train.hip).
+typedef Shape<256, 128, 4, 2, 64, 3, 1, 75> Tall;
 // Streaming weights past few rows: three (two) workgroups per CU, 96 (64) KiB under way.
 typedef Shape<64, 64, 2, 2, 64, 3, 3, 60> Flat;
 typedef Shape<128, 128, 2, 4, 64, 2, 2, 60> Half;
@@ -401,9 +403,11 @@ inline unsigned xcd_run_grid(long long total) { return (unsigned)((total + 255) 
 
 // What a launch of `groups` times M x N results takes: rounds of tiles times a tile's area, at the shape's RATE (percent of the large ones').  A tile
 // of few rows takes a body of its height, but no less than half of the large ones' for what it loads of B.
+// `even`: every group has M rows; else M is their mean, and beyond half a block each has half a block more.
 template <class S>
-inline long long cost(long long groups, long long M, long long N) {
-    const long long tiles = groups * ((M + S::BM - 1) / S::BM) * ((N + S::BN - 1) / S::BN), rows = (M + 63) / 64 * 64;
+inline long long cost(long long groups, long long M, long long N, bool even = true) {
+    const long long blocks = even ? groups * ((M + S::BM - 1) / S::BM) : 2 * M <= S::BM ? groups : (groups * (2 * M + S::BM) + 2 * S::BM - 1) / (2 * S::BM);
+    const long long tiles = blocks * ((N + S::BN - 1) / S::BN), rows = (M + 63) / 64 * 64;
     const long long height = rows < S::BM ? (rows > 128 ? rows : S::BM < 128 ? S::BM : 128) : S::BM;
     return (tiles + 256 * S::PER - 1) / (256 * S::PER) * S::PER * height * S::BN * 100 / S::RATE;
 }

@@ -118,7 +118,7 @@ SHAPES = [
 
 
 # enough results for the large tiles: of both projections, of dh (wide F) and of dx (wide d), with whole and ragged blocks and an expert without rows
-LARGE = [([500, 0, 1000, 13], 512, 8192), ([700, 259, 512], 8192, 448)]
+LARGE = [([500, 0, 1000, 13], 512, 8192), ([700, 259, 512], 8192, 448), ([120, 0, 140, 128, 257], 1024, 1088)]
 
 
 @pytest.mark.parametrize("counts,d,F", SHAPES + LARGE)
