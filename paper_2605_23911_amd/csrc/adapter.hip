@@ -1,10 +1,14 @@
 // Low-rank adapters of many requests at once beside a shared projection:
 //   y[t] = (base[t] +) x[t] W^T + scale[a] (x[t] A[a]^T) B[a]^T,   a = adapter_of[t]
 // and the gated pair of two such projections of one input, h = SiLU(gate) (.) up.
-// Two launches.  low_rank_kernel forms v[t] = scale[a] x[t] A[a]^T; the projection's kernel then takes v[t] B[a]^T as `rank` more
-// elements of its reduction, so the result is rounded once and never read back.  Tokens stay in the caller's order: a block
-// of tokens goes through the adapters that occur in it one after the other, the other tokens' v masked to zero.  Tokens of a
-// request lie together in a prompt (one adapter per block); in a decode batch every adapter is needed anyway.
+// Always two launches: v[t] = scale[a] x[t] A[a]^T has to be whole before it meets B.
+//   prompts         low_rank_kernel forms v; adapter_rows_kernel takes v[t] B[a]^T as `rank` more elements of the projection's reduction, so
+//                   the result is rounded once and never read back.
+//   decode batches  adapter_part_kernel forms v and x W^T side by side, in pieces of K where there are few tiles; adapter_join_kernel adds
+//                   v B^T to the sums.  (And projections with few tiles.)
+// Tokens stay in the caller's order: a block of tokens goes through the adapters that occur in it one after the other, the other
+// tokens' v masked to zero.  Tokens of a request lie together in a prompt (one adapter per block); in a decode batch every adapter is
+// needed anyway.
 #include "mma_tile.hpp"
 
 namespace moe {
@@ -22,7 +26,7 @@ struct AdapterArgs {
     int splits;
     uint16_t* y;                      // [T, N]
     int T, N, K, n, rank;
-    int parts, lists;                 // low_rank_kernel: pieces of K, workgroups per token block
+    int parts, lists;                 // pieces of K that v is summed in; adapters' workgroups per block of tokens
 };
 
 constexpr int kThreads = 512, kWaves = kThreads / kWave;       // of the kernels that are not tiled
@@ -35,7 +39,8 @@ __device__ __forceinline__ int adapter_of(const AdapterArgs& p, int t) {
 }
 
 // v: a workgroup takes 32 tokens, one piece of K, and of the adapters that occur in the block every lists-th.  Its eight wavefronts split the
-// piece again and are joined through LDS.  Bound by reading A (once per block of 32 tokens that has the adapter).
+// piece again and are joined through LDS.  Bound by the latency of a few dependent loads: 4096 tokens of K = 4096, two adapters of rank 16 22 us,
+// 1999 of 2048, rank 32 12 us (x read at 1.5 and 0.7 TB/s).
 template <int RB, int MATS>
 __global__ __launch_bounds__(kThreads) void low_rank_kernel(AdapterArgs p) {
     __shared__ float part[kWaves][32][RB * 32 + 1];
@@ -150,7 +155,8 @@ __device__ __forceinline__ float silu(float g) { return g * __builtin_amdgcn_rcp
 constexpr int kMaxRank = 128, kPiece = 64;         // of the rank, at a time
 
 
-// Many tokens: tiles of the projection as in ffn_train.hip, then the adapters of the tile's tokens.
+// Many tokens: tiles of the projection as in ffn_train.hip, then the adapters of the tile's tokens, 64 of the rank at a time.  Bound by the matrix
+// cores at the power-limited clock: 4096 tokens, 4096 -> 2 x 14336, rank 16 770-840 us (1.15-1.25 PFLOP/s); 1999 tokens, 2048 -> 7168 64 us.
 template <class S, int MATS>
 __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void adapter_rows_kernel(AdapterArgs p) {
     constexpr int FB = S::BN / MATS, kRow = 2 * kPiece * 2 + 16, kV = MATS * S::BM * kRow;   // bytes of a token's v in LDS: a piece of the rank
@@ -298,8 +304,9 @@ __device__ __forceinline__ int occurring(const AdapterArgs& p, int t0, int rows,
 }
 
 // Decode batches, and projections with too few tiles for the CUs: the fp32 sums of x W^T over one of `splits` pieces of K, and in the same launch
-// v, one tile per adapter that occurs (its A takes W's place, the rows that have it are kept).  Bound by streaming W and A, of which every
-// workgroup has three steps (48 KiB) under way: 14336 -> 4096 for one token 18 us, 6.5 TB/s.
+// v, one tile per adapter that occurs (its A takes W's place, the rows that have it are kept).  Bound by streaming W and A, of which a CU's
+// three workgroups have 96 KiB under way: 14336 -> 4096 for one token 22 us (5.4 TB/s), 4096 -> 2 x 14336 for 48 tokens with 48 adapters of rank 64
+// 67-75 us (4 TB/s; tiles of 128 features, one workgroup per CU 87, two 83).
 template <class S, int MATS>
 __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void adapter_part_kernel(AdapterArgs p) {
     constexpr int FB = S::BN / MATS;
@@ -353,7 +360,8 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void adapter_part_kernel
 }
 
 // Adds adapter_part_kernel's sums and the adapters' part.  A workgroup takes up to 64 tokens (MB blocks of 16) and NB blocks of 16 features (of each
-// matrix); its eight wavefronts share the adapters that occur and are joined through LDS.  Bound by reading B.
+// matrix); its eight wavefronts share the adapters that occur and are joined through LDS.  Bound by reading B: 48 adapters of rank 64, 2 x 14336
+// features 43 us (4.1 TB/s); one token, 4096 features 6.5 us, a launch.
 template <int MB, int NB, int MATS>
 __global__ __launch_bounds__(kThreads, 4) void adapter_join_kernel(AdapterArgs p) {
     constexpr int kRow = kMaxRank * 4 + 16, kV = MATS * MB * 16 * kRow, kPart = kWaves / 2 * MATS * NB * MB * 64 * 16;
@@ -550,7 +558,7 @@ PartGrid part_grid(const moe_adapter_config& c, int mats) {
 PartGrid part_grid(const moe_adapter_config& c, int mats) { return c.T <= Flat::BM ? part_grid<Flat>(c, mats) : part_grid<Half>(c, mats); }
 // Pieces of K for adapter_part_kernel; 0: one launch does the projection and the adapters (adapter_rows_kernel).  The former for up to 128 tokens, whose
 // adapters its launch and the join take side by side (4096 -> 2 x 14336, 48 tokens with adapters of rank 64 of their own 122 us in the latter,
-// 110 in the former), and where there are tiles for fewer than half of the CUs (14336 -> 4096, 512 tokens).
+// 110 in the former), and where there are tiles for fewer than half of the CUs (2048 -> 2048, 512 tokens with 64 adapters of rank 128 190 us in the latter, 61 in the former).
 int splits(const moe_adapter_config& c, int mats) {
     const PartGrid g = part_grid(c, mats);
     if (c.T > Half::BM && g.main >= 128) return 0;

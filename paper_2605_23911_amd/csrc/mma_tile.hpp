@@ -2,10 +2,11 @@
 // the reduction dimension contiguous: gradients with respect to rows (the weights' rows run along k), gradients with respect to
 // weights (both operands' rows run along k), and the projections with row-major weights beside them.
 //
-// Both operands go global -> LDS by DMA from buffer descriptors, BK of k per step into a ring of buffers; a descriptor's range is the tile's own rows, so what lies beyond a ragged end (rows of the next
-// expert, whatever they hold) arrives as zeros and needs no mask.
-//   operand stored with k contiguous:   LDS rows of 64 k (128 bytes), one ds_read_b128 per MFMA fragment.  Position p of row r
-//       holds 16-byte chunk p ^ ((r >> 1) & 7): sixteen lanes that read one chunk column of sixteen rows hit all 64 banks once.
+// Both operands go global -> LDS by DMA from buffer descriptors, BK of k per step into a ring of buffers; a descriptor's range is the
+// tile's own rows, so what lies beyond a ragged end (rows of the next expert, whatever they hold) arrives as zeros and needs no mask.
+//   operand stored with k contiguous:   LDS rows of BK k (128 or 64 bytes), one ds_read_b128 per MFMA fragment.  Position p of row r
+//       holds 16-byte chunk p ^ ((r >> 1) & 7) (BK 32: p ^ ((r >> 2) & 3)): sixteen lanes that read one chunk column of sixteen
+//       rows hit all 64 banks once.
 //   operand stored with m (n) contiguous: LDS rows of the tile's width, one per k; a fragment is two ds_read_b64_tr_b16, each of
 //       which transposes 4 k x 16 m among sixteen lanes.  32-byte piece q of row k lies at q ^ 2 (k & 3) (two bits of it where the
 //       row has only four pieces): the eight pieces that half a wavefront reads lie in different banks.
@@ -25,7 +26,6 @@ namespace {
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
 
 // The thread's number at the start of a body.  Opaque to the compiler, which would work out what all bodies of a kernel derive from it once, in
 // front of them, and hold it in registers that the tallest body does not have.
@@ -194,7 +194,6 @@ typedef Shape<256, 256, 2, 4, 32, 4, 1, 100> Deep;
 typedef Shape<128, 256, 1, 4, 32, 3, 2, 95> Pair;
 // Few tiles: a quarter of the work each and three steps under way.
 typedef Shape<128, 128, 2, 4, 64, 4, 1, 60> Small;
-
 // Weights past up to 256 rows per expert in one block: half as wide as Deep, so twice as many tiles (tiles_for in ffn_train.hip).
 typedef Shape<256, 128, 4, 2, 64, 3, 1, 75> Tall;
 // Streaming weights past few rows: three (two) workgroups per CU, 96 (64) KiB under way.
