@@ -189,6 +189,20 @@ def test_rows_of_one_expert_do_not_reach_another(moe, counts, d, F):
         assert torch.isfinite(t[:65]).all() and torch.isfinite(t[68:]).all() and torch.isnan(t[65:68]).all()
 
 
+def test_gates_far_from_zero(moe):
+    """SiLU and its slope where exp(-g) overflows and where it vanishes, and at zero: the formula's limits, nothing that is not finite."""
+    b = Block([70, 58], 64, 64, seed=6)
+    far = torch.tensor([-1e30, -1e4, -100.0, -88.5, -50.0, -0.0, 0.0, 50.0, 88.5, 100.0, 1e4, 1e30]).to(torch.bfloat16)
+    b.host["g"][:] = far[torch.arange(128 * 64) % 12].view(128, 64)
+    b.to_gpu(moe)
+    got = b.backward(moe, b.grads(torch.float32, fill=float("nan")))
+    torch.cuda.synchronize()
+    want, bound = b.oracle()
+    for n in ("dx", "dwg", "dwu", "dwd"):
+        r = B if got[n].dtype == torch.bfloat16 else F32
+        _close(got[n], want[n], bound[n] + r * np.abs(want[n]) + 1e-30, n)      # s below the smallest normal number may be zero
+
+
 def test_rows_behind_the_last_expert_stay(moe):
     b = Block([40, 25], 128, 192, seed=4, tail=50)
     for n in ("x", "g", "u", "dy"):
