@@ -263,7 +263,7 @@ moe_status moe_grouped_ffn_train(const moe_config* cfg, const void* x_perm, cons
  * dx_perm and each dW may be NULL: it is then not computed.  An expert without rows (and T == 0) has weight
  * gradients of zero, which are written unless MOE_GRAD_ACCUMULATE is set.  Outputs must not overlap inputs; calls that may run at
  * the same time need a workspace each.
- * workspace: moe_ffn_backward_workspace_size(cfg) bytes (dg, du, h: 6*R*F), 256-byte aligned. */
+ * workspace: moe_ffn_backward_workspace_size(cfg) bytes (dg, du, h: 6*R*F, and partial sums of dx in small launches), 256-byte aligned. */
 size_t moe_ffn_backward_workspace_size(const moe_config* cfg);
 moe_status moe_grouped_ffn_backward(const moe_config* cfg, const void* x_perm, const int32_t* offsets,
                                     const void* W_gate, const void* W_up, const void* W_down,

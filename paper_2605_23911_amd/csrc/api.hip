@@ -399,7 +399,7 @@ moe_status moe_grouped_ffn_train(const moe_config* c, const void* x_perm, const 
 size_t moe_ffn_backward_workspace_size(const moe_config* c) {
     if (check_train(c) != MOE_OK) return 0;
     const size_t rows = align_up((size_t)c->T * c->k * c->F * sizeof(uint16_t));
-    return rows ? 3 * rows : kAlign;
+    return rows ? 3 * rows + align_up(rows_grad_bytes(*c)) : kAlign;
 }
 
 moe_status moe_grouped_ffn_backward(const moe_config* c, const void* x_perm, const int32_t* offsets, const void* W_gate, const void* W_up,
@@ -418,7 +418,7 @@ moe_status moe_grouped_ffn_backward(const moe_config* c, const void* x_perm, con
     char* ws = (char*)workspace;
     const FfnGrad p{(const uint16_t*)x_perm, (const uint16_t*)W_gate, (const uint16_t*)W_up, (const uint16_t*)W_down, (const uint16_t*)g, (const uint16_t*)u,
                     (const uint16_t*)dy_perm, offsets, (uint16_t*)ws, (uint16_t*)(ws + rows), (uint16_t*)(ws + 2 * rows), (uint16_t*)dx_perm,
-                    dW_gate, dW_up, dW_down, flags & MOE_GRAD_F32, flags & MOE_GRAD_ACCUMULATE};
+                    dW_gate, dW_up, dW_down, flags & MOE_GRAD_F32, flags & MOE_GRAD_ACCUMULATE, (float*)(ws + 3 * rows)};
     return hip_status(launch_ffn_backward(*c, p, (hipStream_t)stream));
 }
 

@@ -64,6 +64,8 @@ struct GradArgs {
     void *dwg, *dwu, *dwd;     // bf16 or fp32; null: not wanted
     int E, d, F;
     int f32, add;              // weight gradients in fp32; added to what is there
+    float* sums;               // [pieces][R, d] of dx, where its sum is cut (rows_pieces)
+    int pieces, R;
 };
 
 // dh = dy Wd, and from the tile's dh and the kept g and u: dg, du and h.  dg and du are rounded to bf16, as the operands that the
@@ -115,7 +117,8 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void gated_grad_kernel(G
 }
 
 // dx = dg Wg + du Wu: one sum over 2 F.  Mixtral shape, 8192 rows 1850-1950 us (1.0 PFLOP/s; one expert 1490, 1.29).
-template <class S>
+// CUT: one of `pieces` pieces of that sum (the grid's y) as fp32, for sum_pieces_kernel to add up.
+template <class S, bool CUT = false>
 __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void rows_grad_kernel(GradArgs a) {
     __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
     RowTile t;
@@ -130,14 +133,42 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void rows_grad_kernel(Gr
         constexpr int MB = decltype(height)::value;
         Acc<S, MB> acc;
         clear<S, MB>(acc);
+        const int all = a.F / S::BK, each = CUT ? (2 * all + a.pieces - 1) / a.pieces : 2 * all, from = CUT ? blockIdx.y * each : 0;
 #pragma unroll 1
-        for (int m = 0; m < 2; ++m)
-            multiply<S, MB, true, false>(acc, Stream<true, S::BK>::make((m ? a.du : a.dg) + (size_t)t.row0 * a.F, a.F, t.rows, a.F),
-                                         Stream<false, S::BK>::make((m ? a.wu : a.wg) + (size_t)t.e * a.F * a.d, a.d, n0, a.F), la, lb, a.F / S::BK, lds);
+        for (int m = 0; m < 2; ++m) {              // the gate's part, then the up projection's
+            const int s0 = from - m * all > 0 ? from - m * all : 0, end = from + each - m * all, s1 = end < all ? end : all, k0 = s0 * S::BK, k = (s1 - s0) * S::BK;
+            multiply<S, MB, true, false>(acc, Stream<true, S::BK>::make((m ? a.du : a.dg) + (size_t)t.row0 * a.F + k0, a.F, t.rows, k, k0),
+                                         Stream<false, S::BK>::make((m ? a.wu : a.wg) + ((size_t)t.e * a.F + k0) * a.d, a.d, n0, k), la, lb, s1 - s0, lds);
+        }
+        if constexpr (CUT) {
+            by_rows<S, S::BN / 8>(acc, lds, AheadNothing{}, [&](int r, int c, const float* row, Nothing) {
+                if (r >= t.rows || n0 + c * 8 >= a.d) return;
+                float* to = a.sums + ((size_t)blockIdx.y * a.R + t.row0 + r) * a.d + n0 + c * 8;
+                *reinterpret_cast<f32x4*>(to) = *reinterpret_cast<const f32x4*>(row + c * 8);
+                *reinterpret_cast<f32x4*>(to + 4) = *reinterpret_cast<const f32x4*>(row + c * 8 + 4);
+            });
+            return;
+        }
         by_rows_bf16<S, MB>(acc, lds, [&](int r, int c, u32x4_t v) {
             if (r < t.rows && n0 + c * 8 < a.d) *reinterpret_cast<u32x4_t*>(a.dx + (size_t)(t.row0 + r) * a.d + n0 + c * 8) = v;
         });
     });
+}
+
+// dx from the pieces of its sum, in their order; rows behind the last expert stay.
+__global__ __launch_bounds__(256) void sum_pieces_kernel(GradArgs a) {
+    const size_t at = ((size_t)blockIdx.x * 256 + threadIdx.x) * 8, n = (size_t)a.R * a.d;
+    if (at >= (size_t)a.offsets[a.E] * a.d) return;
+    float sum[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+    for (int p = 0; p < a.pieces; ++p) {
+        float v[8];
+        load8(a.sums + p * n + at, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += v[i];
+    }
+    *reinterpret_cast<u32x4_t*>(a.dx + at) = pack8(sum);
 }
 
 // dW[m, n] = sum over the expert's rows of P[row, m] Q[row, n] for the three matrices in one launch (the tails of three would add
@@ -245,7 +276,26 @@ int tiles_for(const moe_config& c, long long N) {
     return rows > 64 && tall <= small ? 1 : 2;
 }
 
+// Pieces that the sum of dx (2 F long) is cut into: where the small tiles are for fewer than half of the CUs (a dense block of few rows, a narrow layer),
+// no shorter than sixteen steps (the launch that adds them up takes about 4 us).  Backward pass, us, one sum / cut: dense 2048 x 5632, 1 row 85 / 54, 100 rows
+// 111 / 71, 500 143 / 108, 768 x 6848, 11 rows 84 / 34; Mixtral shape, 1 token 719 / 623.
+int rows_pieces(const moe_config& c) {
+    const long long R = (long long)c.T * c.k, active = R < c.E ? R : c.E, rows = active > 0 ? (R + active - 1) / active : 0;
+    const long long tiles = active * ((rows + Small::BM - 1) / Small::BM) * ((c.d + Small::BN - 1) / Small::BN);
+    if (tiles == 0 || tiles >= 128) return 1;
+    long long n = 256 / tiles;
+    const long long most = 2ll * c.F / Small::BK / 16;
+    if (n > 16) n = 16;
+    if (n > most) n = most;
+    return n < 1 ? 1 : (int)n;
+}
+
 }  // namespace
+
+size_t rows_grad_bytes(const moe_config& c) {
+    const int n = rows_pieces(c);
+    return n > 1 ? (size_t)n * c.T * c.k * c.d * sizeof(float) : 0;
+}
 
 hipError_t launch_gated_keep(const moe_config& c, const uint16_t* x_rows, const int32_t* offsets, const uint16_t* wg, const uint16_t* wu,
                              uint16_t* g, uint16_t* u, uint16_t* h, hipStream_t s) {
@@ -259,7 +309,7 @@ hipError_t launch_gated_keep(const moe_config& c, const uint16_t* x_rows, const 
 }
 
 hipError_t launch_ffn_backward(const moe_config& c, const FfnGrad& p, hipStream_t s) {
-    const GradArgs a{p.x, p.wg, p.wu, p.wd, p.g, p.u, p.dy, p.offsets, p.dg, p.du, p.h, p.dx, p.dwg, p.dwu, p.dwd, c.E, c.d, c.F, p.f32, p.add};
+    const GradArgs a{p.x, p.wg, p.wu, p.wd, p.g, p.u, p.dy, p.offsets, p.dg, p.du, p.h, p.dx, p.dwg, p.dwu, p.dwd, c.E, c.d, c.F, p.f32, p.add, p.sums, rows_pieces(c), c.T * c.k};
     const bool weights = p.dwg || p.dwu || p.dwd;
     if (!(weights && !(c.T == 0 && p.add)) && !(p.dx && c.T > 0)) return hipSuccess;      // nothing is wanted
     if (c.T == 0) {            // no rows: weight gradients of zero, unless they are added to
@@ -273,7 +323,11 @@ hipError_t launch_ffn_backward(const moe_config& c, const FfnGrad& p, hipStream_
         case 1: go_gated_grad<Tall>(a, c, s); break;
         default: go_gated_grad<Small>(a, c, s);
     }
-    if (p.dx) {
+    if (p.dx && a.pieces > 1) {
+        const long long tiles = most_blocks(c, Small::BM) * ((a.d + Small::BN - 1) / Small::BN);
+        hipLaunchKernelGGL((rows_grad_kernel<Small, true>), dim3(16 + xcd_grid(tiles), a.pieces), dim3(Small::THREADS), 0, s, a);
+        hipLaunchKernelGGL(sum_pieces_kernel, dim3((unsigned)(((size_t)a.R * a.d / 8 + 255) / 256)), dim3(256), 0, s, a);
+    } else if (p.dx) {
         switch (tiles_for<Deep>(c, c.d)) {
             case 0: go_rows_grad<Deep>(a, c, s); break;
             case 1: go_rows_grad<Tall>(a, c, s); break;

@@ -144,7 +144,9 @@ struct FfnGrad {
     uint16_t* dx;               // null: not wanted; so the three below
     void *dwg, *dwu, *dwd;
     int f32, add;               // weight gradients: in fp32; added to what the buffers hold
+    float* sums;                // rows_grad_bytes(c) of scratch
 };
+size_t rows_grad_bytes(const moe_config& c);
 hipError_t launch_ffn_backward(const moe_config& c, const FfnGrad& p, hipStream_t s);
 hipError_t launch_combine_backward(const moe_config& c, const uint16_t* dy, const uint16_t* y_perm, const int32_t* row_of, const float* topk_w,
                                    uint16_t* dy_perm, float* d_topk_w, hipStream_t s);

@@ -114,6 +114,7 @@ class Block:
 SHAPES = [
     ([1], 64, 64), ([2, 0, 1], 128, 64), ([0, 65, 0, 63, 64], 320, 448), ([300, 1, 0, 257], 192, 640), ([128] * 4, 256, 512),
     ([700], 448, 320), ([255, 256, 513], 512, 192), ([5, 17, 0, 33, 1, 90, 2], 1088, 704),
+    ([3], 128, 2112), ([40, 0, 129], 192, 1984),       # dx's sum is cut into pieces, of which the last is shorter
 ]
 
 
@@ -203,8 +204,9 @@ def test_gates_far_from_zero(moe):
         _close(got[n], want[n], bound[n] + r * np.abs(want[n]) + 1e-30, n)      # s below the smallest normal number may be zero
 
 
-def test_rows_behind_the_last_expert_stay(moe):
-    b = Block([40, 25], 128, 192, seed=4, tail=50)
+@pytest.mark.parametrize("F", [192, 2112])
+def test_rows_behind_the_last_expert_stay(moe, F):
+    b = Block([40, 25], 128, F, seed=4, tail=50)
     for n in ("x", "g", "u", "dy"):
         b.host[n][b.n:] = float("nan")
     b.to_gpu(moe)
