@@ -114,6 +114,7 @@ class Block:
 SHAPES = [
     ([1], 64, 64), ([2, 0, 1], 128, 64), ([0, 65, 0, 63, 64], 320, 448), ([300, 1, 0, 257], 192, 640), ([128] * 4, 256, 512),
     ([700], 448, 320), ([255, 256, 513], 512, 192), ([5, 17, 0, 33, 1, 90, 2], 1088, 704),
+    ([(7 * e) % 5 * (e % 3) for e in range(256)], 64, 128), ([0] * 130 + [200] + [0] * 124, 128, 64),        # as many experts as there may be, most without rows
     ([3], 128, 2112), ([40, 0, 129], 192, 1984),       # dx's sum is cut into pieces, of which the last is shorter
 ]
 
@@ -213,7 +214,7 @@ def test_rows_behind_the_last_expert_stay(moe, F):
     got = b.backward(moe, b.grads(fill=7.0))
     fwd = b.forward(moe, fill=7.0)
     torch.cuda.synchronize()
-    for t in (got["dx"], fwd["g"], fwd["u"], fwd["h"]):
+    for t in (got["dx"], fwd["g"], fwd["u"], fwd["h"], fwd["y"]):
         assert (t[b.n:] == 7.0).all() and torch.isfinite(t).all()
     assert all(torch.isfinite(got[n]).all() for n in ("dwg", "dwu", "dwd"))
 
