@@ -604,8 +604,11 @@ hipError_t launch(AdapterArgs p, const moe_adapter_config& c, hipStream_t s) {
     low_rank<MATS>(p, (unsigned)(sp.blocks * sp.lists * sp.parts), s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (cost<Small>(1, p.T, (long long)p.N * MATS) < cost<Wide>(1, p.T, (long long)p.N * MATS)) many<Small, MATS>(p, s);
-    else many<Wide, MATS>(p, s);
+    // us, without / with Tall: gated 4096 -> 2 x 14336, 200 tokens 84 / 69; 14336 -> 4096, 2048 tokens 265 / 229; 7168 -> 2048, 3000 129 / 108; others even
+    const long long N = (long long)p.N * MATS, wide = cost<Wide>(1, p.T, N), tall = cost<Tall>(1, p.T, N), small = cost<Small>(1, p.T, N);
+    if (wide <= tall && wide <= small) many<Wide, MATS>(p, s);
+    else if (tall <= small) many<Tall, MATS>(p, s);
+    else many<Small, MATS>(p, s);
     return hipGetLastError();
 }
 

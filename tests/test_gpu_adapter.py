@@ -148,7 +148,7 @@ def test_wide_tiles_and_many_workgroups(moe, T):
 
 
 @pytest.mark.parametrize("T,N,rank,kind,two", [(700, 8192, 128, "mixed", True), (700, 8192, 24, "requests", True), (1400, 8192, 72, "requests", False),
-                                               (1400, 8192, 8, "own", False), (300, 8192, 104, "own", False)])
+                                               (1400, 8192, 8, "own", False), (300, 8192, 104, "own", False), (200, 14336, 72, "mixed", True), (200, 28672, 16, "requests", False)])
 def test_large_tiles(moe, T, N, rank, kind, two):
     """Prompts with enough tiles for one launch of the projection and its adapters, ranks of one and two pieces, blocks of one adapter and of many."""
     c = Case(T, N, 192, 9, rank, kind, two=two, seed=5).gpu(moe)
@@ -161,7 +161,7 @@ def test_large_tiles(moe, T, N, rank, kind, two):
     _close(c.gated(moe), act * u, np.abs(u) * (1.1 * eg + 16 * F32 * np.abs(act)) + np.abs(act) * eu + B * np.abs(act * u), "h")
 
 
-@pytest.mark.parametrize("T,kind,N", [(5, "mixed", 320), (200, "requests", 320), (300, "mixed", 8192), (1400, "requests", 8192)])
+@pytest.mark.parametrize("T,kind,N", [(5, "mixed", 320), (200, "requests", 320), (300, "mixed", 8192), (1400, "requests", 8192), (200, "mixed", 28672)])
 def test_without_the_shared_projection(moe, T, kind, N):
     c = Case(T, N, 192, 6, 16, kind, base=True).gpu(moe)
     y, e = c.want(0, shared=False)
@@ -180,7 +180,7 @@ def test_base_may_be_the_result(moe, T):
     assert torch.equal(y, want)
 
 
-@pytest.mark.parametrize("T,N", [(9, 192), (120, 192), (300, 192), (300, 8192), (1400, 8192)])
+@pytest.mark.parametrize("T,N", [(9, 192), (120, 192), (300, 192), (300, 8192), (1400, 8192), (200, 28672)])
 def test_a_token_s_result_is_its_own(moe, T, N):
     """Tokens and adapters that hold NaN or infinities reach nobody else's result."""
     c = Case(T, N, 256, 5, 24, "mixed", seed=3)
