@@ -10,7 +10,9 @@ namespace moe {
 
 namespace {
 
-// s = sigmoid(g); exp(-g) = inf gives 0.  v_rcp_f32 and v_exp_f32 (1 ulp each): what is formed from s is rounded to bf16.
+// s = sigmoid(g); exp(-g) = inf gives 0.  The exponential's argument g log2(e) is rounded, so its relative error grows with the gate: with v_exp_f32 and v_rcp_f32 at
+// 1 ulp each s is off by ((2 |g| + 2)(1 - s) + 3) 2^-24 of itself at most, 2^-16 at g = -88, below which s (under 2^-126) is zero.  What is formed from
+// s is rounded to bf16, 2^-8.
 __device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
 
 struct GatedArgs {
