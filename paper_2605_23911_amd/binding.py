@@ -125,6 +125,9 @@ def lib() -> C.CDLL:
     L.moe_test_map_launch.restype = C.c_int32  # test hook (host arithmetic only), not part of include/moe.h
     L.moe_test_map_launch.argtypes = [C.c_int32] * 9 + [i32p, i32p, C.c_int32, i32p, C.c_int32, C.c_int32, C.c_int32,
                                       C.c_int32, i32p]
+    for n, p in (("moe_test_train_tiles", cfgp), ("moe_test_adapter_tiles", acfgp)):   # test hooks (host arithmetic only), not part of include/moe.h
+        getattr(L, n).restype = C.c_int32
+        getattr(L, n).argtypes = [p, C.c_int32]
     _lib = L
     return L
 
@@ -219,6 +222,17 @@ def map_launch(gateup: bool, ib: int, wnt: bool, N: int, M: int, offsets, blocks
     if grid < 0:
         raise MoEError(f"moe_test_map_launch refused (gateup={gateup}, ib={ib})")
     return out[:grid, :8 if runs else 6]
+
+
+def train_tiles(cfg, product: str) -> str:
+    """Test hook: the tiles that the training entry points take for a product: "forward" (the two projections), "dh", "dx", or "dw" (all three weight gradients)."""
+    large = {"forward": "Wide", "dh": "Deep", "dx": "Deep", "dw": "Pair"}
+    return (large[product], "Tall", "Small", "Small, sum in pieces")[lib().moe_test_train_tiles(C.byref(cfg), list(large).index(product))]
+
+
+def adapter_tiles(cfg, matrices: int) -> str:
+    """Test hook: the tiles of moe_adapter_linear (one matrix) or moe_adapter_gated_up (two); Flat and Half are the launches whose sums are joined afterwards."""
+    return ("Wide", "Tall", "Small", "Flat", "Half")[lib().moe_test_adapter_tiles(C.byref(cfg), matrices)]
 
 
 def forward_workspace_layout(cfg) -> WorkspaceLayout:

@@ -580,6 +580,13 @@ void many(const AdapterArgs& p, hipStream_t s) {
     hipLaunchKernelGGL((adapter_rows_kernel<S, MATS>), dim3(xcd_grid(tiles)), dim3(S::THREADS), 0, s, p);
 }
 
+// Tiles of adapter_rows_kernel: 0 Wide, 1 Tall, 2 Small.
+// us, without / with Tall: gated 4096 -> 2 x 14336, 200 tokens 84 / 69; 14336 -> 4096, 2048 tokens 265 / 229; 7168 -> 2048, 3000 129 / 108; others even
+int rows_tiles(const moe_adapter_config& c, int mats) {
+    const long long N = (long long)c.N * mats, wide = cost<Wide>(1, c.T, N), tall = cost<Tall>(1, c.T, N), small = cost<Small>(1, c.T, N);
+    return wide <= tall && wide <= small ? 0 : tall <= small ? 1 : 2;
+}
+
 template <int MATS>
 hipError_t launch(AdapterArgs p, const moe_adapter_config& c, hipStream_t s) {
     p.splits = splits(c, MATS);
@@ -604,11 +611,11 @@ hipError_t launch(AdapterArgs p, const moe_adapter_config& c, hipStream_t s) {
     low_rank<MATS>(p, (unsigned)(sp.blocks * sp.lists * sp.parts), s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    // us, without / with Tall: gated 4096 -> 2 x 14336, 200 tokens 84 / 69; 14336 -> 4096, 2048 tokens 265 / 229; 7168 -> 2048, 3000 129 / 108; others even
-    const long long N = (long long)p.N * MATS, wide = cost<Wide>(1, p.T, N), tall = cost<Tall>(1, p.T, N), small = cost<Small>(1, p.T, N);
-    if (wide <= tall && wide <= small) many<Wide, MATS>(p, s);
-    else if (tall <= small) many<Tall, MATS>(p, s);
-    else many<Small, MATS>(p, s);
+    switch (rows_tiles(c, MATS)) {
+        case 0: many<Wide, MATS>(p, s); break;
+        case 1: many<Tall, MATS>(p, s); break;
+        default: many<Small, MATS>(p, s);
+    }
     return hipGetLastError();
 }
 
@@ -638,3 +645,10 @@ hipError_t launch_adapter(const moe_adapter_config& c, int mats, const uint16_t*
 }
 
 }  // namespace moe
+
+// Test hook (host arithmetic only, not part of include/moe.h): the tiles of a call with `mats` matrices.
+// 0: Wide, 1: Tall, 2: Small (adapter_rows_kernel); 3: Flat, 4: Half (adapter_part_kernel).
+extern "C" __attribute__((visibility("default"))) int32_t moe_test_adapter_tiles(const moe_adapter_config* c, int32_t mats) {
+    using namespace moe;
+    return splits(*c, mats) > 0 ? (c->T <= Flat::BM ? 3 : 4) : rows_tiles(*c, mats);
+}

@@ -292,6 +292,9 @@ int rows_pieces(const moe_config& c) {
     return n < 1 ? 1 : (int)n;
 }
 
+// Weight gradients, n matrices of every expert: Small instead of Pair.
+bool small_weight_tiles(const moe_config& c, int n) { return cost<Small>((long long)n * c.E, c.F, c.d) < cost<Pair>((long long)n * c.E, c.F, c.d); }
+
 }  // namespace
 
 size_t rows_grad_bytes(const moe_config& c) {
@@ -338,10 +341,22 @@ hipError_t launch_ffn_backward(const moe_config& c, const FfnGrad& p, hipStream_
     }
     if (weights) {
         const int n = (p.dwg != nullptr) + (p.dwu != nullptr) + (p.dwd != nullptr);
-        if (cost<Small>((long long)n * c.E, c.F, c.d) < cost<Pair>((long long)n * c.E, c.F, c.d)) go_weights_grad<Small>(a, s);
+        if (small_weight_tiles(c, n)) go_weights_grad<Small>(a, s);
         else go_weights_grad<Pair>(a, s);
     }
     return hipGetLastError();
 }
 
 }  // namespace moe
+
+// Test hook (host arithmetic only, not part of include/moe.h): the tiles that a call takes for one of its products.
+// product 0: the forward pass's pair, 1: dh, 2: dx, 3: the weight gradients (all three).  0: the large tiles, 1: Tall, 2: Small, 3: Small with the sum in pieces.
+extern "C" __attribute__((visibility("default"))) int32_t moe_test_train_tiles(const moe_config* c, int32_t product) {
+    using namespace moe;
+    switch (product) {
+        case 0: return tiles_for<Wide>(*c, 2ll * c->F);
+        case 1: return tiles_for<Deep>(*c, c->F);
+        case 2: return rows_pieces(*c) > 1 ? 3 : tiles_for<Deep>(*c, c->d);
+        default: return small_weight_tiles(*c, 3) ? 2 : 0;
+    }
+}
