@@ -310,15 +310,15 @@ class _Call:
         self.index, self.stream = None, stream
 
     def __call__(self, name, t, shape, dtype, optional=False):
-        if t is None:
-            if optional:
-                return None
-            raise ValueError(f"{name} is required")
-        if t.dtype != dtype or t.shape != shape:
+        if t is None and optional:
+            return None
+        if t is not None and (t.dtype != dtype or t.shape != shape):
             raise ValueError(f"{name} has to be {dtype} {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
         return self.raw(name, t)
 
     def raw(self, name, t):
+        if t is None:
+            raise ValueError(f"{name} is required")
         index = t.get_device()
         if index != self.index:
             if index < 0:
