@@ -1,7 +1,7 @@
 /*
- * moe.h - C ABI of the MI355X (gfx950) MoE-layer forward library.
+ * moe.h - C ABI of the MI355X (gfx950) MoE-layer library.
  *
- * One Mixture-of-Experts layer, forward only, as defined in the paper's Sec. 2.1:
+ * One Mixture-of-Experts layer's forward pass, as defined in the paper's Sec. 2.1 (its training operators and low-rank adapters follow at the end):
  *   Eq. 1   s = softmax(W_r x)
  *   Eq. 2   T = top-k(s) = {(e_i, w_i)}
  *   Eq. 3   y = sum_i w_i * FFN_{e_i}(x)
@@ -25,7 +25,7 @@
  *   - Limits: 1 <= k <= E <= 256, d % 64 == 0, F % 64 == 0, T >= 0, T*k <= 2^30, and the
  *     activation buffers (x, x_perm, h: T*k*max(d,F) elements of 2 bytes) below 4 GiB: the GEMM
  *     kernels address their rows with 32-bit byte offsets.  Beyond: MOE_ERR_UNSUPPORTED.
- *     T == 0 returns MOE_OK and enqueues nothing.
+ *     T == 0 returns MOE_OK and enqueues nothing (but moe_grouped_ffn_backward: weight gradients of zero are written).
  *   - Stream capture: the calls record kernel launches only and may be captured into a HIP
  *     graph; replays equal the eager result.  The first use of a GEMM kernel in a process sets
  *     a function attribute (its LDS size), which HIP does not allow during capture: run the
@@ -47,9 +47,9 @@ typedef enum {
     MOE_OK = 0,
     MOE_ERR_NULL = -1,        /* a required pointer is NULL */
     MOE_ERR_SHAPE = -2,       /* T<0, k<1, k>E, E<1, d<1, F<1, unknown gating */
-    MOE_ERR_ALIGN = -3,       /* a tensor base pointer is not 16-byte aligned */
+    MOE_ERR_ALIGN = -3,       /* a tensor base pointer is not 16-byte aligned (or a buffer not as far as its entry point asks) */
     MOE_ERR_WORKSPACE = -4,   /* workspace smaller than the matching *_workspace_size() */
-    MOE_ERR_UNSUPPORTED = -5, /* E > 256, d % 64 != 0, F % 64 != 0, T*k > 2^30, or T*k*max(d,F)*2 bytes >= 4 GiB */
+    MOE_ERR_UNSUPPORTED = -5, /* E > 256, d % 64 != 0, F % 64 != 0, T*k > 2^30, or T*k*max(d,F)*2 bytes >= 4 GiB; further limits stand with the training and adapter operators */
     MOE_ERR_HIP = -6          /* a kernel launch reported a HIP error */
 } moe_status;
 
@@ -283,7 +283,8 @@ moe_status moe_combine_backward(const moe_config* cfg, const void* dy, const voi
  * Tokens in any order and number per adapter; an id outside 0 .. adapters-1 (by convention -1) is a token without one.
  * Stored [out, in] as everywhere: W [N,K], A [adapters, rank, K], B [adapters, N, rank], bf16.  Adapters of a smaller rank are
  * padded with rows (columns) of zeros.  scale [adapters] fp32 or NULL (1).
- * x A^T is summed and scaled in fp32 and enters the product with B as two bf16 numbers (16 bits); the sum of all parts is rounded once.
+ * x A^T is summed and scaled in fp32 and enters the product with B as two bf16 numbers (16 bits); the sum of all parts is rounded once.  (Hence an
+ * infinity in B comes out as NaN as a rule, not as an infinity: it also meets the second number, which may be zero or of the other sign.)
  * Limits: N % 64 == 0, K % 64 == 0, N, K <= 2^20, rank % 8 == 0, 8 <= rank <= 128, adapters <= 65536, T*max(N,K)*2 bytes below
  * 4 GiB, else MOE_ERR_UNSUPPORTED.  T == 0 returns MOE_OK and enqueues nothing.  Every pointer 16-byte aligned but adapter_of and scale.
  * workspace: moe_adapter_workspace_size(cfg) bytes; calls that may run at the same time (other streams, graphs replayed side by side) need

@@ -155,8 +155,9 @@ __device__ __forceinline__ float silu(float g) { return g * __builtin_amdgcn_rcp
 constexpr int kMaxRank = 128, kPiece = 64;         // of the rank, at a time
 
 
-// Many tokens: tiles of the projection as in ffn_train.hip, then the adapters of the tile's tokens, 64 of the rank at a time.  Bound by the matrix
-// cores at the power-limited clock: 4096 tokens, 4096 -> 2 x 14336, rank 16 770-840 us (1.15-1.25 PFLOP/s); 1999 tokens, 2048 -> 7168 64 us.
+// Many tokens: tiles of the projection as in ffn_train.hip, then the adapters of the tile's tokens, 64 of the rank at a time.  4096 tokens of six
+// prompts, 4096 -> 2 x 14336, rank 16 770-840 us (1.15-1.25 PFLOP/s; matrix cores 61 % busy at 1.8 GHz, the wavefronts wait for 46 % of their cycles); 1999 tokens, 2048 ->
+// 7168 64 us.  Where a block holds many adapters they are what takes the time, two multiplications per 16 of the rank for each (splits, below).
 template <class S, int MATS>
 __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void adapter_rows_kernel(AdapterArgs p) {
     constexpr int FB = S::BN / MATS, kRow = 2 * kPiece * 2 + 16, kV = MATS * S::BM * kRow;   // bytes of a token's v in LDS: a piece of the rank
@@ -557,8 +558,12 @@ PartGrid part_grid(const moe_adapter_config& c, int mats) {
 }
 PartGrid part_grid(const moe_adapter_config& c, int mats) { return c.T <= Flat::BM ? part_grid<Flat>(c, mats) : part_grid<Half>(c, mats); }
 // Pieces of K for adapter_part_kernel; 0: one launch does the projection and the adapters (adapter_rows_kernel).  The former for up to 128 tokens, whose
-// adapters its launch and the join take side by side (4096 -> 2 x 14336, 48 tokens with adapters of rank 64 of their own 122 us in the latter,
-// 110 in the former), and where there are tiles for fewer than half of the CUs (2048 -> 2048, 512 tokens with 64 adapters of rank 128 190 us in the latter, 61 in the former).
+// adapters its launch and the join take side by side, and where there are tiles for fewer than half of the CUs.  us, adapter_rows_kernel / adapter_part_kernel and join:
+//   4096 -> 2 x 14336, 48 tokens, adapters of rank 64 of their own 122 / 110;  2048 -> 2048, 512 tokens, 64 adapters of rank 128 190 / 61;
+//   4096 -> 2 x 14336, 512 tokens: one adapter of rank 16 111 / 200, eight prompts' of rank 128 218 / 256, 64 scattered adapters of rank 64 423 / 432, of rank 128 742 / 719;
+//   14336 -> 4096, 512 tokens: one adapter of rank 16 96 / 104, eight prompts' of rank 64 125 / 156, 64 scattered adapters of rank 16 201 / 187, of rank 128 671 / 294.
+// Neither the number of adapters nor the rank is in the rule: a narrow projection of more than 128 tokens that has 128 tiles or more takes up to 2.5 times as long as it
+// would need where many adapters are scattered over the tokens.
 int splits(const moe_adapter_config& c, int mats) {
     const PartGrid g = part_grid(c, mats);
     if (c.T > Half::BM && g.main >= 128) return 0;

@@ -24,7 +24,9 @@ struct GatedArgs {
 
 // Tile: BM rows x BN / 2 features of both projections: the first half of B's rows are the gate's, the second the up projection's,
 // so that one copy of the token tile in LDS feeds both and the activation needs nothing but the tile.  g and u pass the caches by: the backward pass
-// reads them much later.  Mixtral shape, 8192 rows 2080-2200 us (0.9 PFLOP/s; bound by power: 1.5 GHz, matrix cores 56 % busy).
+// reads them much later.  Mixtral shape, 8192 rows 2030-2200 us (0.9 PFLOP/s).  Bound by waits (the ring holds two steps): the
+// wavefronts spend 49 % of their cycles on them and the matrix cores are 54 % busy at 1.6 GHz, where the inference pair's row-major kernel (which stores h alone) is at 17 % and
+// 66 % at the same clock: 1630-1720 us, of which the 0.46 GB of g and u that are stored beside it here would explain 95.  512 tokens 490 / 365, 16 tokens 362 / 295.
 template <class S>
 __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void gated_keep_kernel(GatedArgs a) {
     __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
@@ -175,7 +177,8 @@ __global__ __launch_bounds__(256) void sum_pieces_kernel(GradArgs a) {
 
 // dW[m, n] = sum over the expert's rows of P[row, m] Q[row, n] for the three matrices in one launch (the tails of three would add
 // up): tiles [expert][matrix][patch].  An expert without rows gets zeros.  Results pass the caches by.  Mixtral shape, 8192 rows 2720-2850 us (1.03
-// PFLOP/s, 2.75 GB written); 64 experts of 250 rows, 3584 x 2560, at skew 1 1480 us, of which 3.5 GB written are 600.
+// PFLOP/s, 2.75 GB written); 64 experts of 250 rows, 3584 x 2560, at skew 1 1480 us, of which 3.5 GB written are 600.  Written / added to, bf16 2830 / 3280 and 1510 / 2560,
+// fp32 3460 / 4050 and 2200 / 3350: what is added to is read item by item where it is stored, and passes through the caches.
 template <class S>
 __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void weights_grad_kernel(GradArgs a) {
     __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
