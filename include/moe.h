@@ -239,7 +239,7 @@ moe_status moe_forward_staged(const moe_config* cfg, const void* x, const void* 
  * program changes with every step.  A layer's step:
  *   moe_route, moe_permute, moe_grouped_ffn_train, moe_combine;
  *   moe_combine_backward, moe_grouped_ffn_backward; dx of a token = the sum of its k rows of dx_perm:
- *   moe_combine(dx_perm, row_of, weights of 1).  d_topk_w is what the router's gradient starts from.
+ *   moe_combine(dx_perm, row_of, weights of 1).  d_topk_w is what the router's gradient (moe_route_backward) starts from.
  * offsets are trusted as in moe_grouped_ffn: ascending, offsets[E] <= R.  Rows from offsets[E] on are
  * not written.  Where T == 0 the tensors of rows may be NULL.
  * Beyond the limits above: d, F <= 2^20 and E*d*F <= 2^36, else MOE_ERR_UNSUPPORTED.  No atomics: results are bit-reproducible. */
@@ -276,6 +276,66 @@ moe_status moe_grouped_ffn_backward(const moe_config* cfg, const void* x_perm, c
  * dy_perm may be y_perm itself. */
 moe_status moe_combine_backward(const moe_config* cfg, const void* dy, const void* y_perm, const int32_t* row_of,
                                 const float* topk_w, void* dy_perm, float* d_topk_w, void* stream);
+
+/* Gradient of moe_route: from d_topk_w [T,k] fp32 (of the weights that it gave for topk_idx) to x, W_r and the bias, at cfg->gating.
+ *   dz = the gate's gradient: MOE_GATE_SOFTMAX p_e (G_e - sum_i p_i d_i) over all experts (p = softmax(z), G_e: d of the slot that chose e, else 0);
+ *        MOE_GATE_SOFTMAX_RENORM w_i (d_i - sum_j w_j d_j) over the chosen; MOE_GATE_SIGMOID_NORM the same times 1 - sigmoid(z_i)
+ *   dx [T,d] bf16 = dz W_r,  dW_r [E,d] = dz^T x (bf16, or fp32 with MOE_GRAD_F32),  dbias [E] fp32 = sum_t dz
+ * z is formed again (fp32 sums; not for MOE_GATE_SOFTMAX_RENORM); dz enters both products as two bf16 numbers (16 bits; an infinite one comes out as NaN).
+ * dx, dW_r and dbias may be NULL: not computed.  MOE_GRAD_ACCUMULATE: dW_r and dbias are added to what the tensors hold.  x's whole gradient: moe_dispatch_backward
+ * with this dx as base.  A slot whose index is outside 0 .. E-1 has no part in anything.  T == 0: dW_r and dbias of zero are written unless they are added to.
+ * Limit: d <= 2^20.  Outputs must not overlap inputs.  workspace: moe_route_backward_workspace_size(cfg) bytes, 256-byte aligned; calls that may run at
+ * the same time need one each. */
+size_t moe_route_backward_workspace_size(const moe_config* cfg);
+moe_status moe_route_backward(const moe_config* cfg, const void* x, const void* W_r, const float* bias, const int32_t* topk_idx, const float* topk_w,
+                              const float* d_topk_w, void* dx, void* dW_r, float* dbias, int32_t flags, void* workspace, size_t ws_bytes, void* stream);
+
+/* ---- Slots that may have no row ------------------------------------------------------------
+ * Permutation and combine for a GPU that holds a share of the experts, or whose experts take a limited number of rows, with their gradients, and with what
+ * a training step does beside them: gate weights applied on the way in, the residual, dropout.  Slot j = t*k+i has a row iff
+ * e = topk_idx[j] - first is in 0 .. E-1 and fewer than `capacity` slots in front of it chose e; its row is offsets[e] plus that number (stable, as in moe_permute).
+ * The rows are what moe_grouped_ffn and the training operators take, with the same T*k (their k <= E: T*k tokens with k = 1 say the same).
+ * Limits: d % 8 == 0, d <= 2^20, k <= 256, E <= 256, T*k <= 2^30, first + E <= 2^31 - 1, else MOE_ERR_UNSUPPORTED (MOE_ERR_SHAPE for the last); sizes in bytes are
+ * not limited.  No atomics on memory: results are bit-reproducible.  row_of below: moe_dispatch's; a number outside 0 .. T*k-1 is a slot without a row, and
+ * no two slots may share one.  Tensors of [T*k,d] hold offsets[E] rows; what lies behind is neither read nor written.  topk_w may be NULL: weights of one.  Outputs
+ * must not overlap inputs but where it is said. */
+typedef struct {
+    int32_t T, d, k;           /* tokens, width, slots per token */
+    int32_t E, first;          /* experts held here: ids first .. first+E-1 */
+    int32_t capacity;          /* rows that an expert takes at most, in order of slots; 0: all */
+} moe_dispatch_config;
+
+size_t moe_dispatch_workspace_size(const moe_dispatch_config* cfg);
+
+/* counts [E] = slots that chose e (before the limit), offsets [E+1] = exclusive sums of the rows taken, row_of [T,k] (-1: none),
+ * src_of [T*k]: slot of a row; rows [T*k,d] bf16 = topk_w[t,i] * x[t,:] (one rounding), or copies.  x and rows may both be NULL: the tables alone.
+ * T == 0 writes counts and offsets of zero.  workspace: moe_dispatch_workspace_size(cfg) bytes; calls that may run at the same time need one each. */
+moe_status moe_dispatch(const moe_dispatch_config* cfg, const void* x, const int32_t* topk_idx, const float* topk_w, int32_t* counts, int32_t* offsets,
+                        int32_t* row_of, int32_t* src_of, void* rows, void* workspace, size_t ws_bytes, void* stream);
+
+/* dx[t,:] = base[t,:] + sum_i topk_w[t,i] * drows[row_of[t,i],:] (fp32, slot order, one rounding); base may be NULL (0), and may be dx.
+ * d_topk_w [T,k] fp32 = <x[t,:], drows[row_of[t,i],:]>, 0 without a row; may be NULL (then x may be, too). */
+moe_status moe_dispatch_backward(const moe_dispatch_config* cfg, const void* x, const void* drows, const int32_t* row_of, const float* topk_w, const void* base,
+                                 void* dx, float* d_topk_w, void* stream);
+
+/* Dropout.  Element n of a tensor (t*d + c in the calls with tokens) is kept with probability 1 - p and divided by it; else it is zero, whatever it was.  The mask is
+ * a function of (rng[0], rng[1], n): Philox4x32-10 with key rng[0] and counter (n / 8, rng[1]) gives 128 bits for eight elements, of which
+ * element n takes 16 (n % 8) .. +15; it is dropped if they are below 65536 p.  p is taken in steps of 2^-16 (so is 1 - p): 0 <= p < 1 - 2^-17, else MOE_ERR_SHAPE.
+ * rng: uint64 [2] ON THE DEVICE, seed and offset, so that a captured step draws another mask at each replay; the gradient's call has to find the
+ * values that its forward call found.  It may be NULL where p == 0. */
+
+/* y[t,:] = residual[t,:] + dropout(sum_i topk_w[t,i] * rows[row_of[t,i],:]): fp32, slot order, one rounding.  A token without rows gets its residual.
+ * residual may be NULL (0), and may be y. */
+moe_status moe_collect(const moe_dispatch_config* cfg, const void* rows, const int32_t* row_of, const float* topk_w, const void* residual, float p, const void* rng,
+                       void* y, void* stream);
+
+/* v = dropout(dy[t,:]):  drows[row_of[t,i],:] = topk_w[t,i] * v (one rounding),  d_topk_w[t,i] = <v, rows[row_of[t,i],:]> (fp32), 0 without a row; may be NULL (then rows
+ * may be, too).  drows may be rows.  The residual's gradient is dy itself. */
+moe_status moe_collect_backward(const moe_dispatch_config* cfg, const void* dy, const void* rows, const int32_t* row_of, const float* topk_w, float p,
+                                const void* rng, void* drows, float* d_topk_w, void* stream);
+
+/* y = residual + dropout(x) over n bf16 elements (n <= 2^40, any), residual may be NULL; y may be x or residual.  Its gradient is the same call on dy, without residual. */
+moe_status moe_dropout(int64_t n, const void* x, const void* residual, float p, const void* rng, void* y, void* stream);
 
 /* ---- Low-rank adapters of many requests beside a shared projection -------------------------
  * Serving requests that have each their own low-rank update of a projection (a shared expert's, a dense block's), in one call:

@@ -26,6 +26,8 @@ EXPORTS = (
     "moe_permute", "moe_permute_static", "moe_block_schedule", "moe_grouped_ffn", "moe_combine", "moe_forward", "moe_forward_staged", "moe_packed_weights_size", "moe_pack_weights", "moe_ffn_kernel_name",
     "moe_grouped_ffn_train", "moe_ffn_backward_workspace_size", "moe_grouped_ffn_backward", "moe_combine_backward",
     "moe_adapter_workspace_size", "moe_adapter_linear", "moe_adapter_gated_up",
+    "moe_route_backward_workspace_size", "moe_route_backward",
+    "moe_dispatch_workspace_size", "moe_dispatch", "moe_dispatch_backward", "moe_collect", "moe_collect_backward", "moe_dropout",
 )
 
 
@@ -52,6 +54,15 @@ class AdapterConfig(C.Structure):
     @classmethod
     def of(cls, T, N, K, adapters, rank):
         return cls(T, N, K, adapters, rank)
+
+
+class DispatchConfig(C.Structure):
+    """moe_dispatch_config: T tokens of width d with k slots each; experts first .. first + E - 1 are here, each for `capacity` rows at most (0: no limit)."""
+    _fields_ = [("T", C.c_int32), ("d", C.c_int32), ("k", C.c_int32), ("E", C.c_int32), ("first", C.c_int32), ("capacity", C.c_int32)]
+
+    @classmethod
+    def of(cls, T, d, k, E, first=0, capacity=0):
+        return cls(T, d, k, E, first, capacity)
 
 
 class WorkspaceLayout(C.Structure):
@@ -120,6 +131,23 @@ def lib() -> C.CDLL:
     L.moe_adapter_linear.argtypes = [acfgp, vp, vp, vp, vp, f32p, i32p, vp, vp, vp, C.c_size_t, vp]
     L.moe_adapter_gated_up.restype = C.c_int
     L.moe_adapter_gated_up.argtypes = [acfgp] + [vp] * 7 + [f32p, i32p, vp, vp, C.c_size_t, vp]
+    L.moe_route_backward_workspace_size.restype = C.c_size_t
+    L.moe_route_backward_workspace_size.argtypes = [cfgp]
+    L.moe_route_backward.restype = C.c_int
+    L.moe_route_backward.argtypes = [cfgp, vp, vp, f32p, i32p, f32p, f32p, vp, vp, f32p, C.c_int32, vp, C.c_size_t, vp]
+    dcfgp = C.POINTER(DispatchConfig)
+    L.moe_dispatch_workspace_size.restype = C.c_size_t
+    L.moe_dispatch_workspace_size.argtypes = [dcfgp]
+    L.moe_dispatch.restype = C.c_int
+    L.moe_dispatch.argtypes = [dcfgp, vp, i32p, f32p, i32p, i32p, i32p, i32p, vp, vp, C.c_size_t, vp]
+    L.moe_dispatch_backward.restype = C.c_int
+    L.moe_dispatch_backward.argtypes = [dcfgp, vp, vp, i32p, f32p, vp, vp, f32p, vp]
+    L.moe_collect.restype = C.c_int
+    L.moe_collect.argtypes = [dcfgp, vp, i32p, f32p, vp, C.c_float, vp, vp, vp]
+    L.moe_collect_backward.restype = C.c_int
+    L.moe_collect_backward.argtypes = [dcfgp, vp, vp, i32p, f32p, C.c_float, vp, vp, f32p, vp]
+    L.moe_dropout.restype = C.c_int
+    L.moe_dropout.argtypes = [C.c_int64, vp, vp, C.c_float, vp, vp, vp]
     L.moe_test_knob.restype = C.c_int32       # test hook, not part of include/moe.h
     L.moe_test_knob.argtypes = [C.c_int32, C.c_int32]
     L.moe_test_map_launch.restype = C.c_int32  # test hook (host arithmetic only), not part of include/moe.h
@@ -380,6 +408,69 @@ def moe_combine_backward(cfg, dy, y_perm, row_of, topk_w, dy_perm, d_topk_w, str
     a.run("moe_combine_backward", lib().moe_combine_backward, C.byref(cfg), a("dy", dy, (T, d), b), a("y_perm", y_perm, (T * k, d), b),
           a("row_of", row_of, (T, k), torch.int32), a("topk_w", topk_w, (T, k), torch.float32), a("dy_perm", dy_perm, (T * k, d), b),
           a("d_topk_w", d_topk_w, (T, k), torch.float32))
+
+
+def route_backward_workspace_size(cfg) -> int:
+    return lib().moe_route_backward_workspace_size(C.byref(cfg))
+
+
+def moe_route_backward(cfg, x, W_r, bias, topk_idx, topk_w, d_topk_w, dx, dW_r, dbias, workspace, accumulate=False, stream=None):
+    """Gradients of moe_route's weights.  dx, dW_r (bf16 or fp32) and dbias (fp32) may be None (not computed); accumulate: dW_r and dbias are added to what they hold."""
+    a, b, f, T, k, d, E = _Call(stream), torch.bfloat16, torch.float32, cfg.T, cfg.k, cfg.d, cfg.E
+    f32 = dW_r is not None and dW_r.dtype == f
+    a.run("moe_route_backward", lib().moe_route_backward, C.byref(cfg), a("x", x, (T, d), b), a("W_r", W_r, (E, d), b), a("bias", bias, (E,), f, True),
+          a("topk_idx", topk_idx, (T, k), torch.int32), a("topk_w", topk_w, (T, k), f), a("d_topk_w", d_topk_w, (T, k), f), a("dx", dx, (T, d), b, True),
+          a("dW_r", dW_r, (E, d), f if f32 else b, True), a("dbias", dbias, (E,), f, True), (GRAD_F32 if f32 else 0) | (GRAD_ACCUMULATE if accumulate else 0),
+          a.raw("workspace", workspace), _nbytes(workspace))
+
+
+# ---- slots that may have no row ------------------------------------------------------------------------------------------
+
+
+def dispatch_workspace_size(cfg) -> int:
+    return lib().moe_dispatch_workspace_size(C.byref(cfg))
+
+
+def moe_dispatch(cfg, x, topk_idx, topk_w, counts, offsets, row_of, src_of, rows, workspace, stream=None):
+    """Tables and expert-contiguous rows of the slots that have one; topk_w None: rows are copies of x, else weighted; x and rows None: the tables alone."""
+    a, b, i, T, k, d, E = _Call(stream), torch.bfloat16, torch.int32, cfg.T, cfg.k, cfg.d, cfg.E
+    a.run("moe_dispatch", lib().moe_dispatch, C.byref(cfg), a("x", x, (T, d), b, rows is None), a("topk_idx", topk_idx, (T, k), i),
+          a("topk_w", topk_w, (T, k), torch.float32, True), a("counts", counts, (E,), i), a("offsets", offsets, (E + 1,), i), a("row_of", row_of, (T, k), i),
+          a("src_of", src_of, (T * k,), i), a("rows", rows, (T * k, d), b, x is None), a.raw("workspace", workspace), _nbytes(workspace))
+
+
+def moe_dispatch_backward(cfg, drows, row_of, topk_w, dx, x=None, d_topk_w=None, base=None, stream=None):
+    """dx = (base +) the weighted sum of a token's rows' gradients; d_topk_w (with x): the weights' gradients.  topk_w None: weights of one."""
+    a, b, f, T, k, d = _Call(stream), torch.bfloat16, torch.float32, cfg.T, cfg.k, cfg.d
+    a.run("moe_dispatch_backward", lib().moe_dispatch_backward, C.byref(cfg), a("x", x, (T, d), b, d_topk_w is None), a("drows", drows, (T * k, d), b),
+          a("row_of", row_of, (T, k), torch.int32), a("topk_w", topk_w, (T, k), f, True), a("base", base, (T, d), b, True), a("dx", dx, (T, d), b),
+          a("d_topk_w", d_topk_w, (T, k), f, True))
+
+
+def _rng(a, rng, p):
+    return a("rng", rng, (2,), torch.int64, p == 0)
+
+
+def moe_collect(cfg, rows, row_of, topk_w, y, residual=None, p=0.0, rng=None, stream=None):
+    """y = (residual +) dropout(weighted sum of a token's rows).  rng: int64 [2] on the GPU, seed and offset of the mask; may be None where p is 0."""
+    a, b, T, k, d = _Call(stream), torch.bfloat16, cfg.T, cfg.k, cfg.d
+    a.run("moe_collect", lib().moe_collect, C.byref(cfg), a("rows", rows, (T * k, d), b), a("row_of", row_of, (T, k), torch.int32),
+          a("topk_w", topk_w, (T, k), torch.float32, True), a("residual", residual, (T, d), b, True), p, _rng(a, rng, p), a("y", y, (T, d), b))
+
+
+def moe_collect_backward(cfg, dy, rows, row_of, topk_w, drows, d_topk_w=None, p=0.0, rng=None, stream=None):
+    """Gradients of moe_collect: of the rows and, where d_topk_w is given (with rows), of the weights.  p and rng as in the forward call."""
+    a, b, f, T, k, d = _Call(stream), torch.bfloat16, torch.float32, cfg.T, cfg.k, cfg.d
+    a.run("moe_collect_backward", lib().moe_collect_backward, C.byref(cfg), a("dy", dy, (T, d), b), a("rows", rows, (T * k, d), b, d_topk_w is None),
+          a("row_of", row_of, (T, k), torch.int32), a("topk_w", topk_w, (T, k), f, True), p, _rng(a, rng, p), a("drows", drows, (T * k, d), b),
+          a("d_topk_w", d_topk_w, (T, k), f, True))
+
+
+def moe_dropout(x, y, p, rng, residual=None, stream=None):
+    """y = (residual +) dropout(x), tensors of one shape.  Its gradient: the same call on dy, without residual."""
+    a, b = _Call(stream), torch.bfloat16
+    px = a("x", x, x.shape if x is not None else (), b)
+    a.run("moe_dropout", lib().moe_dropout, x.shape.numel(), px, a("residual", residual, x.shape, b, True), p, _rng(a, rng, p), a("y", y, x.shape, b))
 
 
 # ---- adapters ------------------------------------------------------------------------------------------------------------

@@ -74,6 +74,26 @@ moe_status check_adapter(const moe_adapter_config* c) {
     return MOE_OK;
 }
 
+moe_status check_dispatch(const moe_dispatch_config* c) {
+    if (c == nullptr) return MOE_ERR_NULL;
+    if (c->T < 0 || c->d < 1 || c->k < 1 || c->E < 1 || c->first < 0 || c->capacity < 0 || c->first > INT32_MAX - c->E) return MOE_ERR_SHAPE;
+    if (c->d % 8 != 0 || c->d > kMaxWidth || c->k > 256 || c->E > kMaxExperts) return MOE_ERR_UNSUPPORTED;
+    if ((long long)c->T * c->k > (1ll << 30)) return MOE_ERR_UNSUPPORTED;
+    return MOE_OK;
+}
+
+// 0 <= p < 1 in steps of 2^-16, none of which is 1; a mask needs its generator's state
+moe_status check_dropout(float p, const void* rng) {
+    if (!(p >= 0.0f) || !((double)p * 65536.0 + 0.5 < 65536.0)) return MOE_ERR_SHAPE;
+    if (p > 0.0f && rng == nullptr) return MOE_ERR_NULL;
+    return (reinterpret_cast<uintptr_t>(rng) & 7u) != 0 ? MOE_ERR_ALIGN : MOE_OK;
+}
+
+moe_status check_route_backward(const moe_config* c) {
+    const moe_status st = check_config(c);
+    return st != MOE_OK ? st : c->d > kMaxWidth ? MOE_ERR_UNSUPPORTED : MOE_OK;
+}
+
 moe_status hip_status(hipError_t e) { return e == hipSuccess ? MOE_OK : MOE_ERR_HIP; }
 
 
@@ -464,6 +484,90 @@ moe_status moe_adapter_gated_up(const moe_adapter_config* c, const void* x, cons
     const uint16_t *const w[2] = {(const uint16_t*)W_gate, (const uint16_t*)W_up}, *const a[2] = {(const uint16_t*)A_gate, (const uint16_t*)A_up},
                    *const b[2] = {(const uint16_t*)B_gate, (const uint16_t*)B_up};
     return hip_status(launch_adapter(*c, 2, (const uint16_t*)x, w, a, b, scale, adapter_of, nullptr, (uint16_t*)h, (float*)workspace, (hipStream_t)stream));
+}
+
+size_t moe_dispatch_workspace_size(const moe_dispatch_config* c) {
+    return check_dispatch(c) == MOE_OK ? align_up(dispatch_workspace_bytes(*c) + 1) : 0;
+}
+
+moe_status moe_dispatch(const moe_dispatch_config* c, const void* x, const int32_t* topk_idx, const float* topk_w, int32_t* counts, int32_t* offsets,
+                        int32_t* row_of, int32_t* src_of, void* rows, void* workspace, size_t ws_bytes, void* stream) {
+    const moe_status st = check_dispatch(c);
+    if (st != MOE_OK) return st;
+    if (!counts || !offsets || !workspace) return MOE_ERR_NULL;
+    if (c->T > 0 && (!topk_idx || !row_of || !src_of || (x == nullptr) != (rows == nullptr))) return MOE_ERR_NULL;
+    if (misaligned(x) || misaligned(rows) || misaligned(workspace)) return MOE_ERR_ALIGN;
+    if (ws_bytes < moe_dispatch_workspace_size(c)) return MOE_ERR_WORKSPACE;
+    return hip_status(launch_dispatch(*c, (const uint16_t*)x, topk_idx, topk_w, counts, offsets, row_of, src_of, (uint16_t*)rows, (int32_t*)workspace,
+                                      (hipStream_t)stream));
+}
+
+moe_status moe_dispatch_backward(const moe_dispatch_config* c, const void* x, const void* drows, const int32_t* row_of, const float* topk_w, const void* base,
+                                 void* dx, float* d_topk_w, void* stream) {
+    const moe_status st = check_dispatch(c);
+    if (st != MOE_OK) return st;
+    if (c->T > 0 && (!drows || !row_of || !dx || (d_topk_w != nullptr && !x))) return MOE_ERR_NULL;
+    for (const void* p : {x, drows, base, (const void*)dx})
+        if (misaligned(p)) return MOE_ERR_ALIGN;
+    if (c->T == 0) return MOE_OK;
+    return hip_status(launch_dispatch_backward(*c, (const uint16_t*)x, (const uint16_t*)drows, row_of, topk_w, (const uint16_t*)base, (uint16_t*)dx, d_topk_w,
+                                               (hipStream_t)stream));
+}
+
+moe_status moe_collect(const moe_dispatch_config* c, const void* rows, const int32_t* row_of, const float* topk_w, const void* residual, float p, const void* rng,
+                       void* y, void* stream) {
+    moe_status st = check_dispatch(c);
+    if (st == MOE_OK) st = check_dropout(p, rng);
+    if (st != MOE_OK) return st;
+    if (c->T > 0 && (!rows || !row_of || !y)) return MOE_ERR_NULL;
+    for (const void* q : {rows, residual, (const void*)y})
+        if (misaligned(q)) return MOE_ERR_ALIGN;
+    if (c->T == 0) return MOE_OK;
+    return hip_status(launch_collect(*c, (const uint16_t*)rows, row_of, topk_w, (const uint16_t*)residual, p, rng, (uint16_t*)y, (hipStream_t)stream));
+}
+
+moe_status moe_collect_backward(const moe_dispatch_config* c, const void* dy, const void* rows, const int32_t* row_of, const float* topk_w, float p,
+                                const void* rng, void* drows, float* d_topk_w, void* stream) {
+    moe_status st = check_dispatch(c);
+    if (st == MOE_OK) st = check_dropout(p, rng);
+    if (st != MOE_OK) return st;
+    if (c->T > 0 && (!dy || !row_of || !drows || (d_topk_w != nullptr && !rows))) return MOE_ERR_NULL;
+    for (const void* q : {dy, rows, (const void*)drows})
+        if (misaligned(q)) return MOE_ERR_ALIGN;
+    if (c->T == 0) return MOE_OK;
+    return hip_status(launch_collect_backward(*c, (const uint16_t*)dy, (const uint16_t*)rows, row_of, topk_w, p, rng, (uint16_t*)drows, d_topk_w,
+                                              (hipStream_t)stream));
+}
+
+moe_status moe_dropout(int64_t n, const void* x, const void* residual, float p, const void* rng, void* y, void* stream) {
+    if (n < 0) return MOE_ERR_SHAPE;
+    const moe_status st = check_dropout(p, rng);
+    if (st != MOE_OK) return st;
+    if (n > (1ll << 40)) return MOE_ERR_UNSUPPORTED;
+    if (n > 0 && (!x || !y)) return MOE_ERR_NULL;
+    if (misaligned(x) || misaligned(residual) || misaligned(y)) return MOE_ERR_ALIGN;
+    if (n == 0) return MOE_OK;
+    return hip_status(launch_dropout(n, (const uint16_t*)x, (const uint16_t*)residual, p, rng, (uint16_t*)y, (hipStream_t)stream));
+}
+
+size_t moe_route_backward_workspace_size(const moe_config* c) {
+    return check_route_backward(c) == MOE_OK ? align_up(route_backward_workspace_bytes(*c) + 1) : 0;
+}
+
+moe_status moe_route_backward(const moe_config* c, const void* x, const void* W_r, const float* bias, const int32_t* topk_idx, const float* topk_w,
+                              const float* d_topk_w, void* dx, void* dW_r, float* dbias, int32_t flags, void* workspace, size_t ws_bytes, void* stream) {
+    const moe_status st = check_route_backward(c);
+    if (st != MOE_OK) return st;
+    if ((flags & ~(MOE_GRAD_F32 | MOE_GRAD_ACCUMULATE)) != 0) return MOE_ERR_SHAPE;
+    if (!W_r || !workspace) return MOE_ERR_NULL;
+    if (c->T > 0 && (!x || !topk_idx || !topk_w || !d_topk_w)) return MOE_ERR_NULL;
+    for (const void* p : {x, W_r, (const void*)dx, (const void*)dW_r})
+        if (misaligned(p)) return MOE_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(workspace) & (kAlign - 1)) != 0) return MOE_ERR_ALIGN;
+    if (ws_bytes < moe_route_backward_workspace_size(c)) return MOE_ERR_WORKSPACE;
+    const RouteGrad p{(const uint16_t*)x, (const uint16_t*)W_r, bias, topk_idx, topk_w, d_topk_w, (uint16_t*)dx, dW_r, dbias,
+                      flags & MOE_GRAD_F32, flags & MOE_GRAD_ACCUMULATE, (char*)workspace};
+    return hip_status(launch_route_backward(*c, p, (hipStream_t)stream));
 }
 
 }  // extern "C"

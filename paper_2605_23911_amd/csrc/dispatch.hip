@@ -1,0 +1,501 @@
+// Tokens sorted by expert, their rows' way back, and the gradients of both, where not every slot has a row.
+//   slot j = t k + i has a row iff e = idx[j] - first is in 0 .. E - 1 and fewer than `capacity` slots in front of j chose e (its rank)
+//   counts[e] = slots that chose e;  offsets = exclusive sums of min(counts, capacity);  row(j) = offsets[e] + rank
+//   dispatch   rows[row(t,i)] = (w[t,i]) x[t]          its gradient  dx[t] = (base[t] +) sum_i (w[t,i]) drows[row(t,i)],  dw[t,i] = <x[t], drows[row(t,i)]>
+//   collect    y[t] = (residual[t] +) D(sum_i (w[t,i]) rows[row(t,i)])
+//              its gradient  v = D(dy[t]), drows[row(t,i)] = (w[t,i]) v,  dw[t,i] = <v, rows[row(t,i)]>
+// Each pass moves every row once, so all four are bound by memory, the small ones by the launch.  No atomics on memory: results are bit-reproducible.
+#include <type_traits>
+
+#include "token_rows.hpp"
+
+namespace moe {
+
+namespace {
+
+constexpr int kChunk = 1024;              // slots per workgroup of the count
+constexpr int kBins = 2048;               // counters in LDS: as many copies of the experts' as fit, so that one wavefront's slots rarely meet
+
+struct DispatchArgs {
+    const uint16_t* x;
+    const int32_t* idx;
+    const float* w;
+    int32_t *counts, *offsets, *row_of, *src_of;
+    uint16_t* rows;
+    int32_t* hist;            // [chunks, E]; null: every workgroup counts all slots itself
+    int T, d, k, E, first, capacity;
+    int per;                  // tokens per workgroup
+    int chunks;
+    bool summed;              // hist holds the counts of all chunks in front, counts the totals
+};
+
+__device__ __forceinline__ int local_expert(const DispatchArgs& a, long long j) {
+    const int e = (int)((uint32_t)a.idx[j] - (uint32_t)a.first);      // wraps for ids below first
+    return (uint32_t)e < (uint32_t)a.E ? e : -1;
+}
+
+// Slots j0 .. j1 - 1 into the bins; those from `split` on into the second half.
+__device__ __forceinline__ void count_slots(const DispatchArgs& a, long long j0, long long j1, long long split, int copies, int* bins) {
+    const int mine = (threadIdx.x & (copies - 1)) * a.E;
+#pragma unroll 4
+    for (long long j = j0 + threadIdx.x; j < j1; j += kTokenThreads) {
+        const int e = local_expert(a, j);
+        if (e >= 0) atomicAdd(&bins[(j >= split ? kBins : 0) + mine + e], 1);
+    }
+}
+__device__ __forceinline__ int bin_copies(int E) {
+    int n = 64;
+    while (n * E > kBins) n >>= 1;
+    return n;
+}
+__device__ __forceinline__ int bin_total(const int* bins, int copies, int E, int e) {
+    int n = 0;
+    for (int c = 0; c < copies; ++c) n += bins[c * E + e];
+    return n;
+}
+
+__global__ __launch_bounds__(kTokenThreads) void count_chunks_kernel(DispatchArgs a) {
+    __shared__ int bins[2 * kBins];
+    const int copies = bin_copies(a.E);
+    for (int i = threadIdx.x; i < copies * a.E; i += kTokenThreads) bins[i] = 0;
+    __syncthreads();
+    const long long R = (long long)a.T * a.k, j0 = (long long)blockIdx.x * kChunk, j1 = j0 + kChunk < R ? j0 + kChunk : R;
+    count_slots(a, j0, j1, j1, copies, bins);
+    __syncthreads();
+    if ((int)threadIdx.x < a.E) a.hist[(size_t)blockIdx.x * a.E + threadIdx.x] = bin_total(bins, copies, a.E, threadIdx.x);
+}
+
+// Exclusive sums over the chunks, 64 experts per workgroup: each wavefront takes a run of chunks, first its total, then, with those of the wavefronts in
+// front, the sums.
+constexpr int kSumThreads = 1024;
+__global__ __launch_bounds__(kSumThreads) void sum_chunks_kernel(DispatchArgs a) {
+    __shared__ int part[kSumThreads / kWave][kWave];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, e = blockIdx.x * kWave + lane;
+    const int each = (a.chunks + kSumThreads / kWave - 1) / (kSumThreads / kWave), c0 = wave * each, c1 = c0 + each < a.chunks ? c0 + each : a.chunks;
+    int n = 0;
+    if (e < a.E) {
+#pragma unroll 8
+        for (int c = c0; c < c1; ++c) n += a.hist[(size_t)c * a.E + e];
+    }
+    part[wave][lane] = n;
+    __syncthreads();
+    if (e >= a.E) return;
+    int at = 0, all = 0;
+    for (int w = 0; w < kSumThreads / kWave; ++w) {
+        if (w < wave) at += part[w][lane];
+        all += part[w][lane];
+    }
+    if (wave == 0) a.counts[e] = all;
+    for (int c = c0; c < c1; ++c) {
+        const int m = a.hist[(size_t)c * a.E + e];
+        a.hist[(size_t)c * a.E + e] = at;
+        at += m;
+    }
+}
+
+// in[t] (after dropout, where there is any) times a slot's weight into its row.  Slots i0 .. of the token; DOT: and <in[t], row of `with`>.
+struct ScatterArgs {
+    const uint16_t* in;
+    const uint16_t* with;
+    uint16_t* out;
+    int d;
+    bool scaled;              // false: rows are copies
+    Dropout p;
+};
+template <int N, bool DOT, bool NT>
+__device__ __forceinline__ void scatter_slots(const ScatterArgs& a, const Slots<N>& s, int t, int lane, int threads, uint64_t seed, uint64_t offset, float (&dot)[N]) {
+    const Row in = row_at(a.in, (size_t)t * a.d * 2, s.any, a.d * 2);
+    Row out[N], with[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        out[i] = s.at(a.out, i, a.d);
+        if constexpr (DOT) with[i] = s.at(a.with, i, a.d);
+        dot[i] = 0.0f;
+    }
+    for (int c = lane * 8; c < a.d; c += threads * 8) {
+        const u32x4_t raw = read8<false>(in, c * 2);
+        u32x4_t other[N];
+        if constexpr (DOT) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) other[i] = read8<NT>(with[i], c * 2);
+        }
+        float v[8];
+        floats8(raw, v);
+        if (a.p.rng) drop8(v, ((uint64_t)t * a.d + c) / 8, seed, offset, a.p);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if constexpr (DOT) {
+                float q[8];
+                floats8(other[i], q);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) dot[i] = fmaf(v[j], q[j], dot[i]);
+            }
+            float o[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] = s.w[i] * v[j];
+            write8<NT>(a.scaled ? bf16s8(o) : raw, out[i], c * 2);
+        }
+    }
+}
+
+// What the lanes of a wavefront did to LDS so far comes before what they do from here on.
+__device__ __forceinline__ void order_lanes() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// A workgroup takes `per` tokens.  It counts the slots in front of its own (all of them, or those of its chunk, with the other chunks' counts from the
+// launch before), sums the experts' totals up, ranks its own slots in order, and moves its tokens' rows: with several tokens a wavefront each.
+template <int N, bool NT>
+__global__ __launch_bounds__(kTokenThreads) void dispatch_kernel(DispatchArgs a) {
+    __shared__ int bins[2 * kBins];
+    __shared__ int next[kMaxExperts], start[kMaxExperts], sums[kTokenWaves];
+    __shared__ int row[kChunk];
+    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const long long R = (long long)a.T * a.k, s0 = (long long)blockIdx.x * a.per * a.k, s1 = s0 + (long long)a.per * a.k < R ? s0 + (long long)a.per * a.k : R;
+    const int copies = bin_copies(a.E);
+    for (int i = tid; i < copies * a.E; i += kTokenThreads) bins[i] = bins[kBins + i] = 0;
+    __syncthreads();
+    const int chunk = (int)(s0 / kChunk);
+    if (a.hist) count_slots(a, (long long)chunk * kChunk, s0, s0, copies, bins);
+    else count_slots(a, 0, R, s0, copies, bins);
+    __syncthreads();
+    int total = 0, before = 0;
+    if (tid < a.E) {
+        before = bin_total(bins, copies, a.E, tid);
+        if (!a.hist) total = before + bin_total(bins + kBins, copies, a.E, tid);
+        else if (a.summed) before += a.hist[(size_t)chunk * a.E + tid], total = a.counts[tid];
+        else {
+#pragma unroll 16
+            for (int c = 0; c < a.chunks; ++c) {
+                const int n = a.hist[(size_t)c * a.E + tid];
+                total += n;
+                before += c < chunk ? n : 0;
+            }
+        }
+    }
+    const int most = a.capacity ? a.capacity : 0x7fffffff, kept = total < most ? total : most;
+    int upto = kept;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+        const int up = __shfl_up(upto, o, kWave);
+        if (lane >= o) upto += up;
+    }
+    if (lane == kWave - 1) sums[wave] = upto;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) upto += sums[w];
+    if (tid < a.E) {
+        next[tid] = before;
+        start[tid] = upto - kept;
+        if (blockIdx.x == 0) {
+            if (!a.summed) a.counts[tid] = total;
+            a.offsets[tid] = upto - kept;
+            if (tid == a.E - 1) a.offsets[a.E] = upto;
+        }
+    }
+    __syncthreads();
+    // ranks: 64 slots at a time; the lanes whose slot chose the same expert are those that agree in all eight bits
+    if (wave == 0) {
+        for (long long j0 = s0; j0 < s1; j0 += kWave) {
+            const long long j = j0 + lane;
+            const int e = j < s1 ? local_expert(a, j) : -1;
+            unsigned long long same = __ballot(e >= 0);
+#pragma unroll
+            for (int b = 0; b < 8; ++b) {
+                const unsigned long long has = __ballot((e >> b) & 1);
+                same &= (e >> b) & 1 ? has : ~has;
+            }
+            const int in_front = __popcll(same & ((1ull << lane) - 1)), base = e >= 0 ? next[e] : 0;
+            order_lanes();                 // every lane has read the count before the first of its expert advances it
+            if (e >= 0 && in_front == 0) next[e] = base + __popcll(same);
+            order_lanes();
+            const int r = e >= 0 && base + in_front < most ? start[e] + base + in_front : -1;
+            if (j < s1) {
+                row[j - s0] = r;
+                a.row_of[j] = r;
+                if (r >= 0) a.src_of[r] = (int32_t)j;
+            }
+        }
+    }
+    if (!a.rows) return;
+    __syncthreads();
+    const ScatterArgs to{a.x, nullptr, a.rows, a.d, a.w != nullptr, {}};
+    const bool whole = a.per < kTokenWaves;
+    const int tokens = (int)((s1 - s0) / a.k), first = (int)(s0 / a.k);
+    for (int t = whole ? 0 : wave; t < tokens; t += whole ? 1 : kTokenWaves) {
+        for (int i0 = 0; i0 < a.k; i0 += N) {
+            Slots<N> s;
+            s.load(row + t * a.k, a.w ? a.w + (size_t)(first + t) * a.k : nullptr, i0, a.k, R);
+            float dot[N];
+            scatter_slots<N, false, NT>(to, s, first + t, whole ? tid : lane, whole ? kTokenThreads : kWave, 0, 0, dot);
+        }
+    }
+}
+
+struct CollectArgs {
+    ScatterArgs to;           // of the gradient
+    const uint16_t *rows, *add, *x;
+    const int32_t* row_of;
+    const float* w;
+    uint16_t* y;
+    float* dw;
+    Dropout p;
+    int T, d, k, t0;
+    bool whole;               // a workgroup per token, else a wavefront
+};
+
+__device__ __forceinline__ int my_token(const CollectArgs& a) {
+    return a.t0 + (a.whole ? (int)blockIdx.x : (int)blockIdx.x * kTokenWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave));
+}
+
+// MANY: more than N slots per token, in batches
+template <int N, bool DOT, bool NT, bool MANY>
+__global__ __launch_bounds__(kTokenThreads) void gather_kernel(CollectArgs a) {
+    __shared__ float part[kTokenWaves][8];
+    const int t = my_token(a);
+    if (t >= a.T) return;
+    const int lane = a.whole ? threadIdx.x : threadIdx.x % kWave, threads = a.whole ? kTokenThreads : kWave;
+    const long long R = (long long)a.T * a.k;
+    const int32_t* row_of = a.row_of + (size_t)t * a.k;
+    const float* w = a.w ? a.w + (size_t)t * a.k : nullptr;
+    const Row add = row_at(a.add, (size_t)t * a.d * 2, a.add != nullptr, a.d * 2), y = row_at(a.y, (size_t)t * a.d * 2, true, a.d * 2);
+    const uint64_t seed = a.p.rng ? a.p.rng[0] : 0, offset = a.p.rng ? a.p.rng[1] : 0;
+    Slots<N> s;
+    if constexpr (!MANY) s.load(row_of, w, 0, a.k, R);
+    float dot[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) dot[i] = 0.0f;
+    const Row x = row_at(a.x, (size_t)t * a.d * 2, DOT && !MANY && s.any, a.d * 2);
+    for (int c = lane * 8; c < a.d; c += threads * 8) {
+        float sum[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
+        const u32x4_t more = read8<false>(add, c * 2);
+        u32x4_t with;
+        if constexpr (DOT && !MANY) with = read8<false>(x, c * 2);
+        auto batch = [&] {
+            u32x4_t v[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = read8<NT>(s.at(a.rows, i, a.d), c * 2);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                float q[8];
+                floats8(v[i], q);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[j] = fmaf(s.w[i], q[j], sum[j]);
+                if constexpr (DOT && !MANY) {
+                    float o[8];
+                    floats8(with, o);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) dot[i] = fmaf(o[j], q[j], dot[i]);
+                }
+            }
+        };
+        if constexpr (MANY) {
+            for (int i0 = 0; i0 < a.k; i0 += N) {
+                s.load(row_of, w, i0, a.k, R);
+                batch();
+            }
+        } else {
+            batch();
+        }
+        if (a.p.rng) drop8(sum, ((uint64_t)t * a.d + c) / 8, seed, offset, a.p);
+        float o[8];
+        floats8(more, o);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] += o[j];
+        write8<false>(bf16s8(sum), y, c * 2);
+    }
+    if constexpr (DOT && !MANY) store_dots<N>(dot, s, part, a.whole, a.k, a.dw + (size_t)t * a.k);
+    if constexpr (DOT && MANY) {           // the rows once more, a batch of slots at a time
+        for (int i0 = 0; i0 < a.k; i0 += N) {
+            s.load(row_of, w, i0, a.k, R);
+            const Row in = row_at(a.x, (size_t)t * a.d * 2, s.any, a.d * 2);
+#pragma unroll
+            for (int i = 0; i < N; ++i) dot[i] = 0.0f;
+            for (int c = lane * 8; c < a.d; c += threads * 8) {
+                float o[8];
+                floats8(read8<false>(in, c * 2), o);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    float q[8];
+                    floats8(read8<false>(s.at(a.rows, i, a.d), c * 2), q);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) dot[i] = fmaf(o[j], q[j], dot[i]);
+                }
+            }
+            store_dots<N>(dot, s, part, a.whole, a.k - i0 < N ? a.k - i0 : N, a.dw + (size_t)t * a.k + i0);
+        }
+    }
+}
+
+template <int N, bool DOT, bool NT>
+__global__ __launch_bounds__(kTokenThreads) void scatter_kernel(CollectArgs a) {
+    __shared__ float part[kTokenWaves][8];
+    const int t = my_token(a);
+    if (t >= a.T) return;
+    const int lane = a.whole ? threadIdx.x : threadIdx.x % kWave, threads = a.whole ? kTokenThreads : kWave;
+    const uint64_t seed = a.to.p.rng ? a.to.p.rng[0] : 0, offset = a.to.p.rng ? a.to.p.rng[1] : 0;
+    for (int i0 = 0; i0 < a.k; i0 += N) {
+        Slots<N> s;
+        s.load(a.row_of + (size_t)t * a.k, a.w ? a.w + (size_t)t * a.k : nullptr, i0, a.k, (long long)a.T * a.k);
+        float dot[N];
+        scatter_slots<N, DOT, NT>(a.to, s, t, lane, threads, seed, offset, dot);
+        if constexpr (DOT) store_dots<N>(dot, s, part, a.whole, a.k - i0 < N ? a.k - i0 : N, a.dw + (size_t)t * a.k + i0);
+    }
+}
+
+template <bool ADD>
+__global__ __launch_bounds__(kTokenThreads) void dropout_kernel(const uint16_t* x, const uint16_t* add, uint16_t* y, long long n, Dropout p) {
+    const uint64_t seed = p.rng ? p.rng[0] : 0, offset = p.rng ? p.rng[1] : 0;
+    for (long long b = (long long)blockIdx.x * kTokenThreads + threadIdx.x; b * 8 < n; b += (long long)gridDim.x * kTokenThreads) {
+        float v[8], o[8];
+        if (b * 8 + 8 <= n) {
+            floats8(reinterpret_cast<const u32x4_t*>(x)[b], v);
+            if (p.rng) drop8(v, b, seed, offset, p);
+            if constexpr (ADD) {
+                floats8(reinterpret_cast<const u32x4_t*>(add)[b], o);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] += o[j];
+            }
+            reinterpret_cast<u32x4_t*>(y)[b] = bf16s8(v);
+        } else {                           // the last, partial block
+            const u32x4_t bits = philox(seed, b, offset);
+            for (int j = 0; b * 8 + j < n; ++j) {
+                float q = bf16_bits_to_float(x[b * 8 + j]);
+                if (p.rng) q = ((j & 1 ? bits[j / 2] >> 16 : bits[j / 2] & 0xffffu) >= p.limit) ? q * p.scale : 0.0f;
+                if constexpr (ADD) q += bf16_bits_to_float(add[b * 8 + j]);
+                y[b * 8 + j] = float_to_bf16_bits(q);
+            }
+        }
+    }
+}
+
+constexpr int kCountAll = 8192;           // slots up to which a workgroup counts them all
+constexpr int kSumInside = 64;            // chunks up to which a workgroup adds their counts up
+
+int chunks_of(const moe_dispatch_config& c) { return (int)(((long long)c.T * c.k + kChunk - 1) / kChunk); }
+
+bool passes_caches(const moe_dispatch_config& c) { return (long long)c.T * c.k * c.d >= (1ll << 26); }
+
+// go(integral_constant<slots per batch>)
+template <class F>
+void by_slots(int k, F&& go) {
+    using std::integral_constant;
+    if (k == 1) go(integral_constant<int, 1>{});
+    else if (k == 2) go(integral_constant<int, 2>{});
+    else if (k <= 4) go(integral_constant<int, 4>{});
+    else go(integral_constant<int, 8>{});
+}
+
+// Tokens of one launch: it has less than 2^32 threads.
+template <class F>
+void by_launch(CollectArgs a, F&& go) {
+    a.whole = a.d > 1024;
+    const int step = a.whole ? 1 << 23 : 1 << 25;
+    for (long long t = 0; t < a.T; t += step) {
+        a.t0 = (int)t;
+        const long long n = a.T - t < step ? a.T - t : step;
+        go(a, dim3((unsigned)(a.whole ? n : (n + kTokenWaves - 1) / kTokenWaves)));
+    }
+}
+
+}  // namespace
+
+size_t dispatch_workspace_bytes(const moe_dispatch_config& c) {
+    return (long long)c.T * c.k > kCountAll ? (size_t)chunks_of(c) * c.E * sizeof(int32_t) : 0;
+}
+
+hipError_t launch_dispatch(const moe_dispatch_config& c, const uint16_t* x, const int32_t* topk_idx, const float* topk_w, int32_t* counts, int32_t* offsets,
+                           int32_t* row_of, int32_t* src_of, uint16_t* rows, int32_t* hist, hipStream_t s) {
+    DispatchArgs a{x, topk_idx, topk_w, counts, offsets, row_of, src_of, rows, nullptr, c.T, c.d, c.k, c.E, c.first, c.capacity, 1, chunks_of(c), false};
+    if ((long long)c.T * c.k > kCountAll) {
+        a.hist = hist;
+        a.summed = a.chunks > kSumInside;
+        hipLaunchKernelGGL(count_chunks_kernel, dim3(a.chunks), dim3(kTokenThreads), 0, s, a);
+        if (a.summed) hipLaunchKernelGGL(sum_chunks_kernel, dim3((c.E + kWave - 1) / kWave), dim3(kSumThreads), 0, s, a);
+    }
+    // about a thousand workgroups; without rows to move, workgroups of a thousand slots
+    const int most = kChunk / c.k;
+    a.per = rows ? (c.T + 1023) / 1024 : most;
+    if (a.per > most) a.per = most;
+    if (a.per < 1) a.per = 1;
+    const unsigned grid = c.T > 0 ? (unsigned)(((long long)c.T + a.per - 1) / a.per) : 1;
+    const bool nt = passes_caches(c);
+    by_slots(c.k, [&](auto n) {
+        constexpr int N = decltype(n)::value;
+        if (nt) hipLaunchKernelGGL((dispatch_kernel<N, true>), dim3(grid), dim3(kTokenThreads), 0, s, a);
+        else hipLaunchKernelGGL((dispatch_kernel<N, false>), dim3(grid), dim3(kTokenThreads), 0, s, a);
+    });
+    return hipGetLastError();
+}
+
+static hipError_t launch_gather(const moe_dispatch_config& c, CollectArgs a, hipStream_t s) {
+    const bool nt = passes_caches(c);
+    by_slots(c.k, [&](auto n) {
+        constexpr int N = decltype(n)::value;
+        by_launch(a, [&](const CollectArgs& b, dim3 grid) {
+            auto go = [&](auto dot, auto many) {
+                constexpr bool DOT = decltype(dot)::value, MANY = decltype(many)::value;
+                if (nt) hipLaunchKernelGGL((gather_kernel<N, DOT, true, MANY>), grid, dim3(kTokenThreads), 0, s, b);
+                else hipLaunchKernelGGL((gather_kernel<N, DOT, false, MANY>), grid, dim3(kTokenThreads), 0, s, b);
+            };
+            if constexpr (N == 8) {
+                if (c.k > N) {
+                    if (b.dw) go(std::true_type{}, std::true_type{});
+                    else go(std::false_type{}, std::true_type{});
+                    return;
+                }
+            }
+            if (b.dw) go(std::true_type{}, std::false_type{});
+            else go(std::false_type{}, std::false_type{});
+        });
+    });
+    return hipGetLastError();
+}
+
+static Dropout dropout_of(float p, const void* rng) {
+    const uint32_t limit = (uint32_t)((double)p * 65536.0 + 0.5);
+    return {limit ? (const uint64_t*)rng : nullptr, limit, 65536.0f / (float)(65536u - limit)};
+}
+
+hipError_t launch_dispatch_backward(const moe_dispatch_config& c, const uint16_t* x, const uint16_t* drows, const int32_t* row_of, const float* topk_w,
+                                    const uint16_t* base, uint16_t* dx, float* d_topk_w, hipStream_t s) {
+    return launch_gather(c, CollectArgs{{}, drows, base, x, row_of, topk_w, dx, d_topk_w, {}, c.T, c.d, c.k, 0, false}, s);
+}
+
+hipError_t launch_collect(const moe_dispatch_config& c, const uint16_t* rows, const int32_t* row_of, const float* topk_w, const uint16_t* residual, float p,
+                          const void* rng, uint16_t* y, hipStream_t s) {
+    return launch_gather(c, CollectArgs{{}, rows, residual, nullptr, row_of, topk_w, y, nullptr, dropout_of(p, rng), c.T, c.d, c.k, 0, false}, s);
+}
+
+hipError_t launch_collect_backward(const moe_dispatch_config& c, const uint16_t* dy, const uint16_t* rows, const int32_t* row_of, const float* topk_w, float p,
+                                   const void* rng, uint16_t* drows, float* d_topk_w, hipStream_t s) {
+    const Dropout drop = dropout_of(p, rng);
+    const CollectArgs a{{dy, rows, drows, c.d, topk_w != nullptr || drop.rng != nullptr, drop}, nullptr, nullptr, nullptr, row_of, topk_w, nullptr, d_topk_w, {}, c.T, c.d, c.k, 0, false};
+    const bool nt = passes_caches(c);
+    by_slots(c.k, [&](auto n) {
+        constexpr int N = decltype(n)::value;
+        by_launch(a, [&](const CollectArgs& b, dim3 grid) {
+            if (b.dw) {
+                if (nt) hipLaunchKernelGGL((scatter_kernel<N, true, true>), grid, dim3(kTokenThreads), 0, s, b);
+                else hipLaunchKernelGGL((scatter_kernel<N, true, false>), grid, dim3(kTokenThreads), 0, s, b);
+            } else {
+                if (nt) hipLaunchKernelGGL((scatter_kernel<N, false, true>), grid, dim3(kTokenThreads), 0, s, b);
+                else hipLaunchKernelGGL((scatter_kernel<N, false, false>), grid, dim3(kTokenThreads), 0, s, b);
+            }
+        });
+    });
+    return hipGetLastError();
+}
+
+hipError_t launch_dropout(long long n, const uint16_t* x, const uint16_t* residual, float p, const void* rng, uint16_t* y, hipStream_t s) {
+    const Dropout drop = dropout_of(p, rng);
+    const long long groups = (n + 8ll * kTokenThreads - 1) / (8ll * kTokenThreads);
+    const dim3 grid((unsigned)(groups < 8192 ? groups : 8192));
+    if (residual) hipLaunchKernelGGL(dropout_kernel<true>, grid, dim3(kTokenThreads), 0, s, x, residual, y, n, drop);
+    else hipLaunchKernelGGL(dropout_kernel<false>, grid, dim3(kTokenThreads), 0, s, x, residual, y, n, drop);
+    return hipGetLastError();
+}
+
+}  // namespace moe

@@ -151,6 +151,36 @@ hipError_t launch_ffn_backward(const moe_config& c, const FfnGrad& p, hipStream_
 hipError_t launch_combine_backward(const moe_config& c, const uint16_t* dy, const uint16_t* y_perm, const int32_t* row_of, const float* topk_w,
                                    uint16_t* dy_perm, float* d_topk_w, hipStream_t s);
 
+// ---- slots that may have no row -----------------------------------------------------------
+// hist: dispatch_workspace_bytes(c) of scratch; x, rows both null: the tables alone
+size_t dispatch_workspace_bytes(const moe_dispatch_config& c);
+hipError_t launch_dispatch(const moe_dispatch_config& c, const uint16_t* x, const int32_t* topk_idx, const float* topk_w, int32_t* counts, int32_t* offsets,
+                           int32_t* row_of, int32_t* src_of, uint16_t* rows, int32_t* hist, hipStream_t s);
+// topk_w may be null (weights of one), base and residual too; d_topk_w null: not wanted
+hipError_t launch_dispatch_backward(const moe_dispatch_config& c, const uint16_t* x, const uint16_t* drows, const int32_t* row_of, const float* topk_w,
+                                    const uint16_t* base, uint16_t* dx, float* d_topk_w, hipStream_t s);
+// p in [0, 1 - 2^-17), rng: seed and offset on the device
+hipError_t launch_collect(const moe_dispatch_config& c, const uint16_t* rows, const int32_t* row_of, const float* topk_w, const uint16_t* residual, float p,
+                          const void* rng, uint16_t* y, hipStream_t s);
+hipError_t launch_collect_backward(const moe_dispatch_config& c, const uint16_t* dy, const uint16_t* rows, const int32_t* row_of, const float* topk_w, float p,
+                                   const void* rng, uint16_t* drows, float* d_topk_w, hipStream_t s);
+hipError_t launch_dropout(long long n, const uint16_t* x, const uint16_t* residual, float p, const void* rng, uint16_t* y, hipStream_t s);
+
+// ---- the router's gradient ----------------------------------------------------------------
+struct RouteGrad {
+    const uint16_t *x, *wr;
+    const float* bias;          // may be null
+    const int32_t* idx;
+    const float *w, *g;         // gate weights and their gradients
+    uint16_t* dx;               // null: not wanted; so the two below
+    void* dwr;                  // fp32 if f32, else bf16
+    float* dbias;
+    int f32, add;               // add: dwr and dbias are added to what they hold
+    char* workspace;
+};
+size_t route_backward_workspace_bytes(const moe_config& c);
+hipError_t launch_route_backward(const moe_config& c, const RouteGrad& p, hipStream_t s);
+
 // ---- adapters -----------------------------------------------------------------------------
 size_t adapter_workspace_bytes(const moe_adapter_config& c);
 // mats: 1 (w[0], a[0], b[0]; base may be null, so may w[0]) or 2, the gated pair.  v: the workspace.

@@ -1,0 +1,342 @@
+// The router's gradient: from those of the gate weights w[t,i] = gate(z[t])[idx[t,i]], z = x W_r^T + bias, to x, W_r and bias.
+//   softmax over all experts   dz_e = p_e (G_e - sum_i p_i g_i),  p = softmax(z), G_e = sum of g over the slots that chose e
+//   renormalised               dz_i = w_i (g_i - sum_j w_j g_j) for the chosen experts (no logits are needed)
+//   sigmoid, normalised        the same times 1 - sigmoid(z_i)
+//   dx = dz W_r,  dW_r = dz^T x,  dbias = sum_t dz
+// Launches: logits in pieces of d (where needed), dz of a token by a wavefront, dx and pieces of dW_r over the tokens, their sum.
+// dz enters the two products as two bf16 numbers (16 bits), so dx and dW_r are off by little more than their own rounding.
+#include "mma_tile.hpp"
+
+namespace moe {
+
+namespace {
+
+struct RouteArgs {
+    const uint16_t *x, *wr;
+    const float* bias;
+    const int32_t* idx;
+    const float *w, *g;
+    uint16_t* dx;
+    void* dwr;
+    float* dbias;
+    int f32, add;
+    float* part;       // [logit_pieces][T, Ep]
+    uint16_t* dz;      // [T, 2 Ep]: the larger halves of all experts, then the smaller ones
+    float* bias_part;  // [dz_blocks][Ep]
+    float* sums;       // [weight_pieces][E, d]
+    int T, d, E, k, Ep, gating;
+    int logit_pieces, weight_pieces, dz_blocks;
+};
+
+// Tile: BM tokens x BN experts, one piece of d.
+template <class S>
+__global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void route_logits_kernel(RouteArgs a) {
+    __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
+    const int cols = (a.E + S::BN - 1) / S::BN, m0 = (int)(blockIdx.x / cols) * S::BM, n0 = (int)(blockIdx.x % cols) * S::BN;
+    const int rows = a.T - m0 < S::BM ? a.T - m0 : S::BM, experts = a.E - n0 < S::BN ? a.E - n0 : S::BN;
+    const int all = a.d / S::BK, each = (all + a.logit_pieces - 1) / a.logit_pieces, s0 = blockIdx.y * each, s1 = s0 + each < all ? s0 + each : all;
+    const int k0 = s0 * S::BK, k = (s1 - s0) * S::BK;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    typename S::template LoadA<true> la;
+    typename S::template LoadB<true> lb;
+    la.init(a.d, wave, lane);
+    lb.init(a.d, wave, lane);
+    by_height<S>(rows, [&](auto height) {
+        constexpr int MB = decltype(height)::value;
+        Acc<S, MB> acc;
+        clear<S, MB>(acc);
+        multiply<S, MB, true, true>(acc, Stream<true, S::BK>::make(a.x + (size_t)m0 * a.d + k0, a.d, rows, k, k0),
+                                    Stream<true, S::BK>::make(a.wr + (size_t)n0 * a.d + k0, a.d, experts, k, k0), la, lb, s1 - s0, lds);
+        by_rows<S, S::BN / 8>(acc, lds, AheadNothing{}, [&](int r, int c, const float* row, Nothing) {
+            if (r >= rows || n0 + c * 8 >= a.Ep) return;
+            float* to = a.part + ((size_t)blockIdx.y * a.T + m0 + r) * a.Ep + n0 + c * 8;
+            *reinterpret_cast<f32x4*>(to) = *reinterpret_cast<const f32x4*>(row + c * 8);
+            *reinterpret_cast<f32x4*>(to + 4) = *reinterpret_cast<const f32x4*>(row + c * 8 + 4);
+        });
+    });
+}
+
+constexpr int kDzThreads = 256, kDzWaves = kDzThreads / kWave;
+
+__device__ __forceinline__ float wave_add(float v) {
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
+    return v;
+}
+__device__ __forceinline__ float wave_most(float v) {
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, kWave));
+    return v;
+}
+
+// dz of a token by a wavefront, Q experts per lane (lane, lane + 64, ...).  The workgroup's share of dbias is summed on the way.  A slot whose expert is outside
+// 0 .. E - 1 has no part in anything.
+template <int Q>
+__global__ __launch_bounds__(kDzThreads) void route_dz_kernel(RouteArgs a) {
+    __shared__ float bias_sum[kDzWaves][Q * kWave];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    float bias_acc[Q];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) bias_acc[q] = 0.0f;
+    for (int t = blockIdx.x * kDzWaves + wave; t < a.T; t += a.dz_blocks * kDzWaves) {
+        float z[Q], dz[Q];
+#pragma unroll
+        for (int q = 0; q < Q; ++q) z[q] = dz[q] = 0.0f;
+        if (a.gating != MOE_GATE_SOFTMAX_RENORM) {
+            for (int p = 0; p < a.logit_pieces; ++p) {
+#pragma unroll
+                for (int q = 0; q < Q; ++q) z[q] += a.part[((size_t)p * a.T + t) * a.Ep + q * kWave + lane];
+            }
+            if (a.bias) {
+#pragma unroll
+                for (int q = 0; q < Q; ++q)
+                    if (q * kWave + lane < a.E) z[q] += a.bias[q * kWave + lane];
+            }
+        }
+        const int32_t* idx = a.idx + (size_t)t * a.k;
+        const float *w = a.w + (size_t)t * a.k, *g = a.g + (size_t)t * a.k;
+        if (a.gating == MOE_GATE_SOFTMAX) {
+            float most = -INFINITY, sum = 0.0f, c = 0.0f, p[Q];
+#pragma unroll
+            for (int q = 0; q < Q; ++q)
+                if (q * kWave + lane < a.E) most = fmaxf(most, z[q]);
+            most = wave_most(most);
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                p[q] = q * kWave + lane < a.E ? expf(z[q] - most) : 0.0f;
+                sum += p[q];
+            }
+            sum = wave_add(sum);
+            for (int i = 0; i < a.k; ++i) {
+                const int e = idx[i] < a.E ? idx[i] : -1;
+#pragma unroll
+                for (int q = 0; q < Q; ++q)
+                    if (e == q * kWave + lane) dz[q] += g[i];
+            }
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                p[q] /= sum;
+                c = fmaf(p[q], dz[q], c);
+            }
+            c = wave_add(c);
+#pragma unroll
+            for (int q = 0; q < Q; ++q) dz[q] = q * kWave + lane < a.E ? p[q] * (dz[q] - c) : 0.0f;
+        } else {
+            float c = 0.0f;
+            for (int i = 0; i < a.k; ++i)
+                if ((uint32_t)idx[i] < (uint32_t)a.E) c = fmaf(w[i], g[i], c);
+            for (int i = 0; i < a.k; ++i) {
+                const int e = idx[i] < a.E ? idx[i] : -1;
+                const float v = w[i] * (g[i] - c);
+#pragma unroll
+                for (int q = 0; q < Q; ++q)
+                    if (e == q * kWave + lane) dz[q] += v;
+            }
+            if (a.gating == MOE_GATE_SIGMOID_NORM) {
+#pragma unroll
+                for (int q = 0; q < Q; ++q) dz[q] = dz[q] != 0.0f ? dz[q] / (1.0f + expf(z[q])) : 0.0f;
+            }
+        }
+        uint16_t* to = a.dz + (size_t)t * 2 * a.Ep;
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            const int e = q * kWave + lane;
+            bias_acc[q] += dz[q];
+            const uint16_t hi = float_to_bf16_bits(dz[q]);
+            to[e] = hi;
+            to[a.Ep + e] = float_to_bf16_bits(dz[q] - bf16_bits_to_float(hi));
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < Q; ++q) bias_sum[wave][q * kWave + lane] = bias_acc[q];
+    __syncthreads();
+    for (int e = threadIdx.x; e < Q * kWave; e += kDzThreads) {
+        float v = bias_sum[0][e];
+#pragma unroll
+        for (int i = 1; i < kDzWaves; ++i) v += bias_sum[i][e];
+        a.bias_part[(size_t)blockIdx.x * a.Ep + e] = v;
+    }
+}
+
+// dx = dz W_r: the larger halves over all experts, then the smaller ones.
+template <class S>
+__global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void route_dx_kernel(RouteArgs a) {
+    __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
+    const int cols = (a.d + S::BN - 1) / S::BN, m0 = (int)(blockIdx.x / cols) * S::BM, n0 = (int)(blockIdx.x % cols) * S::BN;
+    const int rows = a.T - m0 < S::BM ? a.T - m0 : S::BM, ld = 2 * a.Ep;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    typename S::template LoadA<true> la;
+    typename S::template LoadB<false> lb;
+    la.init(ld, wave, lane);
+    lb.init(a.d, wave, lane);
+    by_height<S>(rows, [&](auto height) {
+        constexpr int MB = decltype(height)::value;
+        Acc<S, MB> acc;
+        clear<S, MB>(acc);
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h)
+            multiply<S, MB, true, false>(acc, Stream<true, S::BK>::make(a.dz + (size_t)m0 * ld + h * a.Ep, ld, rows, a.Ep, h * a.Ep),
+                                         Stream<false, S::BK>::make(a.wr, a.d, n0, a.E), la, lb, a.Ep / S::BK, lds);
+        by_rows_bf16<S, MB>(acc, lds, [&](int r, int c, u32x4_t v) {
+            if (r < rows && n0 + c * 8 < a.d) *reinterpret_cast<u32x4_t*>(a.dx + (size_t)(m0 + r) * a.d + n0 + c * 8) = v;
+        });
+    });
+}
+
+// dW_r = dz^T x over one piece of the tokens.
+template <class S>
+__global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void route_dw_kernel(RouteArgs a) {
+    __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
+    const int cols = (a.d + S::BN - 1) / S::BN, m0 = (int)(blockIdx.x / cols) * S::BM, n0 = (int)(blockIdx.x % cols) * S::BN;
+    const int all = (a.T + S::BK - 1) / S::BK, each = (all + a.weight_pieces - 1) / a.weight_pieces, s0 = blockIdx.y * each, s1 = s0 + each < all ? s0 + each : all;
+    const int t0 = s0 * S::BK, tokens = a.T - t0 < (s1 - s0) * S::BK ? a.T - t0 : (s1 - s0) * S::BK, ld = 2 * a.Ep;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    typename S::template LoadA<false> la;
+    typename S::template LoadB<false> lb;
+    la.init(ld, wave, lane);
+    lb.init(a.d, wave, lane);
+    by_height<S>(a.E - m0, [&](auto height) {
+        constexpr int MB = decltype(height)::value;
+        Acc<S, MB> acc;
+        clear<S, MB>(acc);
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h)
+            multiply<S, MB, false, false>(acc, Stream<false, S::BK>::make(a.dz + (size_t)t0 * ld, ld, m0 + h * a.Ep, tokens),
+                                          Stream<false, S::BK>::make(a.x + (size_t)t0 * a.d, a.d, n0, tokens), la, lb, s1 - s0, lds);
+        by_rows<S, S::BN / 8>(acc, lds, AheadNothing{}, [&](int r, int c, const float* row, Nothing) {
+            if (m0 + r >= a.E || n0 + c * 8 >= a.d) return;
+            float* to = a.sums + ((size_t)blockIdx.y * a.E + m0 + r) * a.d + n0 + c * 8;
+            *reinterpret_cast<f32x4*>(to) = *reinterpret_cast<const f32x4*>(row + c * 8);
+            *reinterpret_cast<f32x4*>(to + 4) = *reinterpret_cast<const f32x4*>(row + c * 8 + 4);
+        });
+    });
+}
+
+// The pieces of dW_r, eight elements per thread, in their order; the last workgroup adds up dbias.
+__global__ __launch_bounds__(256) void route_join_kernel(RouteArgs a) {
+    if (blockIdx.x == gridDim.x - 1) {
+        if (a.dbias && (int)threadIdx.x < a.E) {
+            float v = a.add ? a.dbias[threadIdx.x] : 0.0f;
+#pragma unroll 8
+            for (int b = 0; b < a.dz_blocks; ++b) v += a.bias_part[(size_t)b * a.Ep + threadIdx.x];
+            a.dbias[threadIdx.x] = v;
+        }
+        return;
+    }
+    const size_t at = ((size_t)blockIdx.x * 256 + threadIdx.x) * 8, n = (size_t)a.E * a.d;
+    if (at >= n) return;
+    float sum[8], v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+    for (int p = 0; p < a.weight_pieces; ++p) {
+        load8(a.sums + p * n + at, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += v[i];
+    }
+    if (a.f32) {
+        float* to = reinterpret_cast<float*>(a.dwr) + at;
+        if (a.add) {
+            load8(to, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += v[i];
+        }
+        *reinterpret_cast<f32x4*>(to) = f32x4{sum[0], sum[1], sum[2], sum[3]};
+        *reinterpret_cast<f32x4*>(to + 4) = f32x4{sum[4], sum[5], sum[6], sum[7]};
+    } else {
+        u32x4_t* to = reinterpret_cast<u32x4_t*>(reinterpret_cast<uint16_t*>(a.dwr) + at);
+        if (a.add) {
+            unpack8(*to, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += v[i];
+        }
+        *to = pack8(sum);
+    }
+}
+
+int padded(const moe_config& c) { return (c.E + 63) / 64 * 64; }
+bool few_experts(const moe_config& c) { return c.E <= Flat::BM; }
+
+template <class S>
+int logit_pieces_of(const moe_config& c) {
+    const long long tiles = (long long)((c.T + S::BM - 1) / S::BM) * ((c.E + S::BN - 1) / S::BN), most = c.d / S::BK / 4;
+    long long n = tiles > 0 ? 256 * S::PER / tiles : 1;
+    if (n > 16) n = 16;
+    if (n > most) n = most;
+    return n < 1 ? 1 : (int)n;
+}
+int logit_pieces(const moe_config& c) {
+    if (c.gating == MOE_GATE_SOFTMAX_RENORM) return 0;
+    return few_experts(c) ? logit_pieces_of<Flat>(c) : logit_pieces_of<Small>(c);
+}
+template <class S>
+int weight_pieces_of(const moe_config& c) {
+    const long long tiles = (long long)((c.E + S::BM - 1) / S::BM) * ((c.d + S::BN - 1) / S::BN), most = (c.T + 4 * S::BK - 1) / (4 * S::BK);
+    long long n = 256 * S::PER / tiles;
+    if (n > 16) n = 16;
+    if (n > most) n = most;
+    return n < 1 ? 1 : (int)n;
+}
+int weight_pieces(const moe_config& c) { return few_experts(c) ? weight_pieces_of<Flat>(c) : weight_pieces_of<Small>(c); }
+int dz_blocks(const moe_config& c) {
+    const int n = (c.T + kDzWaves - 1) / kDzWaves;
+    return n < 256 ? n : 256;
+}
+
+struct RouteSpace {
+    size_t part, dz, bias, sums, total;
+};
+RouteSpace space(const moe_config& c) {
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t o = at; at += (bytes + 255) / 256 * 256; return o; };
+    const size_t T = c.T, Ep = padded(c);
+    RouteSpace s;
+    s.part = take((size_t)logit_pieces(c) * T * Ep * sizeof(float));
+    s.dz = take(T * 2 * Ep * sizeof(uint16_t));
+    s.bias = take((size_t)dz_blocks(c) * Ep * sizeof(float));
+    s.sums = take(c.T > 0 ? (size_t)weight_pieces(c) * c.E * c.d * sizeof(float) : 0);
+    s.total = at;
+    return s;
+}
+
+template <class S>
+unsigned tiles_of(long long M, long long N) { return (unsigned)(((M + S::BM - 1) / S::BM) * ((N + S::BN - 1) / S::BN)); }
+
+}  // namespace
+
+size_t route_backward_workspace_bytes(const moe_config& c) { return space(c).total; }
+
+hipError_t launch_route_backward(const moe_config& c, const RouteGrad& p, hipStream_t s) {
+    const RouteSpace at = space(c);
+    RouteArgs a{p.x, p.wr, p.bias, p.idx, p.w, p.g, p.dx, p.dwr, p.dbias, p.f32, p.add, (float*)(p.workspace + at.part), (uint16_t*)(p.workspace + at.dz),
+                (float*)(p.workspace + at.bias), (float*)(p.workspace + at.sums), c.T, c.d, c.E, c.k, padded(c), c.gating,
+                logit_pieces(c), c.T > 0 ? weight_pieces(c) : 0, dz_blocks(c)};
+    const bool weights = (p.dwr || p.dbias) && !(c.T == 0 && p.add), rows = p.dx && c.T > 0;
+    if (!weights && !rows) return hipSuccess;
+    if (c.T > 0) {
+        if (a.logit_pieces > 0) {
+            if (few_experts(c)) hipLaunchKernelGGL(route_logits_kernel<Flat>, dim3(tiles_of<Flat>(c.T, c.E), a.logit_pieces), dim3(Flat::THREADS), 0, s, a);
+            else hipLaunchKernelGGL(route_logits_kernel<Small>, dim3(tiles_of<Small>(c.T, c.E), a.logit_pieces), dim3(Small::THREADS), 0, s, a);
+        }
+        switch (a.Ep / kWave) {
+            case 1: hipLaunchKernelGGL(route_dz_kernel<1>, dim3(a.dz_blocks), dim3(kDzThreads), 0, s, a); break;
+            case 2: hipLaunchKernelGGL(route_dz_kernel<2>, dim3(a.dz_blocks), dim3(kDzThreads), 0, s, a); break;
+            case 3: hipLaunchKernelGGL(route_dz_kernel<3>, dim3(a.dz_blocks), dim3(kDzThreads), 0, s, a); break;
+            default: hipLaunchKernelGGL(route_dz_kernel<4>, dim3(a.dz_blocks), dim3(kDzThreads), 0, s, a);
+        }
+        if (rows) {
+            if (c.T <= Flat::BM) hipLaunchKernelGGL(route_dx_kernel<Flat>, dim3(tiles_of<Flat>(c.T, c.d)), dim3(Flat::THREADS), 0, s, a);
+            else hipLaunchKernelGGL(route_dx_kernel<Small>, dim3(tiles_of<Small>(c.T, c.d)), dim3(Small::THREADS), 0, s, a);
+        }
+        if (p.dwr) {
+            if (few_experts(c)) hipLaunchKernelGGL(route_dw_kernel<Flat>, dim3(tiles_of<Flat>(c.E, c.d), a.weight_pieces), dim3(Flat::THREADS), 0, s, a);
+            else hipLaunchKernelGGL(route_dw_kernel<Small>, dim3(tiles_of<Small>(c.E, c.d), a.weight_pieces), dim3(Small::THREADS), 0, s, a);
+        }
+    }
+    if (weights) {
+        const size_t groups = p.dwr ? ((size_t)c.E * c.d / 8 + 255) / 256 : 0;
+        hipLaunchKernelGGL(route_join_kernel, dim3((unsigned)groups + 1), dim3(256), 0, s, a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace moe
