@@ -3,8 +3,9 @@
 //   renormalised               dz_i = w_i (g_i - sum_j w_j g_j) for the chosen experts (no logits are needed)
 //   sigmoid, normalised        the same times 1 - sigmoid(z_i)
 //   dx = dz W_r,  dW_r = dz^T x,  dbias = sum_t dz
-// Launches: logits in pieces of d (where needed), dz of a token by a wavefront, dx and pieces of dW_r over the tokens, their sum.
-// dz enters the two products as two bf16 numbers (16 bits), so dx and dW_r are off by little more than their own rounding.
+// Launches: logits in pieces of d (where needed), dz of a token by a wavefront, dx and dW_r (its sum over the tokens in pieces) side by side, the pieces' sum.
+// dz enters the products as two bf16 numbers (16 bits) where the result is bf16, as three (all 24 bits) for dW_r in fp32: results are then off by little more than
+// their own rounding.
 #include "mma_tile.hpp"
 
 namespace moe {
@@ -21,10 +22,10 @@ struct RouteArgs {
     float* dbias;
     int f32, add;
     float* part;       // [logit_pieces][T, Ep]
-    uint16_t* dz;      // [T, 2 Ep]: the larger halves of all experts, then the smaller ones
+    uint16_t* dz;      // [T, parts Ep]: dz rounded, of all experts; what that leaves, rounded; and once more
     float* bias_part;  // [dz_blocks][Ep]
     float* sums;       // [weight_pieces][E, d]
-    int T, d, E, k, Ep, gating;
+    int T, d, E, k, Ep, gating, parts;
     int logit_pieces, weight_pieces, dz_blocks;
 };
 
@@ -32,9 +33,12 @@ struct RouteArgs {
 template <class S>
 __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void route_logits_kernel(RouteArgs a) {
     __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
-    const int cols = (a.E + S::BN - 1) / S::BN, m0 = (int)(blockIdx.x / cols) * S::BM, n0 = (int)(blockIdx.x % cols) * S::BN;
+    const int cols = (a.E + S::BN - 1) / S::BN, blocks = (a.T + S::BM - 1) / S::BM;
+    const int t = xcd_tile(blockIdx.x, a.logit_pieces * blocks * cols);        // [piece][block of tokens][experts]: an XCD's tiles share W_r's piece and x's rows
+    if (t < 0) return;
+    const int piece = t / (blocks * cols), m0 = t / cols % blocks * S::BM, n0 = t % cols * S::BN;
     const int rows = a.T - m0 < S::BM ? a.T - m0 : S::BM, experts = a.E - n0 < S::BN ? a.E - n0 : S::BN;
-    const int all = a.d / S::BK, each = (all + a.logit_pieces - 1) / a.logit_pieces, s0 = blockIdx.y * each, s1 = s0 + each < all ? s0 + each : all;
+    const int all = a.d / S::BK, each = (all + a.logit_pieces - 1) / a.logit_pieces, s0 = piece * each, s1 = s0 + each < all ? s0 + each : all;
     const int k0 = s0 * S::BK, k = (s1 - s0) * S::BK;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     typename S::template LoadA<true> la;
@@ -49,7 +53,7 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void route_logits_kernel
                                     Stream<true, S::BK>::make(a.wr + (size_t)n0 * a.d + k0, a.d, experts, k, k0), la, lb, s1 - s0, lds);
         by_rows<S, S::BN / 8>(acc, lds, AheadNothing{}, [&](int r, int c, const float* row, Nothing) {
             if (r >= rows || n0 + c * 8 >= a.Ep) return;
-            float* to = a.part + ((size_t)blockIdx.y * a.T + m0 + r) * a.Ep + n0 + c * 8;
+            float* to = a.part + ((size_t)piece * a.T + m0 + r) * a.Ep + n0 + c * 8;
             *reinterpret_cast<f32x4*>(to) = *reinterpret_cast<const f32x4*>(row + c * 8);
             *reinterpret_cast<f32x4*>(to + 4) = *reinterpret_cast<const f32x4*>(row + c * 8 + 4);
         });
@@ -137,14 +141,17 @@ __global__ __launch_bounds__(kDzThreads) void route_dz_kernel(RouteArgs a) {
                 for (int q = 0; q < Q; ++q) dz[q] = dz[q] != 0.0f ? dz[q] / (1.0f + expf(z[q])) : 0.0f;
             }
         }
-        uint16_t* to = a.dz + (size_t)t * 2 * a.Ep;
+        uint16_t* to = a.dz + (size_t)t * a.parts * a.Ep;
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
             const int e = q * kWave + lane;
             bias_acc[q] += dz[q];
-            const uint16_t hi = float_to_bf16_bits(dz[q]);
-            to[e] = hi;
-            to[a.Ep + e] = float_to_bf16_bits(dz[q] - bf16_bits_to_float(hi));
+            float left = dz[q];
+            for (int h = 0; h < a.parts; ++h) {
+                const uint16_t v = float_to_bf16_bits(left);
+                to[h * a.Ep + e] = v;
+                left -= bf16_bits_to_float(v);
+            }
         }
     }
 #pragma unroll
@@ -158,13 +165,11 @@ __global__ __launch_bounds__(kDzThreads) void route_dz_kernel(RouteArgs a) {
     }
 }
 
-// dx = dz W_r: the larger halves over all experts, then the smaller ones.
+// Tile of dx = dz W_r: dz's first part over all experts, then its second.
 template <class S>
-__global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void route_dx_kernel(RouteArgs a) {
-    __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
-    const int cols = (a.d + S::BN - 1) / S::BN, m0 = (int)(blockIdx.x / cols) * S::BM, n0 = (int)(blockIdx.x % cols) * S::BN;
-    const int rows = a.T - m0 < S::BM ? a.T - m0 : S::BM, ld = 2 * a.Ep;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+__device__ __forceinline__ void dx_tile(const RouteArgs& a, int m0, int n0, char* lds) {
+    const int rows = a.T - m0 < S::BM ? a.T - m0 : S::BM, ld = a.parts * a.Ep;
+    const int wave = __builtin_amdgcn_readfirstlane(body_thread() / kWave), lane = body_thread() % kWave;
     typename S::template LoadA<true> la;
     typename S::template LoadB<false> lb;
     la.init(ld, wave, lane);
@@ -183,14 +188,12 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void route_dx_kernel(Rou
     });
 }
 
-// dW_r = dz^T x over one piece of the tokens.
+// Tile of dW_r = dz^T x over one piece of the tokens, dz's parts one after the other.
 template <class S>
-__global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void route_dw_kernel(RouteArgs a) {
-    __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
-    const int cols = (a.d + S::BN - 1) / S::BN, m0 = (int)(blockIdx.x / cols) * S::BM, n0 = (int)(blockIdx.x % cols) * S::BN;
-    const int all = (a.T + S::BK - 1) / S::BK, each = (all + a.weight_pieces - 1) / a.weight_pieces, s0 = blockIdx.y * each, s1 = s0 + each < all ? s0 + each : all;
-    const int t0 = s0 * S::BK, tokens = a.T - t0 < (s1 - s0) * S::BK ? a.T - t0 : (s1 - s0) * S::BK, ld = 2 * a.Ep;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+__device__ __forceinline__ void dw_tile(const RouteArgs& a, int piece, int m0, int n0, char* lds) {
+    const int all = (a.T + S::BK - 1) / S::BK, each = (all + a.weight_pieces - 1) / a.weight_pieces, s0 = piece * each, s1 = s0 + each < all ? s0 + each : all;
+    const int t0 = s0 * S::BK, tokens = a.T - t0 < (s1 - s0) * S::BK ? a.T - t0 : (s1 - s0) * S::BK, ld = a.parts * a.Ep;
+    const int wave = __builtin_amdgcn_readfirstlane(body_thread() / kWave), lane = body_thread() % kWave;
     typename S::template LoadA<false> la;
     typename S::template LoadB<false> lb;
     la.init(ld, wave, lane);
@@ -200,34 +203,64 @@ __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void route_dw_kernel(Rou
         Acc<S, MB> acc;
         clear<S, MB>(acc);
 #pragma unroll 1
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < a.parts; ++h)
             multiply<S, MB, false, false>(acc, Stream<false, S::BK>::make(a.dz + (size_t)t0 * ld, ld, m0 + h * a.Ep, tokens),
                                           Stream<false, S::BK>::make(a.x + (size_t)t0 * a.d, a.d, n0, tokens), la, lb, s1 - s0, lds);
         by_rows<S, S::BN / 8>(acc, lds, AheadNothing{}, [&](int r, int c, const float* row, Nothing) {
             if (m0 + r >= a.E || n0 + c * 8 >= a.d) return;
-            float* to = a.sums + ((size_t)blockIdx.y * a.E + m0 + r) * a.d + n0 + c * 8;
+            float* to = a.sums + ((size_t)piece * a.E + m0 + r) * a.d + n0 + c * 8;
             *reinterpret_cast<f32x4*>(to) = *reinterpret_cast<const f32x4*>(row + c * 8);
             *reinterpret_cast<f32x4*>(to + 4) = *reinterpret_cast<const f32x4*>(row + c * 8 + 4);
         });
     });
 }
 
-// The pieces of dW_r, eight elements per thread, in their order; the last workgroup adds up dbias.
+// Both products in one launch, the longer tiles (dW_r's) first.
+template <class S>
+__global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void route_products_kernel(RouteArgs a) {
+    __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
+    const int cols = (a.d + S::BN - 1) / S::BN, heads = (a.E + S::BM - 1) / S::BM, blocks = (a.T + S::BM - 1) / S::BM;
+    const int weights = a.dwr ? a.weight_pieces * cols * heads : 0, ids = (weights + 7) / 8 * 8;
+    if ((int)blockIdx.x < ids) {
+        const int t = xcd_tile(blockIdx.x, weights);
+        if (t >= 0) dw_tile<S>(a, t / (cols * heads), t % heads * S::BM, t / heads % cols * S::BN, lds);
+        return;
+    }
+    const int t = xcd_tile(blockIdx.x - ids, blocks * cols);
+    if (t < 0) return;
+    int m, n;
+    patch(t, blocks, cols, m, n);
+    dx_tile<S>(a, m * S::BM, n * S::BN, lds);
+}
+
+// The pieces of dW_r, eight elements per thread, in their order; the first workgroups add up dbias, sixteen experts each.
+constexpr int kBiasExperts = 16;
 __global__ __launch_bounds__(256) void route_join_kernel(RouteArgs a) {
-    if (blockIdx.x == gridDim.x - 1) {
-        if (a.dbias && (int)threadIdx.x < a.E) {
-            float v = a.add ? a.dbias[threadIdx.x] : 0.0f;
+    const int bias_groups = a.dbias ? (a.E + kBiasExperts - 1) / kBiasExperts : 0;
+    if ((int)blockIdx.x < bias_groups) {
+        constexpr int SEGS = 256 / kBiasExperts;
+        __shared__ float part[SEGS][kBiasExperts];
+        const int e = blockIdx.x * kBiasExperts + threadIdx.x % kBiasExperts, seg = threadIdx.x / kBiasExperts;
+        float v = 0.0f;
+        if (e < a.E) {
 #pragma unroll 8
-            for (int b = 0; b < a.dz_blocks; ++b) v += a.bias_part[(size_t)b * a.Ep + threadIdx.x];
-            a.dbias[threadIdx.x] = v;
+            for (int b = seg; b < a.dz_blocks; b += SEGS) v += a.bias_part[(size_t)b * a.Ep + e];
+        }
+        part[seg][threadIdx.x % kBiasExperts] = v;
+        __syncthreads();
+        if (seg == 0 && e < a.E) {
+            float sum = a.add ? a.dbias[e] : 0.0f;
+            for (int i = 0; i < SEGS; ++i) sum += part[i][threadIdx.x];
+            a.dbias[e] = sum;
         }
         return;
     }
-    const size_t at = ((size_t)blockIdx.x * 256 + threadIdx.x) * 8, n = (size_t)a.E * a.d;
+    const size_t at = ((size_t)(blockIdx.x - bias_groups) * 256 + threadIdx.x) * 8, n = (size_t)a.E * a.d;
     if (at >= n) return;
     float sum[8], v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+#pragma unroll 4
     for (int p = 0; p < a.weight_pieces; ++p) {
         load8(a.sums + p * n + at, v);
 #pragma unroll
@@ -268,18 +301,23 @@ int logit_pieces(const moe_config& c) {
     if (c.gating == MOE_GATE_SOFTMAX_RENORM) return 0;
     return few_experts(c) ? logit_pieces_of<Flat>(c) : logit_pieces_of<Small>(c);
 }
+bool few_tokens(const moe_config& c) { return c.T <= Flat::BM; }
+constexpr int kMostParts = 3;
+// Pieces of the tokens that dW_r is summed over: as many as make its tiles about as long as a place's share of the whole launch.
 template <class S>
 int weight_pieces_of(const moe_config& c) {
-    const long long tiles = (long long)((c.E + S::BM - 1) / S::BM) * ((c.d + S::BN - 1) / S::BN), most = (c.T + 4 * S::BK - 1) / (4 * S::BK);
-    long long n = 256 * S::PER / tiles;
-    if (n > 16) n = 16;
+    const long long cols = (c.d + S::BN - 1) / S::BN, weights = (c.E + S::BM - 1) / S::BM * cols, rows = (c.T + S::BM - 1) / S::BM * cols;
+    const long long steps = (long long)kMostParts * ((c.T + S::BK - 1) / S::BK), share = (weights * steps + rows * (2 * padded(c) / S::BK)) / (256 * S::PER);
+    const long long most = (c.T + 4 * S::BK - 1) / (4 * S::BK);
+    long long n = (steps + share) / (share + 1);
+    if (n > 8) n = 8;
     if (n > most) n = most;
     return n < 1 ? 1 : (int)n;
 }
-int weight_pieces(const moe_config& c) { return few_experts(c) ? weight_pieces_of<Flat>(c) : weight_pieces_of<Small>(c); }
+int weight_pieces(const moe_config& c) { return few_tokens(c) ? weight_pieces_of<Flat>(c) : weight_pieces_of<Pair>(c); }
 int dz_blocks(const moe_config& c) {
     const int n = (c.T + kDzWaves - 1) / kDzWaves;
-    return n < 256 ? n : 256;
+    return n < 1024 ? n : 1024;
 }
 
 struct RouteSpace {
@@ -291,7 +329,7 @@ RouteSpace space(const moe_config& c) {
     const size_t T = c.T, Ep = padded(c);
     RouteSpace s;
     s.part = take((size_t)logit_pieces(c) * T * Ep * sizeof(float));
-    s.dz = take(T * 2 * Ep * sizeof(uint16_t));
+    s.dz = take(T * kMostParts * Ep * sizeof(uint16_t));
     s.bias = take((size_t)dz_blocks(c) * Ep * sizeof(float));
     s.sums = take(c.T > 0 ? (size_t)weight_pieces(c) * c.E * c.d * sizeof(float) : 0);
     s.total = at;
@@ -299,7 +337,15 @@ RouteSpace space(const moe_config& c) {
 }
 
 template <class S>
-unsigned tiles_of(long long M, long long N) { return (unsigned)(((M + S::BM - 1) / S::BM) * ((N + S::BN - 1) / S::BN)); }
+void go_logits(const RouteArgs& a, hipStream_t s) {
+    const long long tiles = (long long)a.logit_pieces * ((a.T + S::BM - 1) / S::BM) * ((a.E + S::BN - 1) / S::BN);
+    hipLaunchKernelGGL(route_logits_kernel<S>, dim3(xcd_grid(tiles)), dim3(S::THREADS), 0, s, a);
+}
+template <class S>
+void go_products(const RouteArgs& a, hipStream_t s) {
+    const long long cols = (a.d + S::BN - 1) / S::BN, weights = a.dwr ? a.weight_pieces * cols * ((a.E + S::BM - 1) / S::BM) : 0, rows = a.dx ? cols * ((a.T + S::BM - 1) / S::BM) : 0;
+    hipLaunchKernelGGL(route_products_kernel<S>, dim3(xcd_grid(weights) + xcd_grid(rows)), dim3(S::THREADS), 0, s, a);
+}
 
 }  // namespace
 
@@ -308,14 +354,14 @@ size_t route_backward_workspace_bytes(const moe_config& c) { return space(c).tot
 hipError_t launch_route_backward(const moe_config& c, const RouteGrad& p, hipStream_t s) {
     const RouteSpace at = space(c);
     RouteArgs a{p.x, p.wr, p.bias, p.idx, p.w, p.g, p.dx, p.dwr, p.dbias, p.f32, p.add, (float*)(p.workspace + at.part), (uint16_t*)(p.workspace + at.dz),
-                (float*)(p.workspace + at.bias), (float*)(p.workspace + at.sums), c.T, c.d, c.E, c.k, padded(c), c.gating,
+                (float*)(p.workspace + at.bias), (float*)(p.workspace + at.sums), c.T, c.d, c.E, c.k, padded(c), c.gating, p.dwr && p.f32 ? 3 : 2,
                 logit_pieces(c), c.T > 0 ? weight_pieces(c) : 0, dz_blocks(c)};
     const bool weights = (p.dwr || p.dbias) && !(c.T == 0 && p.add), rows = p.dx && c.T > 0;
     if (!weights && !rows) return hipSuccess;
     if (c.T > 0) {
         if (a.logit_pieces > 0) {
-            if (few_experts(c)) hipLaunchKernelGGL(route_logits_kernel<Flat>, dim3(tiles_of<Flat>(c.T, c.E), a.logit_pieces), dim3(Flat::THREADS), 0, s, a);
-            else hipLaunchKernelGGL(route_logits_kernel<Small>, dim3(tiles_of<Small>(c.T, c.E), a.logit_pieces), dim3(Small::THREADS), 0, s, a);
+            if (few_experts(c)) go_logits<Flat>(a, s);
+            else go_logits<Small>(a, s);
         }
         switch (a.Ep / kWave) {
             case 1: hipLaunchKernelGGL(route_dz_kernel<1>, dim3(a.dz_blocks), dim3(kDzThreads), 0, s, a); break;
@@ -323,18 +369,14 @@ hipError_t launch_route_backward(const moe_config& c, const RouteGrad& p, hipStr
             case 3: hipLaunchKernelGGL(route_dz_kernel<3>, dim3(a.dz_blocks), dim3(kDzThreads), 0, s, a); break;
             default: hipLaunchKernelGGL(route_dz_kernel<4>, dim3(a.dz_blocks), dim3(kDzThreads), 0, s, a);
         }
-        if (rows) {
-            if (c.T <= Flat::BM) hipLaunchKernelGGL(route_dx_kernel<Flat>, dim3(tiles_of<Flat>(c.T, c.d)), dim3(Flat::THREADS), 0, s, a);
-            else hipLaunchKernelGGL(route_dx_kernel<Small>, dim3(tiles_of<Small>(c.T, c.d)), dim3(Small::THREADS), 0, s, a);
-        }
-        if (p.dwr) {
-            if (few_experts(c)) hipLaunchKernelGGL(route_dw_kernel<Flat>, dim3(tiles_of<Flat>(c.E, c.d), a.weight_pieces), dim3(Flat::THREADS), 0, s, a);
-            else hipLaunchKernelGGL(route_dw_kernel<Small>, dim3(tiles_of<Small>(c.E, c.d), a.weight_pieces), dim3(Small::THREADS), 0, s, a);
+        if (rows || p.dwr) {
+            if (few_tokens(c)) go_products<Flat>(a, s);
+            else go_products<Pair>(a, s);
         }
     }
     if (weights) {
-        const size_t groups = p.dwr ? ((size_t)c.E * c.d / 8 + 255) / 256 : 0;
-        hipLaunchKernelGGL(route_join_kernel, dim3((unsigned)groups + 1), dim3(256), 0, s, a);
+        const size_t groups = (p.dwr ? ((size_t)c.E * c.d / 8 + 255) / 256 : 0) + (p.dbias ? (c.E + kBiasExperts - 1) / kBiasExperts : 0);
+        hipLaunchKernelGGL(route_join_kernel, dim3((unsigned)groups), dim3(256), 0, s, a);
     }
     return hipGetLastError();
 }
