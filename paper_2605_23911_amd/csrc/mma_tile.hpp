@@ -99,6 +99,25 @@ struct Stream {
     }
 };
 
+// A stream every step of which is taken `times` times, `jump` bytes further along the rows each time: a product with several parts of an operand, during which the
+// other operand's panel stays in the caches.
+template <class From>
+struct Repeat {
+    From from;
+    uint32_t jump;
+    int times, at;
+    Panel panel;
+    __device__ static __forceinline__ Repeat make(From s, int times, uint32_t jump) { return Repeat{s, jump, times, 0, {0, 0}}; }
+    __device__ __forceinline__ Panel next() {
+        if (at == 0) panel = from.next();
+        Panel p = panel;
+        p.base += (uint64_t)jump * at;
+        p.range = panel.range ? panel.range - jump * at : 0;       // the range ends with the rows
+        at = at + 1 == times ? 0 : at + 1;
+        return p;
+    }
+};
+
 // Permutation of a row's chunks (k contiguous) or pieces, by the row's number in the panel.
 template <int MN, bool KC, int BK>
 __device__ __forceinline__ int swizzle(int r) {
@@ -226,14 +245,15 @@ __device__ __forceinline__ void by_height(int rows, F&& body) {
     body(integral_constant<int, 1>{});
 }
 
-// acc += the tile's product over `steps` steps.  a, b: the operands' streams, loaders with the offsets set.
+// acc += the tile's product over `steps` steps.  la, lb: loaders with the offsets set.
 // Everything is put in its place by hand: a slot (16 of k) is MB x NB multiplications, and between them go the reads of the next slot's fragments,
 // one or two after each, and the next step's loads, one after each from the last slot on.  In a burst the loads of all wavefronts
 // queue up for longer than a slot takes, and the multiplications behind them wait.  A step's barrier stands in front of its last slot, whose
 // multiplications cover the first reads of the next step.
 // Ends with every wavefront past its last LDS read and nothing on its way into LDS.
-template <class S, int MB, bool AKC, bool BKC>
-__device__ __forceinline__ void multiply(f32x16 (&acc)[S::NB][MB], Stream<AKC, S::BK> a, Stream<BKC, S::BK> b, const typename S::template LoadA<AKC>& la,
+// a, b: the operands' streams (Stream, or Repeat of one).
+template <class S, int MB, bool AKC, bool BKC, class StreamA, class StreamB>
+__device__ __forceinline__ void multiply(f32x16 (&acc)[S::NB][MB], StreamA a, StreamB b, const typename S::template LoadA<AKC>& la,
                                          const typename S::template LoadB<BKC>& lb, int steps, char* lds) {
     constexpr int SLOTS = S::BK / 16, NA = S::template LoadA<AKC>::N, LOADS = NA + S::template LoadB<BKC>::N;     // loads per step and wavefront
     constexpr int READS = MB + S::NB, MFMAS = MB * S::NB, PER = (READS + MFMAS - 1) / MFMAS;

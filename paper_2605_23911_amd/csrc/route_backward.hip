@@ -73,91 +73,133 @@ __device__ __forceinline__ float wave_most(float v) {
     return v;
 }
 
-// dz of a token by a wavefront, Q experts per lane (lane, lane + 64, ...).  The workgroup's share of dbias is summed on the way.  A slot whose expert is outside
-// 0 .. E - 1 has no part in anything.
+// Slots' experts and gradients, 64 at a time: a lane each, handed to the others through a scalar register.  f(expert, -1 if it is outside 0 .. E - 1; w; g).
+template <class F>
+__device__ __forceinline__ void for_slots(const RouteArgs& a, size_t t, F&& f) {
+    const int lane = threadIdx.x % kWave;
+    for (int i0 = 0; i0 < a.k; i0 += kWave) {
+        const size_t at = t * a.k + i0 + lane;
+        const bool mine = i0 + lane < a.k;
+        const int32_t id = mine ? a.idx[at] : -1;
+        const float w = mine ? a.w[at] : 0.0f, g = mine ? a.g[at] : 0.0f;
+        const int e = (uint32_t)id < (uint32_t)a.E ? id : -1, n = a.k - i0 < kWave ? a.k - i0 : kWave;
+        for (int i = 0; i < n; ++i)
+            f(__builtin_amdgcn_readlane(e, i), __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), i)), __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g), i)));
+    }
+}
+
+// Q numbers of a lane in one access.
+template <int Q>
+struct Lot;
+template <>
+struct Lot<1> { typedef float f; typedef uint16_t h; };
+template <>
+struct Lot<2> { typedef float f __attribute__((ext_vector_type(2))); typedef uint16_t h __attribute__((ext_vector_type(2))); };
+template <>
+struct Lot<4> { typedef float f __attribute__((ext_vector_type(4))); typedef uint16_t h __attribute__((ext_vector_type(4))); };
+template <class V>
+__device__ __forceinline__ auto part_of(const V& v, int q) {
+    if constexpr (sizeof(V) <= 4 && !std::is_same<V, Lot<2>::h>::value) return v;
+    else return v[q];
+}
+
+// dz of a token by a wavefront, experts Q lane .. Q lane + Q - 1 in a lane.  The workgroup's share of dbias is summed on the way.  A slot whose expert is outside
+// 0 .. E - 1 has no part in anything.  Bound by latency: one load of the pieces of the logits, the exchanges between lanes, one store.
 template <int Q>
 __global__ __launch_bounds__(kDzThreads) void route_dz_kernel(RouteArgs a) {
+    typedef typename Lot<Q>::f Floats;
+    typedef typename Lot<Q>::h Halves;
     __shared__ float bias_sum[kDzWaves][Q * kWave];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-    float bias_acc[Q];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, e0 = lane * Q;
+    const bool held = e0 < a.Ep;          // whole lots: Ep is a multiple of 32
+    float bias_acc[Q], bias[Q];
+    bool in[Q];                           // the lane's q-th expert exists
 #pragma unroll
-    for (int q = 0; q < Q; ++q) bias_acc[q] = 0.0f;
+    for (int q = 0; q < Q; ++q) {
+        in[q] = e0 + q < a.E;
+        bias_acc[q] = 0.0f;
+        bias[q] = a.bias && in[q] ? a.bias[e0 + q] : 0.0f;
+    }
     for (int t = blockIdx.x * kDzWaves + wave; t < a.T; t += a.dz_blocks * kDzWaves) {
         float z[Q], dz[Q];
 #pragma unroll
         for (int q = 0; q < Q; ++q) z[q] = dz[q] = 0.0f;
         if (a.gating != MOE_GATE_SOFTMAX_RENORM) {
-            for (int p = 0; p < a.logit_pieces; ++p) {
+            const char* from = reinterpret_cast<const char*>(a.part + (size_t)t * a.Ep + (held ? e0 : 0));
+            const size_t each = (size_t)a.T * a.Ep * sizeof(float);
+            constexpr int AHEAD = 8;
+            for (int p0 = 0; p0 < a.logit_pieces; p0 += AHEAD) {
+                Floats v[AHEAD];
 #pragma unroll
-                for (int q = 0; q < Q; ++q) z[q] += a.part[((size_t)p * a.T + t) * a.Ep + q * kWave + lane];
-            }
-            if (a.bias) {
+                for (int p = 0; p < AHEAD; ++p) v[p] = held && p0 + p < a.logit_pieces ? *reinterpret_cast<const Floats*>(from + (p0 + p) * each) : Floats(0.0f);
 #pragma unroll
-                for (int q = 0; q < Q; ++q)
-                    if (q * kWave + lane < a.E) z[q] += a.bias[q * kWave + lane];
+                for (int p = 0; p < AHEAD; ++p)
+#pragma unroll
+                    for (int q = 0; q < Q; ++q) z[q] += part_of(v[p], q);
             }
+#pragma unroll
+            for (int q = 0; q < Q; ++q) z[q] += bias[q];
         }
-        const int32_t* idx = a.idx + (size_t)t * a.k;
-        const float *w = a.w + (size_t)t * a.k, *g = a.g + (size_t)t * a.k;
         if (a.gating == MOE_GATE_SOFTMAX) {
             float most = -INFINITY, sum = 0.0f, c = 0.0f, p[Q];
+            for_slots(a, t, [&](int e, float, float g) {
+#pragma unroll
+                for (int q = 0; q < Q; ++q)
+                    if (e == e0 + q) dz[q] += g;
+            });
 #pragma unroll
             for (int q = 0; q < Q; ++q)
-                if (q * kWave + lane < a.E) most = fmaxf(most, z[q]);
+                if (in[q]) most = fmaxf(most, z[q]);
             most = wave_most(most);
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
-                p[q] = q * kWave + lane < a.E ? expf(z[q] - most) : 0.0f;
+                p[q] = in[q] ? expf(z[q] - most) : 0.0f;
                 sum += p[q];
-            }
-            sum = wave_add(sum);
-            for (int i = 0; i < a.k; ++i) {
-                const int e = idx[i] < a.E ? idx[i] : -1;
-#pragma unroll
-                for (int q = 0; q < Q; ++q)
-                    if (e == q * kWave + lane) dz[q] += g[i];
-            }
-#pragma unroll
-            for (int q = 0; q < Q; ++q) {
-                p[q] /= sum;
                 c = fmaf(p[q], dz[q], c);
             }
-            c = wave_add(c);
+            sum = wave_add(sum);
+            c = wave_add(c) / sum;
 #pragma unroll
-            for (int q = 0; q < Q; ++q) dz[q] = q * kWave + lane < a.E ? p[q] * (dz[q] - c) : 0.0f;
+            for (int q = 0; q < Q; ++q) dz[q] = in[q] ? p[q] / sum * (dz[q] - c) : 0.0f;
         } else {
             float c = 0.0f;
-            for (int i = 0; i < a.k; ++i)
-                if ((uint32_t)idx[i] < (uint32_t)a.E) c = fmaf(w[i], g[i], c);
-            for (int i = 0; i < a.k; ++i) {
-                const int e = idx[i] < a.E ? idx[i] : -1;
-                const float v = w[i] * (g[i] - c);
+            for_slots(a, t, [&](int e, float w, float g) {
+                if (e >= 0) c = fmaf(w, g, c);
+            });
+            for_slots(a, t, [&](int e, float w, float g) {
+                const float v = w * (g - c);
 #pragma unroll
                 for (int q = 0; q < Q; ++q)
-                    if (e == q * kWave + lane) dz[q] += v;
-            }
+                    if (e == e0 + q) dz[q] += v;
+            });
             if (a.gating == MOE_GATE_SIGMOID_NORM) {
 #pragma unroll
                 for (int q = 0; q < Q; ++q) dz[q] = dz[q] != 0.0f ? dz[q] / (1.0f + expf(z[q])) : 0.0f;
             }
         }
-        uint16_t* to = a.dz + (size_t)t * a.parts * a.Ep;
+        uint16_t* to = a.dz + (size_t)t * a.parts * a.Ep + e0;
+        float left[Q];
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
-            const int e = q * kWave + lane;
             bias_acc[q] += dz[q];
-            float left = dz[q];
-            for (int h = 0; h < a.parts; ++h) {
-                const uint16_t v = float_to_bf16_bits(left);
-                to[h * a.Ep + e] = v;
-                left -= bf16_bits_to_float(v);
+            left[q] = dz[q];
+        }
+        for (int h = 0; h < a.parts; ++h) {
+            Halves out;
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                const uint16_t v = float_to_bf16_bits(left[q]);
+                if constexpr (Q == 1) out = v;
+                else out[q] = v;
+                left[q] -= bf16_bits_to_float(v);
             }
+            if (held) *reinterpret_cast<Halves*>(to + h * a.Ep) = out;
         }
     }
 #pragma unroll
-    for (int q = 0; q < Q; ++q) bias_sum[wave][q * kWave + lane] = bias_acc[q];
+    for (int q = 0; q < Q; ++q) bias_sum[wave][e0 + q] = bias_acc[q];
     __syncthreads();
-    for (int e = threadIdx.x; e < Q * kWave; e += kDzThreads) {
+    for (int e = threadIdx.x; e < a.E; e += kDzThreads) {
         float v = bias_sum[0][e];
 #pragma unroll
         for (int i = 1; i < kDzWaves; ++i) v += bias_sum[i][e];
@@ -178,94 +220,17 @@ __device__ __forceinline__ void dx_tile(const RouteArgs& a, int m0, int n0, char
         constexpr int MB = decltype(height)::value;
         Acc<S, MB> acc;
         clear<S, MB>(acc);
-#pragma unroll 1
-        for (int h = 0; h < 2; ++h)
-            multiply<S, MB, true, false>(acc, Stream<true, S::BK>::make(a.dz + (size_t)m0 * ld + h * a.Ep, ld, rows, a.Ep, h * a.Ep),
-                                         Stream<false, S::BK>::make(a.wr, a.d, n0, a.E), la, lb, a.Ep / S::BK, lds);
+        multiply<S, MB, true, false>(acc, Repeat<Stream<true, S::BK>>::make(Stream<true, S::BK>::make(a.dz + (size_t)m0 * ld, ld, rows, a.Ep), 2, (uint32_t)a.Ep * 2),
+                                     Repeat<Stream<false, S::BK>>::make(Stream<false, S::BK>::make(a.wr, a.d, n0, a.E), 2, 0), la, lb, a.Ep / S::BK * 2, lds);
         by_rows_bf16<S, MB>(acc, lds, [&](int r, int c, u32x4_t v) {
             if (r < rows && n0 + c * 8 < a.d) *reinterpret_cast<u32x4_t*>(a.dx + (size_t)(m0 + r) * a.d + n0 + c * 8) = v;
         });
     });
 }
 
-// Tile of dW_r = dz^T x over one piece of the tokens, dz's parts one after the other.
-template <class S>
-__device__ __forceinline__ void dw_tile(const RouteArgs& a, int piece, int m0, int n0, char* lds) {
-    const int all = (a.T + S::BK - 1) / S::BK, each = (all + a.weight_pieces - 1) / a.weight_pieces, s0 = piece * each, s1 = s0 + each < all ? s0 + each : all;
-    const int t0 = s0 * S::BK, tokens = a.T - t0 < (s1 - s0) * S::BK ? a.T - t0 : (s1 - s0) * S::BK, ld = a.parts * a.Ep;
-    const int wave = __builtin_amdgcn_readfirstlane(body_thread() / kWave), lane = body_thread() % kWave;
-    typename S::template LoadA<false> la;
-    typename S::template LoadB<false> lb;
-    la.init(ld, wave, lane);
-    lb.init(a.d, wave, lane);
-    by_height<S>(a.E - m0, [&](auto height) {
-        constexpr int MB = decltype(height)::value;
-        Acc<S, MB> acc;
-        clear<S, MB>(acc);
-#pragma unroll 1
-        for (int h = 0; h < a.parts; ++h)
-            multiply<S, MB, false, false>(acc, Stream<false, S::BK>::make(a.dz + (size_t)t0 * ld, ld, m0 + h * a.Ep, tokens),
-                                          Stream<false, S::BK>::make(a.x + (size_t)t0 * a.d, a.d, n0, tokens), la, lb, s1 - s0, lds);
-        by_rows<S, S::BN / 8>(acc, lds, AheadNothing{}, [&](int r, int c, const float* row, Nothing) {
-            if (m0 + r >= a.E || n0 + c * 8 >= a.d) return;
-            float* to = a.sums + ((size_t)piece * a.E + m0 + r) * a.d + n0 + c * 8;
-            *reinterpret_cast<f32x4*>(to) = *reinterpret_cast<const f32x4*>(row + c * 8);
-            *reinterpret_cast<f32x4*>(to + 4) = *reinterpret_cast<const f32x4*>(row + c * 8 + 4);
-        });
-    });
-}
-
-// Both products in one launch, the longer tiles (dW_r's) first.
-template <class S>
-__global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void route_products_kernel(RouteArgs a) {
-    __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
-    const int cols = (a.d + S::BN - 1) / S::BN, heads = (a.E + S::BM - 1) / S::BM, blocks = (a.T + S::BM - 1) / S::BM;
-    const int weights = a.dwr ? a.weight_pieces * cols * heads : 0, ids = (weights + 7) / 8 * 8;
-    if ((int)blockIdx.x < ids) {
-        const int t = xcd_tile(blockIdx.x, weights);
-        if (t >= 0) dw_tile<S>(a, t / (cols * heads), t % heads * S::BM, t / heads % cols * S::BN, lds);
-        return;
-    }
-    const int t = xcd_tile(blockIdx.x - ids, blocks * cols);
-    if (t < 0) return;
-    int m, n;
-    patch(t, blocks, cols, m, n);
-    dx_tile<S>(a, m * S::BM, n * S::BN, lds);
-}
-
-// The pieces of dW_r, eight elements per thread, in their order; the first workgroups add up dbias, sixteen experts each.
-constexpr int kBiasExperts = 16;
-__global__ __launch_bounds__(256) void route_join_kernel(RouteArgs a) {
-    const int bias_groups = a.dbias ? (a.E + kBiasExperts - 1) / kBiasExperts : 0;
-    if ((int)blockIdx.x < bias_groups) {
-        constexpr int SEGS = 256 / kBiasExperts;
-        __shared__ float part[SEGS][kBiasExperts];
-        const int e = blockIdx.x * kBiasExperts + threadIdx.x % kBiasExperts, seg = threadIdx.x / kBiasExperts;
-        float v = 0.0f;
-        if (e < a.E) {
-#pragma unroll 8
-            for (int b = seg; b < a.dz_blocks; b += SEGS) v += a.bias_part[(size_t)b * a.Ep + e];
-        }
-        part[seg][threadIdx.x % kBiasExperts] = v;
-        __syncthreads();
-        if (seg == 0 && e < a.E) {
-            float sum = a.add ? a.dbias[e] : 0.0f;
-            for (int i = 0; i < SEGS; ++i) sum += part[i][threadIdx.x];
-            a.dbias[e] = sum;
-        }
-        return;
-    }
-    const size_t at = ((size_t)(blockIdx.x - bias_groups) * 256 + threadIdx.x) * 8, n = (size_t)a.E * a.d;
-    if (at >= n) return;
-    float sum[8], v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
-#pragma unroll 4
-    for (int p = 0; p < a.weight_pieces; ++p) {
-        load8(a.sums + p * n + at, v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i] += v[i];
-    }
+// Eight elements of dW_r, on top of what it holds or not.
+__device__ __forceinline__ void store_weights(const RouteArgs& a, size_t at, float (&sum)[8]) {
+    float v[8];
     if (a.f32) {
         float* to = reinterpret_cast<float*>(a.dwr) + at;
         if (a.add) {
@@ -286,7 +251,105 @@ __global__ __launch_bounds__(256) void route_join_kernel(RouteArgs a) {
     }
 }
 
-int padded(const moe_config& c) { return (c.E + 63) / 64 * 64; }
+// dbias of sixteen experts, from the sums of the workgroups that formed dz; by any number of threads that is a multiple of sixteen, up to 512.
+constexpr int kBiasExperts = 16;
+template <int THREADS>
+__device__ __forceinline__ void bias_group(const RouteArgs& a, int group, float (*part)[kBiasExperts]) {
+    constexpr int SEGS = THREADS / kBiasExperts;
+    const int mine = threadIdx.x % kBiasExperts, e = group * kBiasExperts + mine, seg = threadIdx.x / kBiasExperts;
+    float v = 0.0f;
+    if (e < a.E) {
+#pragma unroll 8
+        for (int b = seg; b < a.dz_blocks; b += SEGS) v += a.bias_part[(size_t)b * a.Ep + e];
+    }
+    part[seg][mine] = v;
+    __syncthreads();
+    if (seg == 0 && e < a.E) {
+        float sum = a.add ? a.dbias[e] : 0.0f;
+        for (int i = 0; i < SEGS; ++i) sum += part[i][mine];
+        a.dbias[e] = sum;
+    }
+}
+__host__ __device__ inline int bias_groups(const RouteArgs& a) { return a.dbias ? (a.E + kBiasExperts - 1) / kBiasExperts : 0; }
+
+// Tile of dW_r = dz^T x over one piece of the tokens, dz's parts one after the other.
+template <class S>
+__device__ __forceinline__ void dw_tile(const RouteArgs& a, int piece, int m0, int n0, char* lds) {
+    const int all = (a.T + S::BK - 1) / S::BK, each = (all + a.weight_pieces - 1) / a.weight_pieces, s0 = piece * each, s1 = s0 + each < all ? s0 + each : all;
+    const int t0 = s0 * S::BK, tokens = a.T - t0 < (s1 - s0) * S::BK ? a.T - t0 : (s1 - s0) * S::BK, ld = a.parts * a.Ep;
+    const int wave = __builtin_amdgcn_readfirstlane(body_thread() / kWave), lane = body_thread() % kWave;
+    typename S::template LoadA<false> la;
+    typename S::template LoadB<false> lb;
+    la.init(ld, wave, lane);
+    lb.init(a.d, wave, lane);
+    by_height<S>(a.E - m0, [&](auto height) {
+        constexpr int MB = decltype(height)::value;
+        Acc<S, MB> acc;
+        clear<S, MB>(acc);
+        using From = Stream<false, S::BK>;
+        multiply<S, MB, false, false>(acc, Repeat<From>::make(From::make(a.dz + (size_t)t0 * ld, ld, m0, tokens), a.parts, (uint32_t)a.Ep * 2),
+                                      Repeat<From>::make(From::make(a.x + (size_t)t0 * a.d, a.d, n0, tokens), a.parts, 0), la, lb, a.parts * (s1 - s0), lds);
+        by_rows<S, S::BN / 8>(acc, lds, AheadNothing{}, [&](int r, int c, const float* row, Nothing) {
+            if (m0 + r >= a.E || n0 + c * 8 >= a.d) return;
+            const size_t at = (size_t)(m0 + r) * a.d + n0 + c * 8;
+            if (a.weight_pieces == 1) {
+                float v[8];
+                load8(row + c * 8, v);
+                return store_weights(a, at, v);
+            }
+            float* to = a.sums + (size_t)piece * a.E * a.d + at;
+            *reinterpret_cast<f32x4*>(to) = *reinterpret_cast<const f32x4*>(row + c * 8);
+            *reinterpret_cast<f32x4*>(to + 4) = *reinterpret_cast<const f32x4*>(row + c * 8 + 4);
+        });
+    });
+}
+
+// Both products in one launch, and dbias.  The tiles of dW_r, which are several times as long, come first: one per CU at most (weight_pieces_of), whose other workgroup
+// takes tiles of dx.
+template <class S>
+__global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void route_products_kernel(RouteArgs a) {
+    __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
+    const int cols = (a.d + S::BN - 1) / S::BN, heads = (a.E + S::BM - 1) / S::BM, blocks = (a.T + S::BM - 1) / S::BM;
+    const int weights = a.dwr ? a.weight_pieces * cols * heads : 0, rows = a.dx ? blocks * cols : 0, ids_w = (weights + 7) / 8 * 8, ids_r = (rows + 7) / 8 * 8;
+    const int id = blockIdx.x;
+    if (id >= ids_w + ids_r) return bias_group<S::THREADS>(a, id - ids_w - ids_r, reinterpret_cast<float(*)[kBiasExperts]>(lds));
+    if (id < ids_w) {
+        const int t = xcd_tile(id, weights);
+        if (t >= 0) dw_tile<S>(a, t / (cols * heads), t % heads * S::BM, t / heads % cols * S::BN, lds);
+        return;
+    }
+    const int t = xcd_tile(id - ids_w, rows);
+    if (t < 0) return;
+    int m, n;
+    patch(t, blocks, cols, m, n);
+    dx_tile<S>(a, m * S::BM, n * S::BN, lds);
+}
+
+// The pieces of dW_r, eight elements per thread, in their order.
+__global__ __launch_bounds__(256) void route_join_kernel(RouteArgs a) {
+    const size_t at = ((size_t)blockIdx.x * 256 + threadIdx.x) * 8, n = (size_t)a.E * a.d;
+    if (at >= n) return;
+    float sum[8], v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+#pragma unroll 4
+    for (int p = 0; p < a.weight_pieces; ++p) {
+        load8(a.sums + p * n + at, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += v[i];
+    }
+    store_weights(a, at, sum);
+}
+
+// dbias where there is nothing else to do.
+__global__ __launch_bounds__(256) void route_bias_kernel(RouteArgs a) {
+    __shared__ float part[256 / kBiasExperts][kBiasExperts];
+    bias_group<256>(a, blockIdx.x, part);
+}
+
+bool few_tokens(const moe_config& c) { return c.T <= Flat::BM; }
+// Experts rounded up to whole steps of the products' reduction.
+int padded(const moe_config& c) { return few_tokens(c) ? (c.E + Flat::BK - 1) / Flat::BK * Flat::BK : (c.E + Pair::BK - 1) / Pair::BK * Pair::BK; }
 bool few_experts(const moe_config& c) { return c.E <= Flat::BM; }
 
 template <class S>
@@ -301,16 +364,12 @@ int logit_pieces(const moe_config& c) {
     if (c.gating == MOE_GATE_SOFTMAX_RENORM) return 0;
     return few_experts(c) ? logit_pieces_of<Flat>(c) : logit_pieces_of<Small>(c);
 }
-bool few_tokens(const moe_config& c) { return c.T <= Flat::BM; }
 constexpr int kMostParts = 3;
-// Pieces of the tokens that dW_r is summed over: as many as make its tiles about as long as a place's share of the whole launch.
+// Pieces of the tokens that dW_r is summed over: one tile of it per CU, beside which the CU's other workgroups take tiles of dx; no shorter than four steps.
 template <class S>
 int weight_pieces_of(const moe_config& c) {
-    const long long cols = (c.d + S::BN - 1) / S::BN, weights = (c.E + S::BM - 1) / S::BM * cols, rows = (c.T + S::BM - 1) / S::BM * cols;
-    const long long steps = (long long)kMostParts * ((c.T + S::BK - 1) / S::BK), share = (weights * steps + rows * (2 * padded(c) / S::BK)) / (256 * S::PER);
-    const long long most = (c.T + 4 * S::BK - 1) / (4 * S::BK);
-    long long n = (steps + share) / (share + 1);
-    if (n > 8) n = 8;
+    const long long tiles = (long long)((c.d + S::BN - 1) / S::BN) * ((c.E + S::BM - 1) / S::BM), most = c.T / (4 * S::BK);
+    long long n = 256 / tiles;
     if (n > most) n = most;
     return n < 1 ? 1 : (int)n;
 }
@@ -331,7 +390,7 @@ RouteSpace space(const moe_config& c) {
     s.part = take((size_t)logit_pieces(c) * T * Ep * sizeof(float));
     s.dz = take(T * kMostParts * Ep * sizeof(uint16_t));
     s.bias = take((size_t)dz_blocks(c) * Ep * sizeof(float));
-    s.sums = take(c.T > 0 ? (size_t)weight_pieces(c) * c.E * c.d * sizeof(float) : 0);
+    s.sums = take(weight_pieces(c) > 1 ? (size_t)weight_pieces(c) * c.E * c.d * sizeof(float) : 0);
     s.total = at;
     return s;
 }
@@ -344,7 +403,7 @@ void go_logits(const RouteArgs& a, hipStream_t s) {
 template <class S>
 void go_products(const RouteArgs& a, hipStream_t s) {
     const long long cols = (a.d + S::BN - 1) / S::BN, weights = a.dwr ? a.weight_pieces * cols * ((a.E + S::BM - 1) / S::BM) : 0, rows = a.dx ? cols * ((a.T + S::BM - 1) / S::BM) : 0;
-    hipLaunchKernelGGL(route_products_kernel<S>, dim3(xcd_grid(weights) + xcd_grid(rows)), dim3(S::THREADS), 0, s, a);
+    hipLaunchKernelGGL(route_products_kernel<S>, dim3(xcd_grid(weights) + xcd_grid(rows) + bias_groups(a)), dim3(S::THREADS), 0, s, a);
 }
 
 }  // namespace
@@ -356,28 +415,25 @@ hipError_t launch_route_backward(const moe_config& c, const RouteGrad& p, hipStr
     RouteArgs a{p.x, p.wr, p.bias, p.idx, p.w, p.g, p.dx, p.dwr, p.dbias, p.f32, p.add, (float*)(p.workspace + at.part), (uint16_t*)(p.workspace + at.dz),
                 (float*)(p.workspace + at.bias), (float*)(p.workspace + at.sums), c.T, c.d, c.E, c.k, padded(c), c.gating, p.dwr && p.f32 ? 3 : 2,
                 logit_pieces(c), c.T > 0 ? weight_pieces(c) : 0, dz_blocks(c)};
-    const bool weights = (p.dwr || p.dbias) && !(c.T == 0 && p.add), rows = p.dx && c.T > 0;
-    if (!weights && !rows) return hipSuccess;
-    if (c.T > 0) {
-        if (a.logit_pieces > 0) {
-            if (few_experts(c)) go_logits<Flat>(a, s);
-            else go_logits<Small>(a, s);
-        }
-        switch (a.Ep / kWave) {
-            case 1: hipLaunchKernelGGL(route_dz_kernel<1>, dim3(a.dz_blocks), dim3(kDzThreads), 0, s, a); break;
-            case 2: hipLaunchKernelGGL(route_dz_kernel<2>, dim3(a.dz_blocks), dim3(kDzThreads), 0, s, a); break;
-            case 3: hipLaunchKernelGGL(route_dz_kernel<3>, dim3(a.dz_blocks), dim3(kDzThreads), 0, s, a); break;
-            default: hipLaunchKernelGGL(route_dz_kernel<4>, dim3(a.dz_blocks), dim3(kDzThreads), 0, s, a);
-        }
-        if (rows || p.dwr) {
-            if (few_tokens(c)) go_products<Flat>(a, s);
-            else go_products<Pair>(a, s);
-        }
+    const bool add_nothing = c.T == 0 && p.add;
+    if (add_nothing || (!(p.dx && c.T > 0) && !p.dwr && !p.dbias)) return hipSuccess;
+    const unsigned joins = (unsigned)(((size_t)c.E * c.d / 8 + 255) / 256);
+    if (c.T == 0) {            // sums over nothing
+        if (p.dwr) hipLaunchKernelGGL(route_join_kernel, dim3(joins), dim3(256), 0, s, a);
+        if (p.dbias) hipLaunchKernelGGL(route_bias_kernel, dim3(bias_groups(a)), dim3(256), 0, s, a);
+        return hipGetLastError();
     }
-    if (weights) {
-        const size_t groups = (p.dwr ? ((size_t)c.E * c.d / 8 + 255) / 256 : 0) + (p.dbias ? (c.E + kBiasExperts - 1) / kBiasExperts : 0);
-        hipLaunchKernelGGL(route_join_kernel, dim3((unsigned)groups), dim3(256), 0, s, a);
+    if (a.logit_pieces > 0) {
+        if (few_experts(c)) go_logits<Flat>(a, s);
+        else go_logits<Small>(a, s);
     }
+    if (a.Ep <= kWave) hipLaunchKernelGGL(route_dz_kernel<1>, dim3(a.dz_blocks), dim3(kDzThreads), 0, s, a);
+    else if (a.Ep <= 2 * kWave) hipLaunchKernelGGL(route_dz_kernel<2>, dim3(a.dz_blocks), dim3(kDzThreads), 0, s, a);
+    else hipLaunchKernelGGL(route_dz_kernel<4>, dim3(a.dz_blocks), dim3(kDzThreads), 0, s, a);
+    if (!p.dx && !p.dwr) hipLaunchKernelGGL(route_bias_kernel, dim3(bias_groups(a)), dim3(256), 0, s, a);
+    else if (few_tokens(c)) go_products<Flat>(a, s);
+    else go_products<Pair>(a, s);
+    if (p.dwr && a.weight_pieces > 1) hipLaunchKernelGGL(route_join_kernel, dim3(joins), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
