@@ -13,8 +13,10 @@ namespace moe {
 
 namespace {
 
-constexpr int kChunk = 1024;              // slots per workgroup of the count
-constexpr int kBins = 2048;               // counters in LDS: as many copies of the experts' as fit, so that one wavefront's slots rarely meet
+constexpr int kChunk = 1024;              // slots per workgroup of the count and the tables
+constexpr int kMostSlots = 1024;          // of a workgroup that moves rows
+constexpr int kNarrow = 256;              // width up to which lanes of a wavefront take several tokens
+constexpr int kBins = 512;                // counters in LDS: as many copies of the experts' as fit, so that one wavefront's slots rarely meet
 
 struct DispatchArgs {
     const uint16_t* x;
@@ -34,22 +36,28 @@ __device__ __forceinline__ int local_expert(const DispatchArgs& a, long long j) 
     return (uint32_t)e < (uint32_t)a.E ? e : -1;
 }
 
-// Slots j0 .. j1 - 1 into the bins; those from `split` on into the second half.
+// Slots j0 .. j1 - 1 into the bins; those from `split` on into the second half.  Sixteen ids per thread are requested before the first is counted.
+template <int THREADS>
 __device__ __forceinline__ void count_slots(const DispatchArgs& a, long long j0, long long j1, long long split, int copies, int* bins) {
     const int mine = (threadIdx.x & (copies - 1)) * a.E;
-#pragma unroll 4
-    for (long long j = j0 + threadIdx.x; j < j1; j += kTokenThreads) {
-        const int e = local_expert(a, j);
-        if (e >= 0) atomicAdd(&bins[(j >= split ? kBins : 0) + mine + e], 1);
+    constexpr int AHEAD = 16;
+    for (long long j = j0 + threadIdx.x; j < j1; j += AHEAD * THREADS) {
+        int e[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) e[i] = j + i * THREADS < j1 ? local_expert(a, j + i * THREADS) : -1;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            if (e[i] >= 0) atomicAdd(&bins[(j + i * THREADS >= split ? kBins : 0) + mine + e[i]], 1);
     }
 }
 __device__ __forceinline__ int bin_copies(int E) {
-    int n = 64;
+    int n = 32;
     while (n * E > kBins) n >>= 1;
     return n;
 }
 __device__ __forceinline__ int bin_total(const int* bins, int copies, int E, int e) {
     int n = 0;
+#pragma unroll 8
     for (int c = 0; c < copies; ++c) n += bins[c * E + e];
     return n;
 }
@@ -60,7 +68,7 @@ __global__ __launch_bounds__(kTokenThreads) void count_chunks_kernel(DispatchArg
     for (int i = threadIdx.x; i < copies * a.E; i += kTokenThreads) bins[i] = 0;
     __syncthreads();
     const long long R = (long long)a.T * a.k, j0 = (long long)blockIdx.x * kChunk, j1 = j0 + kChunk < R ? j0 + kChunk : R;
-    count_slots(a, j0, j1, j1, copies, bins);
+    count_slots<kTokenThreads>(a, j0, j1, j1, copies, bins);
     __syncthreads();
     if ((int)threadIdx.x < a.E) a.hist[(size_t)blockIdx.x * a.E + threadIdx.x] = bin_total(bins, copies, a.E, threadIdx.x);
 }
@@ -138,78 +146,126 @@ __device__ __forceinline__ void scatter_slots(const ScatterArgs& a, const Slots<
     }
 }
 
+// Where every expert's slots go on from: before[e] slots in front of the workgroup's own, start[e] the expert's first row.  All of it from LDS counts of all slots, or, with
+// `hist`, of the slots between the chunk's start and the workgroup's own and the chunks' counts.  The first workgroup writes counts and offsets.
+template <int THREADS>
+struct Places {
+    int bins[2 * kBins];
+    int next[kMaxExperts], start[kMaxExperts], sums[THREADS / kWave];
+
+    __device__ __forceinline__ void find(const DispatchArgs& a, long long s0) {
+        const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, copies = bin_copies(a.E), chunk = (int)(s0 / kChunk);
+        const long long R = (long long)a.T * a.k;
+        for (int i = tid; i < copies * a.E; i += THREADS) bins[i] = bins[kBins + i] = 0;
+        __syncthreads();
+        if (a.hist) count_slots<THREADS>(a, (long long)chunk * kChunk, s0, s0, copies, bins);
+        else count_slots<THREADS>(a, 0, R, s0, copies, bins);
+        __syncthreads();
+        int total = 0, before = 0;
+        if (tid < a.E) {
+            before = bin_total(bins, copies, a.E, tid);
+            if (!a.hist) total = before + bin_total(bins + kBins, copies, a.E, tid);
+            else if (a.summed) before += a.hist[(size_t)chunk * a.E + tid], total = a.counts[tid];
+            else {
+#pragma unroll 16
+                for (int c = 0; c < a.chunks; ++c) {
+                    const int n = a.hist[(size_t)c * a.E + tid];
+                    total += n;
+                    before += c < chunk ? n : 0;
+                }
+            }
+        }
+        const int most = a.capacity ? a.capacity : 0x7fffffff, kept = total < most ? total : most;
+        int upto = kept;
+#pragma unroll
+        for (int o = 1; o < kWave; o <<= 1) {
+            const int up = __shfl_up(upto, o, kWave);
+            if (lane >= o) upto += up;
+        }
+        if (lane == kWave - 1) sums[wave] = upto;
+        __syncthreads();
+        for (int w = 0; w < wave && w < kMaxExperts / kWave; ++w) upto += sums[w];
+        if (tid < a.E) {
+            next[tid] = before;
+            start[tid] = upto - kept;
+            if (blockIdx.x == 0) {
+                if (!a.summed) a.counts[tid] = total;
+                a.offsets[tid] = upto - kept;
+                if (tid == a.E - 1) a.offsets[a.E] = upto;
+            }
+        }
+        __syncthreads();
+    }
+};
+
+// Of the wavefront's lanes, those whose slot chose the same expert (they agree in all eight bits; e < 0: none).
+__device__ __forceinline__ unsigned long long same_expert(int e) {
+    unsigned long long same = __ballot(e >= 0);
+#pragma unroll
+    for (int b = 0; b < 8; ++b) {
+        const unsigned long long has = __ballot((e >> b) & 1);
+        same &= (e >> b) & 1 ? has : ~has;
+    }
+    return same;
+}
+__device__ __forceinline__ int in_front(unsigned long long lanes, int lane) { return __popcll(lanes & ((1ull << lane) - 1)); }
+
+// The tables alone, 1024 slots per workgroup, a slot per thread.  A wavefront ranks its 64 slots among themselves, a sum over the wavefronts' counts does the rest.
+constexpr int kTableThreads = kChunk, kTableWaves = kTableThreads / kWave;
+__global__ __launch_bounds__(kTableThreads) void tables_kernel(DispatchArgs a) {
+    __shared__ Places<kTableThreads> places;
+    __shared__ int count[kTableWaves][kMaxExperts];      // of every wavefront; then of those in front of it
+    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    const long long R = (long long)a.T * a.k, s0 = (long long)blockIdx.x * kChunk, j = s0 + tid;
+    const int e = j < R ? local_expert(a, j) : -1;
+    for (int i = tid; i < kTableWaves * kMaxExperts; i += kTableThreads) (&count[0][0])[i] = 0;
+    places.find(a, s0);
+    const unsigned long long same = same_expert(e);
+    const int rank = in_front(same, lane);
+    if (e >= 0 && rank == 0) count[wave][e] = __popcll(same);
+    __syncthreads();
+    if (tid < a.E) {
+        int n = places.next[tid];
+#pragma unroll
+        for (int w = 0; w < kTableWaves; ++w) {
+            const int m = count[w][tid];
+            count[w][tid] = n;
+            n += m;
+        }
+    }
+    __syncthreads();
+    if (j >= R) return;
+    const int r = e >= 0 ? count[wave][e] + rank : 0, most = a.capacity ? a.capacity : 0x7fffffff, row = e >= 0 && r < most ? places.start[e] + r : -1;
+    a.row_of[j] = row;
+    if (row >= 0) a.src_of[row] = (int32_t)j;
+}
+
 // What the lanes of a wavefront did to LDS so far comes before what they do from here on.
 __device__ __forceinline__ void order_lanes() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 }
 
-// A workgroup takes `per` tokens.  It counts the slots in front of its own (all of them, or those of its chunk, with the other chunks' counts from the
-// launch before), sums the experts' totals up, ranks its own slots in order, and moves its tokens' rows: with several tokens a wavefront each.
-template <int N, bool NT>
+// Tables and rows: a workgroup takes `per` tokens, finds out where its slots go, ranks them, and moves its tokens' rows: less than four tokens one after the other, more a
+// wavefront each, narrow ones (d up to kNarrow, half a wavefront's loads) a few lanes each.
+template <int N, bool NT, bool NARROW>
 __global__ __launch_bounds__(kTokenThreads) void dispatch_kernel(DispatchArgs a) {
-    __shared__ int bins[2 * kBins];
-    __shared__ int next[kMaxExperts], start[kMaxExperts], sums[kTokenWaves];
-    __shared__ int row[kChunk];
+    __shared__ Places<kTokenThreads> places;
+    __shared__ int row[kMostSlots];
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const long long R = (long long)a.T * a.k, s0 = (long long)blockIdx.x * a.per * a.k, s1 = s0 + (long long)a.per * a.k < R ? s0 + (long long)a.per * a.k : R;
-    const int copies = bin_copies(a.E);
-    for (int i = tid; i < copies * a.E; i += kTokenThreads) bins[i] = bins[kBins + i] = 0;
-    __syncthreads();
-    const int chunk = (int)(s0 / kChunk);
-    if (a.hist) count_slots(a, (long long)chunk * kChunk, s0, s0, copies, bins);
-    else count_slots(a, 0, R, s0, copies, bins);
-    __syncthreads();
-    int total = 0, before = 0;
-    if (tid < a.E) {
-        before = bin_total(bins, copies, a.E, tid);
-        if (!a.hist) total = before + bin_total(bins + kBins, copies, a.E, tid);
-        else if (a.summed) before += a.hist[(size_t)chunk * a.E + tid], total = a.counts[tid];
-        else {
-#pragma unroll 16
-            for (int c = 0; c < a.chunks; ++c) {
-                const int n = a.hist[(size_t)c * a.E + tid];
-                total += n;
-                before += c < chunk ? n : 0;
-            }
-        }
-    }
-    const int most = a.capacity ? a.capacity : 0x7fffffff, kept = total < most ? total : most;
-    int upto = kept;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-        const int up = __shfl_up(upto, o, kWave);
-        if (lane >= o) upto += up;
-    }
-    if (lane == kWave - 1) sums[wave] = upto;
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) upto += sums[w];
-    if (tid < a.E) {
-        next[tid] = before;
-        start[tid] = upto - kept;
-        if (blockIdx.x == 0) {
-            if (!a.summed) a.counts[tid] = total;
-            a.offsets[tid] = upto - kept;
-            if (tid == a.E - 1) a.offsets[a.E] = upto;
-        }
-    }
-    __syncthreads();
-    // ranks: 64 slots at a time; the lanes whose slot chose the same expert are those that agree in all eight bits
+    places.find(a, s0);
     if (wave == 0) {
+        const int most = a.capacity ? a.capacity : 0x7fffffff;
         for (long long j0 = s0; j0 < s1; j0 += kWave) {
             const long long j = j0 + lane;
             const int e = j < s1 ? local_expert(a, j) : -1;
-            unsigned long long same = __ballot(e >= 0);
-#pragma unroll
-            for (int b = 0; b < 8; ++b) {
-                const unsigned long long has = __ballot((e >> b) & 1);
-                same &= (e >> b) & 1 ? has : ~has;
-            }
-            const int in_front = __popcll(same & ((1ull << lane) - 1)), base = e >= 0 ? next[e] : 0;
+            const unsigned long long same = same_expert(e);
+            const int rank = in_front(same, lane), base = e >= 0 ? places.next[e] : 0;
             order_lanes();                 // every lane has read the count before the first of its expert advances it
-            if (e >= 0 && in_front == 0) next[e] = base + __popcll(same);
+            if (e >= 0 && rank == 0) places.next[e] = base + __popcll(same);
             order_lanes();
-            const int r = e >= 0 && base + in_front < most ? start[e] + base + in_front : -1;
+            const int r = e >= 0 && base + rank < most ? places.start[e] + base + rank : -1;
             if (j < s1) {
                 row[j - s0] = r;
                 a.row_of[j] = r;
@@ -217,17 +273,34 @@ __global__ __launch_bounds__(kTokenThreads) void dispatch_kernel(DispatchArgs a)
             }
         }
     }
-    if (!a.rows) return;
     __syncthreads();
-    const ScatterArgs to{a.x, nullptr, a.rows, a.d, a.w != nullptr, {}};
-    const bool whole = a.per < kTokenWaves;
     const int tokens = (int)((s1 - s0) / a.k), first = (int)(s0 / a.k);
-    for (int t = whole ? 0 : wave; t < tokens; t += whole ? 1 : kTokenWaves) {
-        for (int i0 = 0; i0 < a.k; i0 += N) {
-            Slots<N> s;
-            s.load(row + t * a.k, a.w ? a.w + (size_t)(first + t) * a.k : nullptr, i0, a.k, R);
-            float dot[N];
-            scatter_slots<N, false, NT>(to, s, first + t, whole ? tid : lane, whole ? kTokenThreads : kWave, 0, 0, dot);
+    if constexpr (NARROW) {
+        const int lots = a.d / 8;
+        for (int q = tid; q < tokens * lots; q += kTokenThreads) {
+            const int t = q / lots, c = q - t * lots;
+            const u32x4_t raw = *reinterpret_cast<const u32x4_t*>(a.x + ((size_t)first * lots + q) * 8);
+            float v[8], o[8];
+            floats8(raw, v);
+            for (int i = 0; i < a.k; ++i) {
+                const int r = row[t * a.k + i];
+                if (r < 0) continue;
+                const float w = a.w ? a.w[s0 + t * a.k + i] : 1.0f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] = w * v[j];
+                *reinterpret_cast<u32x4_t*>(a.rows + (size_t)r * a.d + c * 8) = a.w ? bf16s8(o) : raw;
+            }
+        }
+    } else {
+        const ScatterArgs to{a.x, nullptr, a.rows, a.d, a.w != nullptr, {}};
+        const bool whole = a.per < kTokenWaves;
+        for (int t = whole ? 0 : wave; t < tokens; t += whole ? 1 : kTokenWaves) {
+            for (int i0 = 0; i0 < a.k; i0 += N) {
+                Slots<N> s;
+                s.load(row + t * a.k, a.w ? a.w + (size_t)(first + t) * a.k : nullptr, i0, a.k, R);
+                float dot[N];
+                scatter_slots<N, false, NT>(to, s, first + t, whole ? tid : lane, whole ? kTokenThreads : kWave, 0, 0, dot);
+            }
         }
     }
 }
@@ -345,6 +418,115 @@ __global__ __launch_bounds__(kTokenThreads) void scatter_kernel(CollectArgs a) {
     }
 }
 
+// NARROW rows (d up to 256): `lots` = d / 8 lanes per token, as many tokens as fit into a wavefront; the other lanes idle.
+struct NarrowPlace {
+    int t, c, lot;             // token (T: none), first column, the lane's place among the token's
+    bool there;
+};
+__device__ __forceinline__ NarrowPlace narrow_place(const CollectArgs& a) {
+    const int lots = a.d / 8, fit = kWave / lots, lane = threadIdx.x % kWave, mine = lane / lots, lot = lane - mine * lots;
+    const long long t = a.t0 + ((long long)blockIdx.x * kTokenWaves + threadIdx.x / kWave) * fit + mine;
+    const bool there = mine < fit && t < a.T;
+    return {there ? (int)t : 0, lot * 8, lot, there};
+}
+// Sum over the token's lanes, in its first one, always in the same order.
+__device__ __forceinline__ float narrow_total(float v, int lot, int lots) {
+#pragma unroll
+    for (int o = kWave / 4; o > 0; o >>= 1) {
+        const float up = __shfl_down(v, o, kWave);
+        if (lot + o < lots) v += up;
+    }
+    return v;
+}
+
+template <int N, bool DOT>
+__global__ __launch_bounds__(kTokenThreads) void narrow_gather_kernel(CollectArgs a) {
+    const NarrowPlace m = narrow_place(a);
+    const int lots = a.d / 8;
+    const size_t at = (size_t)m.t * a.d + m.c;
+    const long long R = (long long)a.T * a.k;
+    const u32x4_t none = {0, 0, 0, 0};
+    const u32x4_t more = m.there && a.add ? *reinterpret_cast<const u32x4_t*>(a.add + at) : none, with = DOT && m.there ? *reinterpret_cast<const u32x4_t*>(a.x + at) : none;
+    float sum[8], x[8];
+    floats8(with, x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
+    for (int i0 = 0; i0 < a.k; i0 += N) {
+        u32x4_t v[N];
+        float w[N];
+        bool has[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const size_t slot = (size_t)m.t * a.k + i0 + i;
+            const int32_t r = m.there && i0 + i < a.k ? a.row_of[slot] : -1;
+            has[i] = r >= 0 && r < R;
+            w[i] = has[i] ? a.w ? a.w[slot] : 1.0f : 0.0f;
+            v[i] = has[i] ? *reinterpret_cast<const u32x4_t*>(a.rows + (size_t)r * a.d + m.c) : none;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float q[8], dot = 0.0f;
+            floats8(v[i], q);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                sum[j] = fmaf(w[i], q[j], sum[j]);
+                if constexpr (DOT) dot = fmaf(x[j], q[j], dot);
+            }
+            if constexpr (DOT) {
+                dot = narrow_total(dot, m.lot, lots);
+                if (m.there && m.lot == 0 && i0 + i < a.k) a.dw[(size_t)m.t * a.k + i0 + i] = has[i] ? dot : 0.0f;
+            }
+        }
+    }
+    if (!m.there) return;
+    if (a.p.rng) drop8(sum, at / 8, a.p.rng[0], a.p.rng[1], a.p);
+    float o[8];
+    floats8(more, o);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j] += o[j];
+    *reinterpret_cast<u32x4_t*>(a.y + at) = bf16s8(sum);
+}
+
+template <int N, bool DOT>
+__global__ __launch_bounds__(kTokenThreads) void narrow_scatter_kernel(CollectArgs a) {
+    const NarrowPlace m = narrow_place(a);
+    const int lots = a.d / 8;
+    const size_t at = (size_t)m.t * a.d + m.c;
+    const long long R = (long long)a.T * a.k;
+    const u32x4_t none = {0, 0, 0, 0}, raw = m.there ? *reinterpret_cast<const u32x4_t*>(a.to.in + at) : none;
+    float v[8];
+    floats8(raw, v);
+    if (a.to.p.rng) drop8(v, at / 8, a.to.p.rng[0], a.to.p.rng[1], a.to.p);
+    for (int i0 = 0; i0 < a.k; i0 += N) {
+        u32x4_t with[N];
+        int32_t r[N];
+        float w[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const size_t slot = (size_t)m.t * a.k + i0 + i;
+            const int32_t n = m.there && i0 + i < a.k ? a.row_of[slot] : -1;
+            r[i] = n >= 0 && n < R ? n : -1;
+            w[i] = r[i] >= 0 && a.w ? a.w[slot] : 1.0f;
+            if constexpr (DOT) with[i] = r[i] >= 0 ? *reinterpret_cast<const u32x4_t*>(a.to.with + (size_t)r[i] * a.d + m.c) : none;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if constexpr (DOT) {
+                float q[8], dot = 0.0f;
+                floats8(with[i], q);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) dot = fmaf(v[j], q[j], dot);
+                dot = narrow_total(dot, m.lot, lots);
+                if (m.there && m.lot == 0 && i0 + i < a.k) a.dw[(size_t)m.t * a.k + i0 + i] = r[i] >= 0 ? dot : 0.0f;
+            }
+            float o[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] = w[i] * v[j];
+            if (r[i] >= 0) *reinterpret_cast<u32x4_t*>(a.to.out + (size_t)r[i] * a.d + m.c) = a.to.scaled ? bf16s8(o) : raw;
+        }
+    }
+}
+
 template <bool ADD>
 __global__ __launch_bounds__(kTokenThreads) void dropout_kernel(const uint16_t* x, const uint16_t* add, uint16_t* y, long long n, Dropout p) {
     const uint64_t seed = p.rng ? p.rng[0] : 0, offset = p.rng ? p.rng[1] : 0;
@@ -371,11 +553,15 @@ __global__ __launch_bounds__(kTokenThreads) void dropout_kernel(const uint16_t* 
     }
 }
 
-constexpr int kCountAll = 8192;           // slots up to which a workgroup counts them all
+// Slots up to which every workgroup counts them all (of the workgroups that move rows, of those that write the tables); beyond, a launch before counts them by chunks.
+constexpr int kCountAllRows = 4096, kCountAll = 16384;
 constexpr int kSumInside = 64;            // chunks up to which a workgroup adds their counts up
 
 int chunks_of(const moe_dispatch_config& c) { return (int)(((long long)c.T * c.k + kChunk - 1) / kChunk); }
 
+// From 128 MiB of rows on, half of the Infinity Cache, they pass the caches by.  Below, what is written is read next: 112 MiB of rows, us, cached / past the caches, the
+// gradient of collect alone 55.5 / 43.7 and with a collect of its rows 74.2 / 80.9, dispatch 31.5 / 31.6 and 58.8 / 58.0; 64 MiB 29.1 / 25.9 and 42.6 / 45.3,
+// 21.1 / 22.5 and 34.8 / 38.8.  Above: 448 MiB, the gradient 217 / 205, collect 120 / 99, dispatch 105 / 85.
 bool passes_caches(const moe_dispatch_config& c) { return (long long)c.T * c.k * c.d >= (1ll << 26); }
 
 // go(integral_constant<slots per batch>)
@@ -392,42 +578,19 @@ void by_slots(int k, F&& go) {
 template <class F>
 void by_launch(CollectArgs a, F&& go) {
     a.whole = a.d > 1024;
-    const int step = a.whole ? 1 << 23 : 1 << 25;
+    const int each = a.whole ? 1 : kTokenWaves * (a.d <= kNarrow ? kWave / (a.d / 8) : 1);       // tokens per workgroup
+    const int step = (1 << 23) * (each < 64 ? each : 64);
     for (long long t = 0; t < a.T; t += step) {
         a.t0 = (int)t;
         const long long n = a.T - t < step ? a.T - t : step;
-        go(a, dim3((unsigned)(a.whole ? n : (n + kTokenWaves - 1) / kTokenWaves)));
+        go(a, dim3((unsigned)((n + each - 1) / each)));
     }
 }
 
 }  // namespace
 
 size_t dispatch_workspace_bytes(const moe_dispatch_config& c) {
-    return (long long)c.T * c.k > kCountAll ? (size_t)chunks_of(c) * c.E * sizeof(int32_t) : 0;
-}
-
-hipError_t launch_dispatch(const moe_dispatch_config& c, const uint16_t* x, const int32_t* topk_idx, const float* topk_w, int32_t* counts, int32_t* offsets,
-                           int32_t* row_of, int32_t* src_of, uint16_t* rows, int32_t* hist, hipStream_t s) {
-    DispatchArgs a{x, topk_idx, topk_w, counts, offsets, row_of, src_of, rows, nullptr, c.T, c.d, c.k, c.E, c.first, c.capacity, 1, chunks_of(c), false};
-    if ((long long)c.T * c.k > kCountAll) {
-        a.hist = hist;
-        a.summed = a.chunks > kSumInside;
-        hipLaunchKernelGGL(count_chunks_kernel, dim3(a.chunks), dim3(kTokenThreads), 0, s, a);
-        if (a.summed) hipLaunchKernelGGL(sum_chunks_kernel, dim3((c.E + kWave - 1) / kWave), dim3(kSumThreads), 0, s, a);
-    }
-    // about a thousand workgroups; without rows to move, workgroups of a thousand slots
-    const int most = kChunk / c.k;
-    a.per = rows ? (c.T + 1023) / 1024 : most;
-    if (a.per > most) a.per = most;
-    if (a.per < 1) a.per = 1;
-    const unsigned grid = c.T > 0 ? (unsigned)(((long long)c.T + a.per - 1) / a.per) : 1;
-    const bool nt = passes_caches(c);
-    by_slots(c.k, [&](auto n) {
-        constexpr int N = decltype(n)::value;
-        if (nt) hipLaunchKernelGGL((dispatch_kernel<N, true>), dim3(grid), dim3(kTokenThreads), 0, s, a);
-        else hipLaunchKernelGGL((dispatch_kernel<N, false>), dim3(grid), dim3(kTokenThreads), 0, s, a);
-    });
-    return hipGetLastError();
+    return (long long)c.T * c.k > kCountAllRows ? (size_t)chunks_of(c) * c.E * sizeof(int32_t) : 0;
 }
 
 static hipError_t launch_gather(const moe_dispatch_config& c, CollectArgs a, hipStream_t s) {
@@ -435,6 +598,11 @@ static hipError_t launch_gather(const moe_dispatch_config& c, CollectArgs a, hip
     by_slots(c.k, [&](auto n) {
         constexpr int N = decltype(n)::value;
         by_launch(a, [&](const CollectArgs& b, dim3 grid) {
+            if (c.d <= kNarrow) {
+                if (b.dw) hipLaunchKernelGGL((narrow_gather_kernel<N, true>), grid, dim3(kTokenThreads), 0, s, b);
+                else hipLaunchKernelGGL((narrow_gather_kernel<N, false>), grid, dim3(kTokenThreads), 0, s, b);
+                return;
+            }
             auto go = [&](auto dot, auto many) {
                 constexpr bool DOT = decltype(dot)::value, MANY = decltype(many)::value;
                 if (nt) hipLaunchKernelGGL((gather_kernel<N, DOT, true, MANY>), grid, dim3(kTokenThreads), 0, s, b);
@@ -469,22 +637,53 @@ hipError_t launch_collect(const moe_dispatch_config& c, const uint16_t* rows, co
     return launch_gather(c, CollectArgs{{}, rows, residual, nullptr, row_of, topk_w, y, nullptr, dropout_of(p, rng), c.T, c.d, c.k, 0, false}, s);
 }
 
-hipError_t launch_collect_backward(const moe_dispatch_config& c, const uint16_t* dy, const uint16_t* rows, const int32_t* row_of, const float* topk_w, float p,
-                                   const void* rng, uint16_t* drows, float* d_topk_w, hipStream_t s) {
-    const Dropout drop = dropout_of(p, rng);
-    const CollectArgs a{{dy, rows, drows, c.d, topk_w != nullptr || drop.rng != nullptr, drop}, nullptr, nullptr, nullptr, row_of, topk_w, nullptr, d_topk_w, {}, c.T, c.d, c.k, 0, false};
+static hipError_t launch_scatter(const moe_dispatch_config& c, const ScatterArgs& to, const int32_t* row_of, const float* topk_w, float* d_topk_w, hipStream_t s) {
+    const CollectArgs a{to, nullptr, nullptr, nullptr, row_of, topk_w, nullptr, d_topk_w, {}, c.T, c.d, c.k, 0, false};
     const bool nt = passes_caches(c);
     by_slots(c.k, [&](auto n) {
         constexpr int N = decltype(n)::value;
         by_launch(a, [&](const CollectArgs& b, dim3 grid) {
-            if (b.dw) {
-                if (nt) hipLaunchKernelGGL((scatter_kernel<N, true, true>), grid, dim3(kTokenThreads), 0, s, b);
-                else hipLaunchKernelGGL((scatter_kernel<N, true, false>), grid, dim3(kTokenThreads), 0, s, b);
-            } else {
-                if (nt) hipLaunchKernelGGL((scatter_kernel<N, false, true>), grid, dim3(kTokenThreads), 0, s, b);
-                else hipLaunchKernelGGL((scatter_kernel<N, false, false>), grid, dim3(kTokenThreads), 0, s, b);
-            }
+            auto go = [&](auto dot) {
+                constexpr bool DOT = decltype(dot)::value;
+                if (c.d <= kNarrow) hipLaunchKernelGGL((narrow_scatter_kernel<N, DOT>), grid, dim3(kTokenThreads), 0, s, b);
+                else if (nt) hipLaunchKernelGGL((scatter_kernel<N, DOT, true>), grid, dim3(kTokenThreads), 0, s, b);
+                else hipLaunchKernelGGL((scatter_kernel<N, DOT, false>), grid, dim3(kTokenThreads), 0, s, b);
+            };
+            if (b.dw) go(std::true_type{});
+            else go(std::false_type{});
         });
+    });
+    return hipGetLastError();
+}
+
+hipError_t launch_collect_backward(const moe_dispatch_config& c, const uint16_t* dy, const uint16_t* rows, const int32_t* row_of, const float* topk_w, float p,
+                                   const void* rng, uint16_t* drows, float* d_topk_w, hipStream_t s) {
+    const Dropout drop = dropout_of(p, rng);
+    return launch_scatter(c, {dy, rows, drows, c.d, topk_w != nullptr || drop.rng != nullptr, drop}, row_of, topk_w, d_topk_w, s);
+}
+
+hipError_t launch_dispatch(const moe_dispatch_config& c, const uint16_t* x, const int32_t* topk_idx, const float* topk_w, int32_t* counts, int32_t* offsets,
+                           int32_t* row_of, int32_t* src_of, uint16_t* rows, int32_t* hist, hipStream_t s) {
+    DispatchArgs a{x, topk_idx, topk_w, counts, offsets, row_of, src_of, rows, nullptr, c.T, c.d, c.k, c.E, c.first, c.capacity, 1, chunks_of(c), false};
+    if ((long long)c.T * c.k > (rows ? kCountAllRows : kCountAll)) {
+        a.hist = hist;
+        a.summed = a.chunks > kSumInside;
+        hipLaunchKernelGGL(count_chunks_kernel, dim3(a.chunks), dim3(kTokenThreads), 0, s, a);
+        if (a.summed) hipLaunchKernelGGL(sum_chunks_kernel, dim3((c.E + kWave - 1) / kWave), dim3(kSumThreads), 0, s, a);
+    }
+    if (!rows || c.T == 0) {
+        hipLaunchKernelGGL(tables_kernel, dim3(a.chunks > 0 ? a.chunks : 1), dim3(kTableThreads), 0, s, a);
+        return hipGetLastError();
+    }
+    a.per = (c.T + 1023) / 1024;           // about a thousand workgroups, of a thousand slots at most
+    if (a.per > kMostSlots / c.k) a.per = kMostSlots / c.k;
+    const dim3 grid((unsigned)(((long long)c.T + a.per - 1) / a.per));
+    const bool nt = passes_caches(c);
+    by_slots(c.k, [&](auto n) {
+        constexpr int N = decltype(n)::value;
+        if (c.d <= kNarrow) hipLaunchKernelGGL((dispatch_kernel<1, false, true>), grid, dim3(kTokenThreads), 0, s, a);
+        else if (nt) hipLaunchKernelGGL((dispatch_kernel<N, true, false>), grid, dim3(kTokenThreads), 0, s, a);
+        else hipLaunchKernelGGL((dispatch_kernel<N, false, false>), grid, dim3(kTokenThreads), 0, s, a);
     });
     return hipGetLastError();
 }
