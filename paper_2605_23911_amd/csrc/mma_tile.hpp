@@ -99,25 +99,6 @@ struct Stream {
     }
 };
 
-// A stream every step of which is taken `times` times, `jump` bytes further along the rows each time: a product with several parts of an operand, during which the
-// other operand's panel stays in the caches.
-template <class From>
-struct Repeat {
-    From from;
-    uint32_t jump;
-    int times, at;
-    Panel panel;
-    __device__ static __forceinline__ Repeat make(From s, int times, uint32_t jump) { return Repeat{s, jump, times, 0, {0, 0}}; }
-    __device__ __forceinline__ Panel next() {
-        if (at == 0) panel = from.next();
-        Panel p = panel;
-        p.base += (uint64_t)jump * at;
-        p.range = panel.range ? panel.range - jump * at : 0;       // the range ends with the rows
-        at = at + 1 == times ? 0 : at + 1;
-        return p;
-    }
-};
-
 // Permutation of a row's chunks (k contiguous) or pieces, by the row's number in the panel.
 template <int MN, bool KC, int BK>
 __device__ __forceinline__ int swizzle(int r) {
@@ -186,14 +167,15 @@ struct Reader {
 };
 
 // BM x BN tile by WM x WN wavefronts, BK elements of k per step, a ring of STAGES steps.
-template <int BM_, int BN_, int WM_, int WN_, int BK_, int STAGES_, int PER_, int RATE_>
+// PARTS: A is a sum of so many parts, each with a panel of its own beside the one of B, whose fragments are read once for all of them.
+template <int BM_, int BN_, int WM_, int WN_, int BK_, int STAGES_, int PER_, int RATE_, int PARTS_ = 1>
 struct Shape {
-    static constexpr int PER = PER_, RATE = RATE_;
+    static constexpr int PER = PER_, RATE = RATE_, PARTS = PARTS_;
     static constexpr int SIMD_WAVES = PER_ * WM_ * WN_ / 4;
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = BK_, STAGES = STAGES_;
     static constexpr int WAVES = WM * WN, THREADS = WAVES * kWave;
     static constexpr int MB = BM / WM / 32, NB = BN / WN / 32;   // 32x32 blocks per wavefront
-    static constexpr int kBufA = BM * BK * 2, kBuf = (BM + BN) * BK * 2, kRing = STAGES * kBuf;
+    static constexpr int kBufA = BM * BK * 2, kBuf = (PARTS * BM + BN) * BK * 2, kRing = STAGES * kBuf;
     static constexpr int LD = BN + 4;                            // floats per staged row: 16 bytes more, which spreads the rows over the banks
     static constexpr int kPassRows = WM * 32;                    // rows staged at a time: one block of every wavefront row
     static constexpr int kStage = kPassRows * LD * 4;
@@ -218,6 +200,10 @@ typedef Shape<256, 128, 4, 2, 64, 3, 1, 75> Tall;
 // Streaming weights past few rows: three (two) workgroups per CU, 96 (64) KiB under way.
 typedef Shape<64, 64, 2, 2, 64, 3, 3, 60> Flat;
 typedef Shape<128, 128, 2, 4, 64, 2, 2, 60> Half;
+
+// The same with a first operand of several parts: two long steps instead of three short ones.
+template <class S, int PARTS, int STAGES>
+using Parted = Shape<S::BM, S::BN, S::WM, S::WN, S::BK, STAGES, S::PER, S::RATE, PARTS>;
 
 // A wavefront's results: MB blocks of 32 rows (up to the shape's: a tile of few rows takes a body with fewer), NB of 32 columns.
 template <class S, int MB>
@@ -251,11 +237,12 @@ __device__ __forceinline__ void by_height(int rows, F&& body) {
 // queue up for longer than a slot takes, and the multiplications behind them wait.  A step's barrier stands in front of its last slot, whose
 // multiplications cover the first reads of the next step.
 // Ends with every wavefront past its last LDS read and nothing on its way into LDS.
-// a, b: the operands' streams (Stream, or Repeat of one).
-template <class S, int MB, bool AKC, bool BKC, class StreamA, class StreamB>
-__device__ __forceinline__ void multiply(f32x16 (&acc)[S::NB][MB], StreamA a, StreamB b, const typename S::template LoadA<AKC>& la,
-                                         const typename S::template LoadB<BKC>& lb, int steps, char* lds) {
-    constexpr int SLOTS = S::BK / 16, NA = S::template LoadA<AKC>::N, LOADS = NA + S::template LoadB<BKC>::N;     // loads per step and wavefront
+// With several parts of A a slot is 16 of k of one part; the parts' panels lie `jump` bytes apart along A's rows.
+template <class S, int MB, bool AKC, bool BKC>
+__device__ __forceinline__ void multiply(f32x16 (&acc)[S::NB][MB], Stream<AKC, S::BK> a, Stream<BKC, S::BK> b, const typename S::template LoadA<AKC>& la,
+                                         const typename S::template LoadB<BKC>& lb, int steps, char* lds, uint32_t jump = 0) {
+    constexpr int PARTS = S::PARTS, SLOTS = S::BK / 16 * PARTS, NA = S::template LoadA<AKC>::N, LOADS = PARTS * NA + S::template LoadB<BKC>::N;     // loads per step and wavefront
+    static_assert(S::BK / 16 % 2 == 0, "the fragments' two sets alternate over the steps");
     constexpr int READS = MB + S::NB, MFMAS = MB * S::NB, PER = (READS + MFMAS - 1) / MFMAS;
     // loads that go with the last slot (of the step after next), the rest with the first slots of the next step
     constexpr int SPREAD = S::STAGES > 2 ? SLOTS : SLOTS - 1;    // slots that loads are spread over
@@ -268,21 +255,27 @@ __device__ __forceinline__ void multiply(f32x16 (&acc)[S::NB][MB], StreamA a, St
     rb.init(wn * S::NB * 32, lane);
     const uint32_t at = (uint32_t)(uintptr_t)lds;
     bf16x8 fa[2][MB], fb[2][S::NB];
-    i32x4 da, db;                                                // the step that is being loaded: descriptors, and where it goes
+    i32x4 da[PARTS], db;                                         // the step that is being loaded: descriptors, and where it goes
     uint32_t to = 0;
     auto begin = [&](uint32_t where) {
-        da = a.next().desc();
+        const Panel pa = a.next();
+#pragma unroll
+        for (int h = 0; h < PARTS; ++h) da[h] = Panel{pa.base + (uint64_t)h * jump, pa.range ? pa.range - h * jump : 0}.desc();   // the range ends with the rows
         db = b.next().desc();
         to = at + where;
     };
     auto load = [&](auto piece) {
         constexpr int p = decltype(piece)::value;
-        if constexpr (p < NA) la.template one<p>(da, to, wave);
-        else if constexpr (p < LOADS) lb.template one<p - NA>(db, to + S::kBufA, wave);
+        if constexpr (p < PARTS * NA) la.template one<p % NA>(da[p / NA], to + p / NA * S::kBufA, wave);
+        else if constexpr (p < LOADS) lb.template one<p - PARTS * NA>(db, to + PARTS * S::kBufA, wave);
     };
-    auto read = [&](uint32_t from, int s, int set, int which) {
-        if (which < S::NB) fb[set][which] = rb.read(lds + from + S::kBufA, which, s);
-        else if (which < READS) fa[set][which - S::NB] = ra.read(lds + from, which - S::NB, s);
+    auto read = [&](uint32_t from, int slot, int which) {
+        const int s = slot / PARTS, h = slot % PARTS;
+        if (which < S::NB) {
+            if (h == 0) fb[s & 1][which] = rb.read(lds + from + PARTS * S::kBufA, which, s);
+        } else if (which < READS) {
+            fa[slot & 1][which - S::NB] = ra.read(lds + from + h * S::kBufA, which - S::NB, s);
+        }
     };
     if (steps <= 0) return;
     // Steps 0 .. STAGES - 2 whole, and of the next one what the last slot of a step loads.
@@ -298,7 +291,7 @@ __device__ __forceinline__ void multiply(f32x16 (&acc)[S::NB][MB], StreamA a, St
     begin((S::STAGES - 1) * S::kBuf);
     static_for<EACH>(load);
 #pragma unroll
-    for (int w = 0; w < READS; ++w) read(0, 0, 0, w);
+    for (int w = 0; w < READS; ++w) read(0, 0, w);
     uint32_t buf = 0;                                            // byte offset of the step that is read
     for (int i = 0; i < steps; ++i) {
         const uint32_t next = buf + S::kBuf == S::kRing ? 0 : buf + S::kBuf;
@@ -314,8 +307,8 @@ __device__ __forceinline__ void multiply(f32x16 (&acc)[S::NB][MB], StreamA a, St
             static_for<MFMAS>([&](auto mfma) {
                 constexpr int j = decltype(mfma)::value, m = j / S::NB, n = j % S::NB;
 #pragma unroll
-                for (int q = 0; q < PER; ++q) read(last ? next : buf, last ? 0 : s + 1, (s + 1) & 1, j * PER + q);
-                acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[s & 1][n], fa[s & 1][m], acc[n][m], 0, 0, 0);
+                for (int q = 0; q < PER; ++q) read(last ? next : buf, last ? 0 : s + 1, j * PER + q);
+                acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[s / PARTS & 1][n], fa[s & 1][m], acc[n][m], 0, 0, 0);
                 if constexpr (j < EACH) load(std::integral_constant<int, first + j>{});
                 if constexpr (j + 1 == MFMAS) static_for<(EACH > MFMAS ? EACH - MFMAS : 0)>([&](auto more) { load(std::integral_constant<int, first + MFMAS + decltype(more)::value>{}); });
                 __builtin_amdgcn_sched_barrier(0);

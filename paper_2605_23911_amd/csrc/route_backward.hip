@@ -12,6 +12,10 @@ namespace moe {
 
 namespace {
 
+// Tiles of the two products: of many tokens, and of up to 64.
+typedef Pair Many;
+typedef Shape<64, 64, 2, 2, 64, 2, 2, 60> Few;
+
 struct RouteArgs {
     const uint16_t *x, *wr;
     const float* bias;
@@ -220,8 +224,8 @@ __device__ __forceinline__ void dx_tile(const RouteArgs& a, int m0, int n0, char
         constexpr int MB = decltype(height)::value;
         Acc<S, MB> acc;
         clear<S, MB>(acc);
-        multiply<S, MB, true, false>(acc, Repeat<Stream<true, S::BK>>::make(Stream<true, S::BK>::make(a.dz + (size_t)m0 * ld, ld, rows, a.Ep), 2, (uint32_t)a.Ep * 2),
-                                     Repeat<Stream<false, S::BK>>::make(Stream<false, S::BK>::make(a.wr, a.d, n0, a.E), 2, 0), la, lb, a.Ep / S::BK * 2, lds);
+        multiply<S, MB, true, false>(acc, Stream<true, S::BK>::make(a.dz + (size_t)m0 * ld, ld, rows, a.Ep), Stream<false, S::BK>::make(a.wr, a.d, n0, a.E), la, lb,
+                                     a.Ep / S::BK, lds, (uint32_t)a.Ep * 2);
         by_rows_bf16<S, MB>(acc, lds, [&](int r, int c, u32x4_t v) {
             if (r < rows && n0 + c * 8 < a.d) *reinterpret_cast<u32x4_t*>(a.dx + (size_t)(m0 + r) * a.d + n0 + c * 8) = v;
         });
@@ -286,9 +290,8 @@ __device__ __forceinline__ void dw_tile(const RouteArgs& a, int piece, int m0, i
         constexpr int MB = decltype(height)::value;
         Acc<S, MB> acc;
         clear<S, MB>(acc);
-        using From = Stream<false, S::BK>;
-        multiply<S, MB, false, false>(acc, Repeat<From>::make(From::make(a.dz + (size_t)t0 * ld, ld, m0, tokens), a.parts, (uint32_t)a.Ep * 2),
-                                      Repeat<From>::make(From::make(a.x + (size_t)t0 * a.d, a.d, n0, tokens), a.parts, 0), la, lb, a.parts * (s1 - s0), lds);
+        multiply<S, MB, false, false>(acc, Stream<false, S::BK>::make(a.dz + (size_t)t0 * ld, ld, m0, tokens), Stream<false, S::BK>::make(a.x + (size_t)t0 * a.d, a.d, n0, tokens),
+                                      la, lb, s1 - s0, lds, (uint32_t)a.Ep * 2);
         by_rows<S, S::BN / 8>(acc, lds, AheadNothing{}, [&](int r, int c, const float* row, Nothing) {
             if (m0 + r >= a.E || n0 + c * 8 >= a.d) return;
             const size_t at = (size_t)(m0 + r) * a.d + n0 + c * 8;
@@ -306,23 +309,26 @@ __device__ __forceinline__ void dw_tile(const RouteArgs& a, int piece, int m0, i
 
 // Both products in one launch, and dbias.  The tiles of dW_r, which are several times as long, come first: one per CU at most (weight_pieces_of), whose other workgroup
 // takes tiles of dx.
-template <class S>
+template <class S, int PARTS>
 __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void route_products_kernel(RouteArgs a) {
-    __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
+    using Weights = Parted<S, PARTS, 2>;
+    using Rows = Parted<S, 2, 2>;
+    __shared__ __attribute__((aligned(1024))) char lds[Weights::kLds];
+    static_assert(Weights::kLds >= Rows::kLds, "room for both");
     const int cols = (a.d + S::BN - 1) / S::BN, heads = (a.E + S::BM - 1) / S::BM, blocks = (a.T + S::BM - 1) / S::BM;
     const int weights = a.dwr ? a.weight_pieces * cols * heads : 0, rows = a.dx ? blocks * cols : 0, ids_w = (weights + 7) / 8 * 8, ids_r = (rows + 7) / 8 * 8;
     const int id = blockIdx.x;
     if (id >= ids_w + ids_r) return bias_group<S::THREADS>(a, id - ids_w - ids_r, reinterpret_cast<float(*)[kBiasExperts]>(lds));
     if (id < ids_w) {
         const int t = xcd_tile(id, weights);
-        if (t >= 0) dw_tile<S>(a, t / (cols * heads), t % heads * S::BM, t / heads % cols * S::BN, lds);
+        if (t >= 0) dw_tile<Weights>(a, t / (cols * heads), t % heads * S::BM, t / heads % cols * S::BN, lds);
         return;
     }
     const int t = xcd_tile(id - ids_w, rows);
     if (t < 0) return;
     int m, n;
     patch(t, blocks, cols, m, n);
-    dx_tile<S>(a, m * S::BM, n * S::BN, lds);
+    dx_tile<Rows>(a, m * S::BM, n * S::BN, lds);
 }
 
 // The pieces of dW_r, eight elements per thread, in their order.
@@ -347,9 +353,9 @@ __global__ __launch_bounds__(256) void route_bias_kernel(RouteArgs a) {
     bias_group<256>(a, blockIdx.x, part);
 }
 
-bool few_tokens(const moe_config& c) { return c.T <= Flat::BM; }
+bool few_tokens(const moe_config& c) { return c.T <= Few::BM; }
 // Experts rounded up to whole steps of the products' reduction.
-int padded(const moe_config& c) { return few_tokens(c) ? (c.E + Flat::BK - 1) / Flat::BK * Flat::BK : (c.E + Pair::BK - 1) / Pair::BK * Pair::BK; }
+int padded(const moe_config& c) { return few_tokens(c) ? (c.E + Few::BK - 1) / Few::BK * Few::BK : (c.E + Many::BK - 1) / Many::BK * Many::BK; }
 bool few_experts(const moe_config& c) { return c.E <= Flat::BM; }
 
 template <class S>
@@ -373,7 +379,7 @@ int weight_pieces_of(const moe_config& c) {
     if (n > most) n = most;
     return n < 1 ? 1 : (int)n;
 }
-int weight_pieces(const moe_config& c) { return few_tokens(c) ? weight_pieces_of<Flat>(c) : weight_pieces_of<Pair>(c); }
+int weight_pieces(const moe_config& c) { return few_tokens(c) ? weight_pieces_of<Few>(c) : weight_pieces_of<Many>(c); }
 int dz_blocks(const moe_config& c) {
     const int n = (c.T + kDzWaves - 1) / kDzWaves;
     return n < 1024 ? n : 1024;
@@ -403,7 +409,9 @@ void go_logits(const RouteArgs& a, hipStream_t s) {
 template <class S>
 void go_products(const RouteArgs& a, hipStream_t s) {
     const long long cols = (a.d + S::BN - 1) / S::BN, weights = a.dwr ? a.weight_pieces * cols * ((a.E + S::BM - 1) / S::BM) : 0, rows = a.dx ? cols * ((a.T + S::BM - 1) / S::BM) : 0;
-    hipLaunchKernelGGL(route_products_kernel<S>, dim3(xcd_grid(weights) + xcd_grid(rows) + bias_groups(a)), dim3(S::THREADS), 0, s, a);
+    const dim3 grid(xcd_grid(weights) + xcd_grid(rows) + bias_groups(a));
+    if (a.parts == 3) hipLaunchKernelGGL((route_products_kernel<S, 3>), grid, dim3(S::THREADS), 0, s, a);
+    else hipLaunchKernelGGL((route_products_kernel<S, 2>), grid, dim3(S::THREADS), 0, s, a);
 }
 
 }  // namespace
@@ -431,8 +439,8 @@ hipError_t launch_route_backward(const moe_config& c, const RouteGrad& p, hipStr
     else if (a.Ep <= 2 * kWave) hipLaunchKernelGGL(route_dz_kernel<2>, dim3(a.dz_blocks), dim3(kDzThreads), 0, s, a);
     else hipLaunchKernelGGL(route_dz_kernel<4>, dim3(a.dz_blocks), dim3(kDzThreads), 0, s, a);
     if (!p.dx && !p.dwr) hipLaunchKernelGGL(route_bias_kernel, dim3(bias_groups(a)), dim3(256), 0, s, a);
-    else if (few_tokens(c)) go_products<Flat>(a, s);
-    else go_products<Pair>(a, s);
+    else if (few_tokens(c)) go_products<Few>(a, s);
+    else go_products<Many>(a, s);
     if (p.dwr && a.weight_pieces > 1) hipLaunchKernelGGL(route_join_kernel, dim3(joins), dim3(256), 0, s, a);
     return hipGetLastError();
 }
