@@ -330,6 +330,7 @@ def moe_forward_staged(cfg, x, W_r, bias, W_gate, W_up, W_down, y, workspace, ev
 
 # The handle of a GPU's current stream, without the Stream object that torch.cuda.current_stream() makes around it (1.1 us, a seventh of a small call).
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 class _Call:
@@ -375,7 +376,7 @@ class _Call:
             raise ValueError(f"{where}: the stream is on cuda:{s.device_index}, the tensors on cuda:{self.index}")
         else:
             handle = s.cuda_stream
-        if torch.cuda.current_device() == self.index:
+        if _current_device() == self.index:
             status = fn(*args, handle)
         else:
             with torch.cuda.device(self.index):

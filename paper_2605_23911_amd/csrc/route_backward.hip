@@ -12,8 +12,10 @@ namespace moe {
 
 namespace {
 
-// Tiles of the two products: of many tokens, and of up to 64.
+// Tiles of the two products: of many tokens, of up to 2048, and of up to 64.  Mid has half of Many's area and three workgroups per CU: kernels of a call, us, Many / Mid:
+// 256 experts of 7168, 512 tokens 43.8 / 38.2, 2048 74.4 / 70.6, 4096 107 / 113; 64 of 3584, 1999 tokens 24.1 / 23.4, 4096 30.5 / 32.1; 8 of 4096, 512 18.8 / 18.1, 8192 52.6 / 59.9.
 typedef Pair Many;
+typedef Shape<128, 128, 2, 2, 32, 2, 3, 60> Mid;
 typedef Shape<64, 64, 2, 2, 64, 2, 2, 60> Few;
 
 struct RouteArgs {
@@ -310,7 +312,9 @@ __device__ __forceinline__ void dw_tile(const RouteArgs& a, int piece, int m0, i
 // Both products in one launch, and dbias.  The tiles of dW_r, which are several times as long, come first: one per CU at most (weight_pieces_of), whose other workgroup
 // takes tiles of dx.
 template <class S, int PARTS>
-__global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void route_products_kernel(RouteArgs a) {
+constexpr int products_per_cu() { return 160 * 1024 / Parted<S, PARTS, 2>::kLds < S::PER ? 160 * 1024 / Parted<S, PARTS, 2>::kLds : S::PER; }
+template <class S, int PARTS>
+__global__ __launch_bounds__(S::THREADS, (products_per_cu<S, PARTS>() * S::WAVES / 4)) void route_products_kernel(RouteArgs a) {
     using Weights = Parted<S, PARTS, 2>;
     using Rows = Parted<S, 2, 2>;
     __shared__ __attribute__((aligned(1024))) char lds[Weights::kLds];
@@ -355,6 +359,7 @@ __global__ __launch_bounds__(256) void route_bias_kernel(RouteArgs a) {
 
 bool few_tokens(const moe_config& c) { return c.T <= Few::BM; }
 // Experts rounded up to whole steps of the products' reduction.
+static_assert(Mid::BK == Many::BK, "one padding");
 int padded(const moe_config& c) { return few_tokens(c) ? (c.E + Few::BK - 1) / Few::BK * Few::BK : (c.E + Many::BK - 1) / Many::BK * Many::BK; }
 bool few_experts(const moe_config& c) { return c.E <= Flat::BM; }
 
@@ -379,7 +384,8 @@ int weight_pieces_of(const moe_config& c) {
     if (n > most) n = most;
     return n < 1 ? 1 : (int)n;
 }
-int weight_pieces(const moe_config& c) { return few_tokens(c) ? weight_pieces_of<Few>(c) : weight_pieces_of<Many>(c); }
+bool mid_tokens(const moe_config& c) { return c.T <= 2048; }
+int weight_pieces(const moe_config& c) { return few_tokens(c) ? weight_pieces_of<Few>(c) : mid_tokens(c) ? weight_pieces_of<Mid>(c) : weight_pieces_of<Many>(c); }
 int dz_blocks(const moe_config& c) {
     const int n = (c.T + kDzWaves - 1) / kDzWaves;
     return n < 1024 ? n : 1024;
@@ -440,6 +446,7 @@ hipError_t launch_route_backward(const moe_config& c, const RouteGrad& p, hipStr
     else hipLaunchKernelGGL(route_dz_kernel<4>, dim3(a.dz_blocks), dim3(kDzThreads), 0, s, a);
     if (!p.dx && !p.dwr) hipLaunchKernelGGL(route_bias_kernel, dim3(bias_groups(a)), dim3(256), 0, s, a);
     else if (few_tokens(c)) go_products<Few>(a, s);
+    else if (mid_tokens(c)) go_products<Mid>(a, s);
     else go_products<Many>(a, s);
     if (p.dwr && a.weight_pieces > 1) hipLaunchKernelGGL(route_join_kernel, dim3(joins), dim3(256), 0, s, a);
     return hipGetLastError();

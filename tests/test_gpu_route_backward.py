@@ -98,7 +98,7 @@ class Case:
 
 
 SHAPES = [(1, 64, 1, 1), (1, 4096, 8, 2), (3, 128, 2, 2), (17, 256, 7, 3), (64, 512, 64, 8), (65, 320, 65, 8), (130, 192, 128, 5), (257, 576, 60, 8), (100, 1024, 256, 8),
-          (700, 640, 200, 12), (1999, 128, 16, 4), (515, 1216, 129, 2), (63, 64, 256, 256), (5000, 64, 33, 6)]
+          (700, 640, 200, 12), (1999, 128, 16, 4), (515, 1216, 129, 2), (63, 64, 256, 256), (5000, 64, 33, 6), (64, 64, 40, 2), (2048, 64, 40, 3), (2049, 192, 70, 4), (4100, 320, 256, 8)]
 
 
 @pytest.mark.parametrize("gating", [orc.SOFTMAX, orc.RENORM, orc.SIGMOID])
@@ -110,9 +110,10 @@ def test_values(moe, shape, gating):
     c.check(c.run(moe, f32=False), f32=False)
 
 
-@pytest.mark.parametrize("gating", [orc.SOFTMAX, orc.RENORM, orc.SIGMOID])
-def test_what_is_not_wanted_and_what_is_added_to(moe, gating):
-    c = Case(150, 256, 20, 4, gating, whole=True)
+@pytest.mark.parametrize("T,gating", [(40, orc.SOFTMAX), (150, orc.RENORM), (900, orc.SIGMOID), (2500, orc.SOFTMAX)])
+def test_what_is_not_wanted_and_what_is_added_to(moe, T, gating):
+    """dW_r in one piece and in several, that a last launch joins."""
+    c = Case(T, 256, 20, 4, gating, whole=True)
     whole = c.run(moe)
     c.check(whole)
     for want in (("dx",), ("dwr",), ("dbias",), ("dx", "dbias"), ("dwr", "dbias")):
