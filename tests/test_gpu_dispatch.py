@@ -257,6 +257,14 @@ def test_widths(moe, k, d):
     p.check_collect_backward(True, 0.1)
 
 
+def test_the_widest_rows(moe):
+    p = Plan(moe, 3, 1 << 20, 2, 4, 3, 1)
+    p.check_dispatch(True)
+    p.check_collect(True, True, 0.0, "dispatch_backward")
+    p.check_collect(True, True, 0.0)
+    p.check_collect_backward(True, 0.0)
+
+
 def test_in_place_on_the_residual_and_the_base(moe):
     p = Plan(moe, 33, 264, 3, 8, 6, 1)
     for call in ("collect", "backward"):

@@ -163,6 +163,28 @@ def test_no_tokens(moe):
     assert torch.equal(o["dwr"], held[0]) and torch.equal(o["dbias"], held[1])
 
 
+@pytest.mark.parametrize("gating", [orc.SOFTMAX, orc.RENORM, orc.SIGMOID])
+def test_the_widest_rows(moe, gating):
+    c = Case(3, 1 << 20, 5, 2, gating, whole=True)
+    c.check(c.run(moe))
+
+
+def test_nan_in_one_channel(moe):
+    """Without logits in between a NaN of x reaches its column of dW_r and nothing else; neighbours of the router's rows in memory are not read."""
+    c = Case(77, 192, 9, 2, orc.RENORM, whole=True)
+    good = c.run(moe)
+    wide = torch.full((c.wr.shape[0] + 128, 192), NAN, dtype=torch.bfloat16, device="cuda")
+    wide[:9] = c.wr.cuda()
+    c.x[5, 17] = NAN
+    cfg = moe.MoEConfig.of(77, 192, 64, 9, 2, orc.RENORM)
+    dx, dwr, dbias = full((77, 192)), full((9, 192), torch.float32), full((9,), torch.float32)
+    moe.moe_route_backward(cfg, c.x.cuda(), wide[:9], None, *(torch.from_numpy(v).cuda() for v in (c.idx, c.w, c.g)), dx, dwr, dbias,
+                           full((moe.route_backward_workspace_size(cfg),), torch.uint8, 255))
+    assert torch.equal(dx, good["dx"]) and torch.equal(dbias, good["dbias"]) and torch.isnan(dwr[:, 17]).all()
+    rest = torch.arange(192) != 17
+    assert torch.equal(dwr[:, rest], good["dwr"][:, rest])
+
+
 def test_the_same_every_time(moe):
     c = Case(900, 512, 96, 6, orc.SOFTMAX)
     a, b = c.run(moe), c.run(moe)

@@ -97,3 +97,39 @@ def test_dropout_beyond_32_bits(moe):
     block = n // 8                                                       # the last, partial block
     words = orc.philox((3, 0), (block & 0xFFFFFFFF, block >> 32, 4, 0))
     assert y[block * 8:].tolist() == [2.0 if (words[j // 2] >> 16 * (j % 2) & 0xFFFF) >= 32768 else 0.0 for j in range(n % 8)]
+
+
+def test_router_of_many_tokens(moe):
+    """dz of more than 4 GiB.  x and W_r are whole numbers over powers of two, so logits are exact; dW_r is a sum of a hundred and more pieces of up to 2^15 tokens each: off by
+    at most (2^15 + 2^8) 2^-24 of the sum of absolute values."""
+    T, d, E, k = 3_000_000, 64, 256, 2
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randint(-2, 3, (T, d), generator=gen, device="cuda").bfloat16()
+    wr = (torch.randint(-4, 5, (E, d), generator=gen, device="cuda") / 32).bfloat16()
+    g = torch.randn((T, k), generator=gen, device="cuda")
+    cfg = moe.MoEConfig.of(T, d, 64, E, k)
+    idx, w = torch.empty((T, k), dtype=torch.int32, device="cuda"), torch.empty((T, k), device="cuda")
+    for a in range(0, T, 1 << 18):
+        b = min(a + (1 << 18), T)
+        top = torch.topk(torch.softmax(x[a:b].double() @ wr.double().T, 1), k, dim=1)
+        idx[a:b], w[a:b] = top.indices.int(), top.values.float()
+    size = moe.route_backward_workspace_size(cfg)
+    assert T * 3 * E * 2 > 1 << 32 and size > T * 3 * E * 2
+    dx, dwr, dbias = torch.empty_like(x), torch.empty((E, d), device="cuda"), torch.empty(E, device="cuda")
+    moe.moe_route_backward(cfg, x, wr, None, idx, w, g, dx, dwr, dbias, torch.empty(size, dtype=torch.uint8, device="cuda"))
+    want_w, size_w = torch.zeros((E, d), dtype=torch.float64, device="cuda"), torch.zeros((E, d), dtype=torch.float64, device="cuda")
+    want_b, size_b = torch.zeros(E, dtype=torch.float64, device="cuda"), torch.zeros(E, dtype=torch.float64, device="cuda")
+    for a in range(0, T, 1 << 18):
+        b = min(a + (1 << 18), T)
+        xx, p = x[a:b].double(), torch.softmax(x[a:b].double() @ wr.double().T, 1)
+        G = torch.zeros_like(p).scatter_add_(1, idx[a:b].long(), g[a:b].double())
+        dz = p * (G - (p * G).sum(1, keepdim=True))
+        off = p * (24 * 2.0**-24) * (G.abs() + 2 * (p * G.abs()).sum(1, keepdim=True))
+        ref = dz @ wr.double()
+        bound = (off + 2.0**-16 * dz.abs() + 2 * E * 2.0**-24 * dz.abs()) @ wr.double().abs() + 2.0**-8 * ref.abs()
+        assert ((dx[a:b].double() - ref).abs() <= bound * (1 + 2.0**-8)).all(), a
+        want_w += dz.T @ xx
+        size_w += (dz.abs() * (2**15 + 2**8) * 2.0**-24 + off).T @ xx.abs()
+        want_b += dz.sum(0)
+        size_b += (dz.abs() * (2**13) * 2.0**-24 + off).sum(0)           # 4096 wavefronts' sums of 733 tokens, then their sum
+    assert ((dwr.double() - want_w).abs() <= size_w).all() and ((dbias.double() - want_b).abs() <= size_b).all()

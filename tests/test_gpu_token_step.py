@@ -233,6 +233,40 @@ def test_a_share_of_every_gpu_adds_up_to_the_whole(moe):
     assert float((total.double() - whole.y.double()).norm()) <= 4 * B * size
 
 
+@pytest.mark.parametrize("T", [1, 24, 300])
+@pytest.mark.parametrize("packed", [True, False])
+def test_serving_a_share_of_the_experts(moe, T, packed):
+    """The inference block over the rows that a share of the experts has (fewer than T k, for some tokens none), and the way back onto the residual stream: for each token the
+    paper's sum over the experts that are here (h, y_perm and y are rounded once each)."""
+    s = mi.MoEShape("serve", T, 256, 320, 8, 3)
+    E, first = 3, 4
+    x, wr = mi.make_x(s).cuda(), mi.make_router(s).cuda()
+    w = [t[first:first + E].contiguous().cuda() for t in mi.make_all_experts(s)]
+    route, disp, ffn = moe.MoEConfig.of(T, s.d, s.F, s.E, s.k), moe.DispatchConfig.of(T, s.d, s.k, E, first), moe.MoEConfig.of(T * s.k, s.d, s.F, E, 1)
+    i32, f32 = torch.int32, torch.float32
+    idx, tw, counts, off, row, src = _gpu((T, s.k), i32), _gpu((T, s.k), f32), _gpu(E, i32), _gpu(E + 1, i32), _gpu((T, s.k), i32), _gpu(T * s.k, i32)
+    rows, h, yp, y = _gpu((T * s.k, s.d)), _gpu((T * s.k, s.F)), _gpu((T * s.k, s.d)).fill_(float("nan")), _gpu((T, s.d))
+    ws = _gpu(max(moe.route_workspace_size(route), moe.dispatch_workspace_size(disp), moe.ffn_workspace_size(ffn)), torch.uint8)
+    W = None
+    if packed:
+        W = _gpu(moe.packed_weights_size(ffn), torch.uint8)
+        moe.moe_pack_weights(ffn, *w, W)
+    moe.moe_route(route, x, wr, None, idx, tw, ws)
+    moe.moe_dispatch(disp, x, idx, None, counts, off, row, src, rows, ws)
+    moe.moe_grouped_ffn(ffn, rows, off, *((None,) * 3 if packed else w), h, yp, ws, W_packed=W)
+    moe.moe_collect(disp, yp, row, tw, y, residual=x)
+    torch.cuda.synchronize()
+    xx, ii, want = x.cpu().double(), idx.cpu(), x.cpu().double()
+    for e in range(E):
+        t, i = torch.nonzero(ii == first + e, as_tuple=True)
+        g, u, d = (m[e].cpu().double() for m in w)
+        f = (torch.nn.functional.silu(xx[t] @ g.T) * (xx[t] @ u.T)) @ d.T
+        want = want.index_add(0, t, tw.cpu().double()[t, i][:, None] * f)
+    _near(y, want, 3, "y")
+    none = ~((ii >= first) & (ii < first + E)).any(1)
+    assert torch.equal(y.cpu()[none], x.cpu()[none])
+
+
 def test_calls_that_are_refused_leave_their_results_alone(moe):
     st = Step(moe, *STEPS[1])
     st.run()
