@@ -102,6 +102,7 @@ __global__ __launch_bounds__(kSumThreads) void sum_chunks_kernel(DispatchArgs a)
 }
 
 // in[t] (after dropout, where there is any) times a slot's weight into its row.  Slots i0 .. of the token; DOT: and <in[t], row of `with`>.
+// PAST: the rows pass the caches by, 1: those written, 2: those read, too.
 struct ScatterArgs {
     const uint16_t* in;
     const uint16_t* with;
@@ -110,7 +111,7 @@ struct ScatterArgs {
     bool scaled;              // false: rows are copies
     Dropout p;
 };
-template <int N, bool DOT, bool NT>
+template <int N, bool DOT, int PAST>
 __device__ __forceinline__ void scatter_slots(const ScatterArgs& a, const Slots<N>& s, int t, int lane, int threads, uint64_t seed, uint64_t offset, float (&dot)[N]) {
     const Row in = row_at(a.in, (size_t)t * a.d * 2, s.any, a.d * 2);
     Row out[N], with[N];
@@ -125,7 +126,7 @@ __device__ __forceinline__ void scatter_slots(const ScatterArgs& a, const Slots<
         u32x4_t other[N];
         if constexpr (DOT) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) other[i] = read8<NT>(with[i], c * 2);
+            for (int i = 0; i < N; ++i) other[i] = read8<PAST == 2>(with[i], c * 2);
         }
         float v[8];
         floats8(raw, v);
@@ -141,7 +142,7 @@ __device__ __forceinline__ void scatter_slots(const ScatterArgs& a, const Slots<
             float o[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) o[j] = s.w[i] * v[j];
-            write8<NT>(a.scaled ? bf16s8(o) : raw, out[i], c * 2);
+            write8<PAST >= 1>(a.scaled ? bf16s8(o) : raw, out[i], c * 2);
         }
     }
 }
@@ -299,7 +300,7 @@ __global__ __launch_bounds__(kTokenThreads) void dispatch_kernel(DispatchArgs a)
                 Slots<N> s;
                 s.load(row + t * a.k, a.w ? a.w + (size_t)(first + t) * a.k : nullptr, i0, a.k, R);
                 float dot[N];
-                scatter_slots<N, false, NT>(to, s, first + t, whole ? tid : lane, whole ? kTokenThreads : kWave, 0, 0, dot);
+                scatter_slots<N, false, NT ? 1 : 0>(to, s, first + t, whole ? tid : lane, whole ? kTokenThreads : kWave, 0, 0, dot);
             }
         }
     }
@@ -402,7 +403,7 @@ __global__ __launch_bounds__(kTokenThreads) void gather_kernel(CollectArgs a) {
     }
 }
 
-template <int N, bool DOT, bool NT>
+template <int N, bool DOT, int PAST>
 __global__ __launch_bounds__(kTokenThreads) void scatter_kernel(CollectArgs a) {
     __shared__ float part[kTokenWaves][8];
     const int t = my_token(a);
@@ -413,7 +414,7 @@ __global__ __launch_bounds__(kTokenThreads) void scatter_kernel(CollectArgs a) {
         Slots<N> s;
         s.load(a.row_of + (size_t)t * a.k, a.w ? a.w + (size_t)t * a.k : nullptr, i0, a.k, (long long)a.T * a.k);
         float dot[N];
-        scatter_slots<N, DOT, NT>(a.to, s, t, lane, threads, seed, offset, dot);
+        scatter_slots<N, DOT, PAST>(a.to, s, t, lane, threads, seed, offset, dot);
         if constexpr (DOT) store_dots<N>(dot, s, part, a.whole, a.k - i0 < N ? a.k - i0 : N, a.dw + (size_t)t * a.k + i0);
     }
 }
@@ -559,19 +560,30 @@ constexpr int kSumInside = 64;            // chunks up to which a workgroup adds
 
 int chunks_of(const moe_dispatch_config& c) { return (int)(((long long)c.T * c.k + kChunk - 1) / kChunk); }
 
-// From 128 MiB of rows on, half of the Infinity Cache, they pass the caches by.  Below, what is written is read next: 112 MiB of rows, us, cached / past the caches, the
-// gradient of collect alone 55.5 / 43.7 and with a collect of its rows 74.2 / 80.9, dispatch 31.5 / 31.6 and 58.8 / 58.0; 64 MiB 29.1 / 25.9 and 42.6 / 45.3,
-// 21.1 / 22.5 and 34.8 / 38.8.  Above: 448 MiB, the gradient 217 / 205, collect 120 / 99, dispatch 105 / 85.
+// From 128 MiB of rows on, half of the Infinity Cache, they pass the caches by: 448 MiB, us, cached / past the caches, collect 120 / 99, its gradient 217 / 205, dispatch 105 / 85.
+// Below, dispatch's rows are read next: 94 MiB 28.5 / 30.1 alone, 64 MiB 34.8 / 38.8 with a collect of them.
 bool passes_caches(const moe_dispatch_config& c) { return (long long)c.T * c.k * c.d >= (1ll << 26); }
+// The gradient of collect, which reads as much as it writes, writes past them from 64 MiB on: 94 MiB 42 / 35.5 us alone.  In a step, where its rows are not in the caches, it
+// takes longer and the block's gradient behind it less: together 304 / 303.5, 82 MiB 397 / 393, 109 MiB 515 / 507.
+int passes_caches_gradient(const moe_dispatch_config& c) {
+    const long long n = (long long)c.T * c.k * c.d;
+    return n >= (1ll << 26) ? 2 : n >= (1ll << 25) ? 1 : 0;
+}
 
-// go(integral_constant<slots per batch>)
+// go(integral_constant<slots per batch>): as many as a token has, up to eight.  Batches of 4 and 8 with empty rows cost 1-3 % at 3, 5, 6 and 7 slots.
 template <class F>
 void by_slots(int k, F&& go) {
     using std::integral_constant;
-    if (k == 1) go(integral_constant<int, 1>{});
-    else if (k == 2) go(integral_constant<int, 2>{});
-    else if (k <= 4) go(integral_constant<int, 4>{});
-    else go(integral_constant<int, 8>{});
+    switch (k) {
+        case 1: go(integral_constant<int, 1>{}); break;
+        case 2: go(integral_constant<int, 2>{}); break;
+        case 3: go(integral_constant<int, 3>{}); break;
+        case 4: go(integral_constant<int, 4>{}); break;
+        case 5: go(integral_constant<int, 5>{}); break;
+        case 6: go(integral_constant<int, 6>{}); break;
+        case 7: go(integral_constant<int, 7>{}); break;
+        default: go(integral_constant<int, 8>{});
+    }
 }
 
 // Tokens of one launch: it has less than 2^32 threads.
@@ -639,15 +651,16 @@ hipError_t launch_collect(const moe_dispatch_config& c, const uint16_t* rows, co
 
 static hipError_t launch_scatter(const moe_dispatch_config& c, const ScatterArgs& to, const int32_t* row_of, const float* topk_w, float* d_topk_w, hipStream_t s) {
     const CollectArgs a{to, nullptr, nullptr, nullptr, row_of, topk_w, nullptr, d_topk_w, {}, c.T, c.d, c.k, 0, false};
-    const bool nt = passes_caches(c);
+    const int past = d_topk_w ? passes_caches_gradient(c) : passes_caches(c);
     by_slots(c.k, [&](auto n) {
         constexpr int N = decltype(n)::value;
         by_launch(a, [&](const CollectArgs& b, dim3 grid) {
             auto go = [&](auto dot) {
                 constexpr bool DOT = decltype(dot)::value;
                 if (c.d <= kNarrow) hipLaunchKernelGGL((narrow_scatter_kernel<N, DOT>), grid, dim3(kTokenThreads), 0, s, b);
-                else if (nt) hipLaunchKernelGGL((scatter_kernel<N, DOT, true>), grid, dim3(kTokenThreads), 0, s, b);
-                else hipLaunchKernelGGL((scatter_kernel<N, DOT, false>), grid, dim3(kTokenThreads), 0, s, b);
+                else if (past == 2) hipLaunchKernelGGL((scatter_kernel<N, DOT, DOT ? 2 : 1>), grid, dim3(kTokenThreads), 0, s, b);
+                else if (past == 1) hipLaunchKernelGGL((scatter_kernel<N, DOT, 1>), grid, dim3(kTokenThreads), 0, s, b);
+                else hipLaunchKernelGGL((scatter_kernel<N, DOT, 0>), grid, dim3(kTokenThreads), 0, s, b);
             };
             if (b.dw) go(std::true_type{});
             else go(std::false_type{});

@@ -1,4 +1,4 @@
-"""Operators over slots that may have no row, where offsets pass 32 bits: more than 4 GiB of rows, more than 2^32 elements.  Compared on the GPU: tables and copies exactly,
+"""Operators over slots that may have no row, where offsets pass 32 bits: more than 4 GiB of rows, more than 2^32 elements; and where rows pass the caches by.  Compared on the GPU: tables and copies exactly,
 sums of two or three terms and products against fp32 torch operations on the same values, whose own errors are below (k + 4) 2^-24 of the terms' sizes: with the one rounding
 to bf16, 2^-8 |y| + 2^-20 A holds for both."""
 import pytest
@@ -23,7 +23,18 @@ def _rand(gen, *shape):
 @pytest.mark.parametrize("T,d,k,capacity", [(300_000, 4104, 2, 90_000), (11_000_000, 200, 1, 0)])
 def test_rows_beyond_four_gib(moe, T, d, k, capacity):
     assert T * k * d * 2 > 1 << 32
-    E, R = 8, T * k
+    assert _there_and_back(moe, T, d, k, capacity) * d * 2 > (1 << 32) - (1 << 30)
+
+
+@pytest.mark.parametrize("T,d,k,capacity", [(2300, 4104, 4, 1000), (2050, 7176, 6, 0), (1500, 7176, 8, 0), (70_000, 520, 2, 0), (6000, 1032, 12, 8000)])
+def test_rows_that_pass_the_caches_by(moe, T, d, k, capacity):
+    """From 64 MiB on those that collect's gradient writes, from 128 MiB on all; every batch of slots."""
+    assert T * k * d >= 1 << 25
+    _there_and_back(moe, T, d, k, capacity)
+
+
+def _there_and_back(moe, T, d, k, capacity):
+    E, R = 8 if k < 8 else 16, T * k
     gen = torch.Generator(device="cuda").manual_seed(3)
     x = torch.empty((T, d), dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
     idx = torch.rand((T, E + 1), generator=gen, device="cuda").topk(k, dim=1).indices.to(torch.int32)          # the last expert is elsewhere
@@ -45,7 +56,7 @@ def test_rows_beyond_four_gib(moe, T, d, k, capacity):
     want = torch.where(have, start[e.clamp(max=E - 1)] + rank, -1)
     N = int(start[-1])
     assert torch.equal(counts, n[:E].int()) and torch.equal(off, start.int()) and torch.equal(row.view(-1), want.int())
-    assert (src[N:] == -7).all() and torch.equal(want[src[:N].long()], torch.arange(N, device="cuda")) and N * d * 2 > (1 << 32) - (1 << 30)
+    assert (src[N:] == -7).all() and torch.equal(want[src[:N].long()], torch.arange(N, device="cuda"))
     for a in range(0, R, 1 << 17):
         b = min(a + (1 << 17), R)
         got = rows[a:b]
@@ -76,6 +87,7 @@ def test_rows_beyond_four_gib(moe, T, d, k, capacity):
         v = s * xx
         total, size = xx + ws[a:b].sum(1, keepdim=True) * v, xx.abs() + ws[a:b].abs().sum(1, keepdim=True) * v.abs()
         assert ((dx[a:b].float() - total).abs() <= 2.0**-8 * total.abs() + 2.0**-8 * 1.01 * size).all(), a
+    return N
 
 
 def test_dropout_beyond_32_bits(moe):
