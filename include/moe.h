@@ -281,7 +281,8 @@ moe_status moe_combine_backward(const moe_config* cfg, const void* dy, const voi
  *   dz = the gate's gradient: MOE_GATE_SOFTMAX p_e (G_e - sum_i p_i d_i) over all experts (p = softmax(z), G_e: d of the slot that chose e, else 0);
  *        MOE_GATE_SOFTMAX_RENORM w_i (d_i - sum_j w_j d_j) over the chosen; MOE_GATE_SIGMOID_NORM the same times 1 - sigmoid(z_i)
  *   dx [T,d] bf16 = dz W_r,  dW_r [E,d] = dz^T x (bf16, or fp32 with MOE_GRAD_F32),  dbias [E] fp32 = sum_t dz
- * z is formed again (fp32 sums; not for MOE_GATE_SOFTMAX_RENORM); dz enters both products as two bf16 numbers (16 bits; an infinite one comes out as NaN).
+ * z is formed again (fp32 sums; not for MOE_GATE_SOFTMAX_RENORM); dz enters the products as two bf16 numbers (16 bits), for dW_r in fp32 as three (24 bits): an infinity in dz,
+ * x or W_r comes out as NaN as a rule.
  * dx, dW_r and dbias may be NULL: not computed.  MOE_GRAD_ACCUMULATE: dW_r and dbias are added to what the tensors hold.  x's whole gradient: moe_dispatch_backward
  * with this dx as base.  A slot whose index is outside 0 .. E-1 has no part in anything.  T == 0: dW_r and dbias of zero are written unless they are added to.
  * Limit: d <= 2^20.  Outputs must not overlap inputs.  workspace: moe_route_backward_workspace_size(cfg) bytes, 256-byte aligned; calls that may run at
@@ -297,7 +298,8 @@ moe_status moe_route_backward(const moe_config* cfg, const void* x, const void* 
  * The rows are what moe_grouped_ffn and the training operators take, with the same T*k (their k <= E: T*k tokens with k = 1 say the same).
  * Limits: d % 8 == 0, d <= 2^20, k <= 256, E <= 256, T*k <= 2^30, first + E <= 2^31 - 1, else MOE_ERR_UNSUPPORTED (MOE_ERR_SHAPE for the last); sizes in bytes are
  * not limited.  No atomics on memory: results are bit-reproducible.  row_of below: moe_dispatch's; a number outside 0 .. T*k-1 is a slot without a row, and
- * no two slots may share one.  Tensors of [T*k,d] hold offsets[E] rows; what lies behind is neither read nor written.  topk_w may be NULL: weights of one.  Outputs
+ * no two slots may share one.  Tensors of [T*k,d] hold offsets[E] rows; what lies behind is neither read nor written.
+ * The calls after moe_dispatch go by T, d and k of cfg.  topk_w may be NULL: weights of one.  Outputs
  * must not overlap inputs but where it is said. */
 typedef struct {
     int32_t T, d, k;           /* tokens, width, slots per token */

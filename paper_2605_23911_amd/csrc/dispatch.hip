@@ -4,7 +4,8 @@
 //   dispatch   rows[row(t,i)] = (w[t,i]) x[t]          its gradient  dx[t] = (base[t] +) sum_i (w[t,i]) drows[row(t,i)],  dw[t,i] = <x[t], drows[row(t,i)]>
 //   collect    y[t] = (residual[t] +) D(sum_i (w[t,i]) rows[row(t,i)])
 //              its gradient  v = D(dy[t]), drows[row(t,i)] = (w[t,i]) v,  dw[t,i] = <v, rows[row(t,i)]>
-// Each pass moves every row once, so all four are bound by memory, the small ones by the launch.  No atomics on memory: results are bit-reproducible.
+// Each pass moves every row once, so all four are bound by memory from about a thousand rows on, the small ones by a launch's 2-5 us.  No atomics on memory: results are
+// bit-reproducible.
 #include <type_traits>
 
 #include "token_rows.hpp"
@@ -62,6 +63,7 @@ __device__ __forceinline__ int bin_total(const int* bins, int copies, int E, int
     return n;
 }
 
+// What each chunk of 1024 slots has of every expert, for calls in which counting all slots in every workgroup takes longer than a launch: 3.4-4.8 us at 32768 slots.
 __global__ __launch_bounds__(kTokenThreads) void count_chunks_kernel(DispatchArgs a) {
     __shared__ int bins[2 * kBins];
     const int copies = bin_copies(a.E);
@@ -211,7 +213,8 @@ __device__ __forceinline__ unsigned long long same_expert(int e) {
 }
 __device__ __forceinline__ int in_front(unsigned long long lanes, int lane) { return __popcll(lanes & ((1ull << lane) - 1)); }
 
-// The tables alone, 1024 slots per workgroup, a slot per thread.  A wavefront ranks its 64 slots among themselves, a sum over the wavefronts' counts does the rest.
+// The tables alone, 1024 slots per workgroup, a slot per thread.  A wavefront ranks its 64 slots among themselves, a sum over the wavefronts' counts does the rest (one wavefront
+// after the other 15 us).  Bound by latency: 4.2 us at 2 slots, 5.3 at 4096, with the count 8.4 at 32768.
 constexpr int kTableThreads = kChunk, kTableWaves = kTableThreads / kWave;
 __global__ __launch_bounds__(kTableThreads) void tables_kernel(DispatchArgs a) {
     __shared__ Places<kTableThreads> places;
@@ -248,7 +251,9 @@ __device__ __forceinline__ void order_lanes() {
 }
 
 // Tables and rows: a workgroup takes `per` tokens, finds out where its slots go, ranks them, and moves its tokens' rows: less than four tokens one after the other, more a
-// wavefront each, narrow ones (d up to kNarrow, half a wavefront's loads) a few lanes each.
+// wavefront each, narrow ones (d up to kNarrow, half a wavefront's loads) a few lanes each.  One launch for tables and rows, since a launch of its own for the rows takes 3 us more
+// than it saves (24576 slots x 2048 31.3 / 28.6 us).  x is read once, not once per slot.  1 token 4.5 us, 1024 x 2 x 4096 9.3; 4096 x 8 x 7168, 0.39 GB written, 82 us (5.5 TB/s).
+// x requested before the count, to cover its latency: 512 x 8 x 7168 18.9 / 19.9, 1 token 4.7 / 6.1 us (longer code), not kept.
 template <int N, bool NT, bool NARROW>
 __global__ __launch_bounds__(kTokenThreads) void dispatch_kernel(DispatchArgs a) {
     __shared__ Places<kTokenThreads> places;
@@ -322,7 +327,9 @@ __device__ __forceinline__ int my_token(const CollectArgs& a) {
     return a.t0 + (a.whole ? (int)blockIdx.x : (int)blockIdx.x * kTokenWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave));
 }
 
-// MANY: more than N slots per token, in batches
+// y[t] = (add[t] +) D(sum_i w[t,i] row(t,i)), and with DOT <x[t], row(t,i)>, in slot order.  A token's rows are requested before the first is used.  Bound by memory: 4096 x 8 x
+// 7168 97-98 us (0.59 GB, 6.0 TB/s), with dropout the same; 512 x 8 x 7168 13.1, 64 x 2 x 4096 3.1.
+// MANY: more than N slots per token, in batches, over which the columns run for the sum and which run over the columns for the dot products.
 template <int N, bool DOT, bool NT, bool MANY>
 __global__ __launch_bounds__(kTokenThreads) void gather_kernel(CollectArgs a) {
     __shared__ float part[kTokenWaves][8];
@@ -403,6 +410,7 @@ __global__ __launch_bounds__(kTokenThreads) void gather_kernel(CollectArgs a) {
     }
 }
 
+// The gradient of collect: rows read (DOT) and their gradients written.  Bound by memory: 4096 x 8 x 7168, 1.0 GB, 191-209 us (4.8-5.2 TB/s, a copy's rate), 1999 x 8 x 3584 31.
 template <int N, bool DOT, int PAST>
 __global__ __launch_bounds__(kTokenThreads) void scatter_kernel(CollectArgs a) {
     __shared__ float part[kTokenWaves][8];
@@ -419,9 +427,10 @@ __global__ __launch_bounds__(kTokenThreads) void scatter_kernel(CollectArgs a) {
     }
 }
 
-// NARROW rows (d up to 256): `lots` = d / 8 lanes per token, as many tokens as fit into a wavefront; the other lanes idle.
+// NARROW rows (d up to 256): `lots` = d / 8 lanes per token, as many tokens as fit into a wavefront; the other lanes idle.  16384 tokens of 8 slots, d = 8, the way back and
+// its gradient, a wavefront per token / so: 11.2 / 7.3 and 29.6 / 7.7 us, of 4 slots, d = 64 8.2 / 7.1 and 16.6 / 7.6 (what a call takes on the host).
 struct NarrowPlace {
-    int t, c, lot;             // token (T: none), first column, the lane's place among the token's
+    int t, c, lot;             // token (0 where the lane idles), first column, the lane's place among the token's
     bool there;
 };
 __device__ __forceinline__ NarrowPlace narrow_place(const CollectArgs& a) {
@@ -528,6 +537,8 @@ __global__ __launch_bounds__(kTokenThreads) void narrow_scatter_kernel(CollectAr
     }
 }
 
+// Sixteen bits per element, so that one call of the generator serves the eight elements of a load and stays below memory's time: 4096 x 7168 with a residual 26.5-30 us
+// (176 MB, 5.9-6.6 TB/s), with the generator called twice 32.
 template <bool ADD>
 __global__ __launch_bounds__(kTokenThreads) void dropout_kernel(const uint16_t* x, const uint16_t* add, uint16_t* y, long long n, Dropout p) {
     const uint64_t seed = p.rng ? p.rng[0] : 0, offset = p.rng ? p.rng[1] : 0;
@@ -554,7 +565,8 @@ __global__ __launch_bounds__(kTokenThreads) void dropout_kernel(const uint16_t* 
     }
 }
 
-// Slots up to which every workgroup counts them all (of the workgroups that move rows, of those that write the tables); beyond, a launch before counts them by chunks.
+// Slots up to which every workgroup counts them all (of the workgroups that move rows, of those that write the tables); beyond, a launch before counts them by chunks.  Rows, all
+// counted / by chunks, us: 2800 slots x 2048 8.9 / 11.7, 4096 x 7168 18.4 / 19.0, 8192 x 7168 35 / 31; tables: 16384 slots 8.0 / 8.4, 32768 10.9 / 9.0.
 constexpr int kCountAllRows = 4096, kCountAll = 16384;
 constexpr int kSumInside = 64;            // chunks up to which a workgroup adds their counts up
 
@@ -586,7 +598,8 @@ void by_slots(int k, F&& go) {
     }
 }
 
-// Tokens of one launch: it has less than 2^32 threads.
+// Tokens of one launch: it has less than 2^32 threads.  A wavefront per token up to 1024 columns, two loads of it, else a workgroup: us, a wavefront / a workgroup, collect
+// 16384 x 2 x 1024 21.7 / 22.8, 8192 x 2 x 2048 22.0 / 21.6, 512 x 3 x 7168 10.4 / 8.0; its gradient 16384 x 2 x 1024 34.5 / 42.9, 8192 x 2 x 2048 35.7 / 32.9.
 template <class F>
 void by_launch(CollectArgs a, F&& go) {
     a.whole = a.d > 1024;
