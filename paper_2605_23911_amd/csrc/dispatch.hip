@@ -37,18 +37,27 @@ __device__ __forceinline__ int local_expert(const DispatchArgs& a, long long j) 
     return (uint32_t)e < (uint32_t)a.E ? e : -1;
 }
 
-// Slots j0 .. j1 - 1 into the bins; those from `split` on into the second half.  Sixteen ids per thread are requested before the first is counted.
+// Slots j0 .. j1 - 1 into the bins; those from `split` on into the second half.  Sixteen ids per thread are requested before the first is counted, and what is no slot of an
+// expert here goes to a bin of the lane's own behind the others: no branch that a wavefront takes by its ids (with such branches 4096 slots took a workgroup 4.8 us, so 1.8).
 template <int THREADS>
 __device__ __forceinline__ void count_slots(const DispatchArgs& a, long long j0, long long j1, long long split, int copies, int* bins) {
-    const int mine = (threadIdx.x & (copies - 1)) * a.E;
     constexpr int AHEAD = 16;
-    for (long long j = j0 + threadIdx.x; j < j1; j += AHEAD * THREADS) {
-        int e[AHEAD];
+    const int mine = (threadIdx.x & (copies - 1)) * a.E, none = 2 * kBins + threadIdx.x % kWave;
+    for (long long at = j0; at < j1; at += AHEAD * THREADS) {
+        const int32_t* idx = a.idx + at;
+        const int n = j1 - at < AHEAD * THREADS ? (int)(j1 - at) : AHEAD * THREADS, half = split - at < n ? (int)(split - at) : n;     // may be negative
+        int id[AHEAD];
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) e[i] = j + i * THREADS < j1 ? local_expert(a, j + i * THREADS) : -1;
+        for (int i = 0; i < AHEAD; ++i) {
+            const int j = threadIdx.x + i * THREADS;
+            if (i * THREADS < n) id[i] = idx[j < n ? j : n - 1];
+        }
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i)
-            if (e[i] >= 0) atomicAdd(&bins[(j + i * THREADS >= split ? kBins : 0) + mine + e[i]], 1);
+        for (int i = 0; i < AHEAD; ++i) {
+            const int j = threadIdx.x + i * THREADS;
+            const uint32_t e = (uint32_t)id[i] - (uint32_t)a.first;
+            if (i * THREADS < n) atomicAdd(&bins[j < n && e < (uint32_t)a.E ? (j >= half ? kBins : 0) + mine + (int)e : none], 1);
+        }
     }
 }
 __device__ __forceinline__ int bin_copies(int E) {
@@ -65,7 +74,7 @@ __device__ __forceinline__ int bin_total(const int* bins, int copies, int E, int
 
 // What each chunk of 1024 slots has of every expert, for calls in which counting all slots in every workgroup takes longer than a launch: 3.4-4.8 us at 32768 slots.
 __global__ __launch_bounds__(kTokenThreads) void count_chunks_kernel(DispatchArgs a) {
-    __shared__ int bins[2 * kBins];
+    __shared__ int bins[2 * kBins + kWave];
     const int copies = bin_copies(a.E);
     for (int i = threadIdx.x; i < copies * a.E; i += kTokenThreads) bins[i] = 0;
     __syncthreads();
@@ -153,7 +162,7 @@ __device__ __forceinline__ void scatter_slots(const ScatterArgs& a, const Slots<
 // `hist`, of the slots between the chunk's start and the workgroup's own and the chunks' counts.  The first workgroup writes counts and offsets.
 template <int THREADS>
 struct Places {
-    int bins[2 * kBins];
+    int bins[2 * kBins + kWave];
     int next[kMaxExperts], start[kMaxExperts], sums[THREADS / kWave];
 
     __device__ __forceinline__ void find(const DispatchArgs& a, long long s0) {
@@ -214,7 +223,7 @@ __device__ __forceinline__ unsigned long long same_expert(int e) {
 __device__ __forceinline__ int in_front(unsigned long long lanes, int lane) { return __popcll(lanes & ((1ull << lane) - 1)); }
 
 // The tables alone, 1024 slots per workgroup, a slot per thread.  A wavefront ranks its 64 slots among themselves, a sum over the wavefronts' counts does the rest (one wavefront
-// after the other 15 us).  Bound by latency: 4.2 us at 2 slots, 5.3 at 4096, with the count 8.4 at 32768.
+// after the other 15 us).  Bound by latency: 4.2 us at 2 slots, 5.3 at 4096, 8 at 32768.
 constexpr int kTableThreads = kChunk, kTableWaves = kTableThreads / kWave;
 __global__ __launch_bounds__(kTableThreads) void tables_kernel(DispatchArgs a) {
     __shared__ Places<kTableThreads> places;
@@ -252,8 +261,9 @@ __device__ __forceinline__ void order_lanes() {
 
 // Tables and rows: a workgroup takes `per` tokens, finds out where its slots go, ranks them, and moves its tokens' rows: less than four tokens one after the other, more a
 // wavefront each, narrow ones (d up to kNarrow, half a wavefront's loads) a few lanes each.  One launch for tables and rows, since a launch of its own for the rows takes 3 us more
-// than it saves (24576 slots x 2048 31.3 / 28.6 us).  x is read once, not once per slot.  1 token 4.5 us, 1024 x 2 x 4096 9.3; 4096 x 8 x 7168, 0.39 GB written, 82 us (5.5 TB/s).
-// x requested before the count, to cover its latency: 512 x 8 x 7168 18.9 / 19.9, 1 token 4.7 / 6.1 us (longer code), not kept.
+// than it saves (24576 slots x 2048 31.3 / 28.6 us).  x is read once, not once per slot.  1 token 4.5 us, 1024 x 2 x 4096 8; 4096 x 8 x 7168, 0.39 GB written, 82 us (5.5 TB/s).
+// What comes before the rows, of a workgroup's time: 0.2 us to clear the bins, 1-2 to count, 0.4-1.6 for the totals, 0.6 for the sums, 0.6 for the ranks.  Not kept: x (1 token 4.5 us,
+// so 6.1), the chunks' counts and the workgroup's own ids (even or 0.2 us more) requested before the count.
 template <int N, bool NT, bool NARROW>
 __global__ __launch_bounds__(kTokenThreads) void dispatch_kernel(DispatchArgs a) {
     __shared__ Places<kTokenThreads> places;
@@ -565,9 +575,10 @@ __global__ __launch_bounds__(kTokenThreads) void dropout_kernel(const uint16_t* 
     }
 }
 
-// Slots up to which every workgroup counts them all (of the workgroups that move rows, of those that write the tables); beyond, a launch before counts them by chunks.  Rows, all
-// counted / by chunks, us: 2800 slots x 2048 8.9 / 11.7, 4096 x 7168 18.4 / 19.0, 8192 x 7168 35 / 31; tables: 16384 slots 8.0 / 8.4, 32768 10.9 / 9.0.
-constexpr int kCountAllRows = 4096, kCountAll = 16384;
+// Slots up to which every workgroup counts them all (of the workgroups that move rows, of those that write the tables); beyond, a launch before counts them by chunks.  Rows, us, all
+// counted / by chunks: 8192 slots x 2048 14.3 / 15.9, x 7168 27.9 / 30.8, 12000 x 7168 40.9 / 43.0, 16384 x 2048 22.5 / 20.7, 32768 x 512 27.5 / 16.6; tables: 32768 slots 9.0 / 9.7,
+// 65536 13.5 / 9.6.
+constexpr int kCountAllRows = 8192, kCountAll = 32768;
 constexpr int kSumInside = 64;            // chunks up to which a workgroup adds their counts up
 
 int chunks_of(const moe_dispatch_config& c) { return (int)(((long long)c.T * c.k + kChunk - 1) / kChunk); }

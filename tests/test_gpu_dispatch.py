@@ -213,7 +213,7 @@ def test_one_expert_chosen_by_every_slot(moe):
         p.check_dispatch(True)
 
 
-@pytest.mark.parametrize("T,k,experts,cap", [(8192, 1, 8, 0), (8193, 1, 8, 0), (4097, 2, 256, 20), (8200, 8, 256, 0), (65536, 1, 60, 0), (65537, 1, 60, 900), (40_000, 12, 33, 0),
+@pytest.mark.parametrize("T,k,experts,cap", [(8192, 1, 8, 0), (8193, 1, 8, 0), (32768, 1, 64, 600), (32769, 1, 64, 600), (4097, 2, 256, 20), (8200, 8, 256, 0), (65536, 1, 60, 0), (65537, 1, 60, 900), (40_000, 12, 33, 0),
                                              (300_000, 4, 256, 4000)])
 def test_tables_of_many_slots(moe, T, k, experts, cap):
     """Both sides of the lines between one, two and three launches; against a stable sort."""
