@@ -339,8 +339,9 @@ __device__ __forceinline__ int my_token(const CollectArgs& a) {
 
 // y[t] = (add[t] +) D(sum_i w[t,i] row(t,i)), and with DOT <x[t], row(t,i)>, in slot order.  A token's rows are requested before the first is used.  Bound by memory: 4096 x 8 x
 // 7168 97-98 us (0.59 GB, 6.0 TB/s), with dropout the same; 512 x 8 x 7168 13.1, 64 x 2 x 4096 3.1.
-// MANY: more than N slots per token, in batches, over which the columns run for the sum and which run over the columns for the dot products.
-template <int N, bool DOT, bool NT, bool MANY>
+// B batches of N slots, all requested before the first is used; B = 0: any number of batches, over which the columns run for the sum and which run over the columns for the dot
+// products.
+template <int N, bool DOT, bool NT, int B>
 __global__ __launch_bounds__(kTokenThreads) void gather_kernel(CollectArgs a) {
     __shared__ float part[kTokenWaves][8];
     const int t = my_token(a);
@@ -351,44 +352,63 @@ __global__ __launch_bounds__(kTokenThreads) void gather_kernel(CollectArgs a) {
     const float* w = a.w ? a.w + (size_t)t * a.k : nullptr;
     const Row add = row_at(a.add, (size_t)t * a.d * 2, a.add != nullptr, a.d * 2), y = row_at(a.y, (size_t)t * a.d * 2, true, a.d * 2);
     const uint64_t seed = a.p.rng ? a.p.rng[0] : 0, offset = a.p.rng ? a.p.rng[1] : 0;
-    Slots<N> s;
-    if constexpr (!MANY) s.load(row_of, w, 0, a.k, R);
-    float dot[N];
+    constexpr int HELD = B ? B : 1;
+    Slots<N> s[HELD];
+    float dot[HELD][N];
+    bool any = false;
 #pragma unroll
-    for (int i = 0; i < N; ++i) dot[i] = 0.0f;
-    const Row x = row_at(a.x, (size_t)t * a.d * 2, DOT && !MANY && s.any, a.d * 2);
+    for (int b = 0; b < B; ++b) {
+        s[b].load(row_of, w, b * N, a.k, R);
+        any |= s[b].any;
+    }
+#pragma unroll
+    for (int b = 0; b < HELD; ++b)
+#pragma unroll
+        for (int i = 0; i < N; ++i) dot[b][i] = 0.0f;
+    const Row x = row_at(a.x, (size_t)t * a.d * 2, DOT && any, a.d * 2);
     for (int c = lane * 8; c < a.d; c += threads * 8) {
         float sum[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
         const u32x4_t more = read8<false>(add, c * 2);
-        u32x4_t with;
-        if constexpr (DOT && !MANY) with = read8<false>(x, c * 2);
-        auto batch = [&] {
-            u32x4_t v[N];
+        auto request = [&](const Slots<N>& from, u32x4_t (&v)[N]) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = read8<NT>(s.at(a.rows, i, a.d), c * 2);
+            for (int i = 0; i < N; ++i) v[i] = read8<NT>(from.at(a.rows, i, a.d), c * 2);
+        };
+        auto take = [&](const Slots<N>& from, const u32x4_t (&v)[N], const u32x4_t& with, float (&dots)[N]) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 float q[8];
                 floats8(v[i], q);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) sum[j] = fmaf(s.w[i], q[j], sum[j]);
-                if constexpr (DOT && !MANY) {
+                for (int j = 0; j < 8; ++j) sum[j] = fmaf(from.w[i], q[j], sum[j]);
+                if constexpr (DOT && B > 0) {
                     float o[8];
                     floats8(with, o);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) dot[i] = fmaf(o[j], q[j], dot[i]);
+                    for (int j = 0; j < 8; ++j) dots[i] = fmaf(o[j], q[j], dots[i]);
                 }
             }
         };
-        if constexpr (MANY) {
-            for (int i0 = 0; i0 < a.k; i0 += N) {
-                s.load(row_of, w, i0, a.k, R);
-                batch();
-            }
+        u32x4_t with = {0, 0, 0, 0};
+        if constexpr (DOT && B > 0) with = read8<false>(x, c * 2);
+        if constexpr (B == 1) {
+            u32x4_t v[N];
+            request(s[0], v);
+            take(s[0], v, with, dot[0]);
+        } else if constexpr (B > 1) {
+            u32x4_t v[HELD][N];
+#pragma unroll
+            for (int b = 0; b < B; ++b) request(s[b], v[b]);
+#pragma unroll
+            for (int b = 0; b < B; ++b) take(s[b], v[b], with, dot[b]);
         } else {
-            batch();
+            for (int i0 = 0; i0 < a.k; i0 += N) {
+                u32x4_t v[N];
+                s[0].load(row_of, w, i0, a.k, R);
+                request(s[0], v);
+                take(s[0], v, with, dot[0]);
+            }
         }
         if (a.p.rng) drop8(sum, ((uint64_t)t * a.d + c) / 8, seed, offset, a.p);
         float o[8];
@@ -397,25 +417,28 @@ __global__ __launch_bounds__(kTokenThreads) void gather_kernel(CollectArgs a) {
         for (int j = 0; j < 8; ++j) sum[j] += o[j];
         write8<false>(bf16s8(sum), y, c * 2);
     }
-    if constexpr (DOT && !MANY) store_dots<N>(dot, s, part, a.whole, a.k, a.dw + (size_t)t * a.k);
-    if constexpr (DOT && MANY) {           // the rows once more, a batch of slots at a time
-        for (int i0 = 0; i0 < a.k; i0 += N) {
-            s.load(row_of, w, i0, a.k, R);
-            const Row in = row_at(a.x, (size_t)t * a.d * 2, s.any, a.d * 2);
+    if constexpr (DOT && B > 0) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) dot[i] = 0.0f;
+        for (int b = 0; b < B; ++b) store_dots<N>(dot[b], s[b], part, a.whole, a.k - b * N < N ? a.k - b * N : N, a.dw + (size_t)t * a.k + b * N);
+    }
+    if constexpr (DOT && B == 0) {         // the rows once more, a batch of slots at a time
+        for (int i0 = 0; i0 < a.k; i0 += N) {
+            s[0].load(row_of, w, i0, a.k, R);
+            const Row in = row_at(a.x, (size_t)t * a.d * 2, s[0].any, a.d * 2);
+#pragma unroll
+            for (int i = 0; i < N; ++i) dot[0][i] = 0.0f;
             for (int c = lane * 8; c < a.d; c += threads * 8) {
                 float o[8];
                 floats8(read8<false>(in, c * 2), o);
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     float q[8];
-                    floats8(read8<false>(s.at(a.rows, i, a.d), c * 2), q);
+                    floats8(read8<false>(s[0].at(a.rows, i, a.d), c * 2), q);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) dot[i] = fmaf(o[j], q[j], dot[i]);
+                    for (int j = 0; j < 8; ++j) dot[0][i] = fmaf(o[j], q[j], dot[0][i]);
                 }
             }
-            store_dots<N>(dot, s, part, a.whole, a.k - i0 < N ? a.k - i0 : N, a.dw + (size_t)t * a.k + i0);
+            store_dots<N>(dot[0], s[0], part, a.whole, a.k - i0 < N ? a.k - i0 : N, a.dw + (size_t)t * a.k + i0);
         }
     }
 }
@@ -593,11 +616,13 @@ int passes_caches_gradient(const moe_dispatch_config& c) {
     return n >= (1ll << 26) ? 2 : n >= (1ll << 25) ? 1 : 0;
 }
 
-// go(integral_constant<slots per batch>): as many as a token has, up to eight.  Batches of 4 and 8 with empty rows cost 1-3 % at 3, 5, 6 and 7 slots.
+// go(integral_constant<slots per batch>): a token's slots in the fewest batches of up to eight, all of one size.  Batches of 4 and 8 with empty rows cost 1-3 % at 3, 5, 6 and 7
+// slots and 1-13 % at 9 to 15.
 template <class F>
 void by_slots(int k, F&& go) {
     using std::integral_constant;
-    switch (k) {
+    const int batches = (k + 7) / 8;
+    switch ((k + batches - 1) / batches) {
         case 1: go(integral_constant<int, 1>{}); break;
         case 2: go(integral_constant<int, 2>{}); break;
         case 3: go(integral_constant<int, 3>{}); break;
@@ -639,20 +664,22 @@ static hipError_t launch_gather(const moe_dispatch_config& c, CollectArgs a, hip
                 else hipLaunchKernelGGL((narrow_gather_kernel<N, false>), grid, dim3(kTokenThreads), 0, s, b);
                 return;
             }
-            auto go = [&](auto dot, auto many) {
-                constexpr bool DOT = decltype(dot)::value, MANY = decltype(many)::value;
-                if (nt) hipLaunchKernelGGL((gather_kernel<N, DOT, true, MANY>), grid, dim3(kTokenThreads), 0, s, b);
-                else hipLaunchKernelGGL((gather_kernel<N, DOT, false, MANY>), grid, dim3(kTokenThreads), 0, s, b);
+            auto go = [&](auto dot, auto batches) {
+                constexpr bool DOT = decltype(dot)::value;
+                constexpr int B = decltype(batches)::value;
+                if (nt) hipLaunchKernelGGL((gather_kernel<N, DOT, true, B>), grid, dim3(kTokenThreads), 0, s, b);
+                else hipLaunchKernelGGL((gather_kernel<N, DOT, false, B>), grid, dim3(kTokenThreads), 0, s, b);
             };
-            if constexpr (N == 8) {
-                if (c.k > N) {
-                    if (b.dw) go(std::true_type{}, std::true_type{});
-                    else go(std::false_type{}, std::true_type{});
-                    return;
-                }
+            auto with_dots = [&](auto batches) {
+                if (b.dw) go(std::true_type{}, batches);
+                else go(std::false_type{}, batches);
+            };
+            using std::integral_constant;
+            if constexpr (N >= 5) {
+                if (c.k > 2 * N) return with_dots(integral_constant<int, 0>{});
+                if (c.k > N) return with_dots(integral_constant<int, 2>{});
             }
-            if (b.dw) go(std::true_type{}, std::false_type{});
-            else go(std::false_type{}, std::false_type{});
+            with_dots(integral_constant<int, 1>{});
         });
     });
     return hipGetLastError();

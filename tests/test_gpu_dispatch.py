@@ -139,7 +139,8 @@ class Plan:
 # tokens, width, slots, experts in all, then experts here, the first of them, capacity, skew
 PLANS = [(1, 8, 1, 1), (1, 4096, 2, 8), (3, 256, 2, 8, 4, 2), (5, 1032, 3, 7, 7, 0, 2), (64, 1024, 4, 16, 5, 9, 3, 1.0), (65, 1040, 8, 64), (257, 72, 8, 60, 60, 0, 20, 1.5),
          (130, 2048, 5, 9, 3, 6), (301, 320, 12, 32, 20, 4, 50), (40, 2056, 11, 256, 256, 0, 1), (33, 128, 64, 200, 100, 50), (2, 64, 256, 256), (7, 16, 9, 3),
-         (700, 64, 12, 40, 40, 0, 100), (1025, 8, 8, 8, 8, 0, 0, 2.0), (9000, 16, 1, 17), (9001, 8, 8, 8, 3, 1, 2000), (5, 48, 2, 100, 2, 90)]
+         (700, 64, 12, 40, 40, 0, 100), (1025, 8, 8, 8, 8, 0, 0, 2.0), (9000, 16, 1, 17), (9001, 8, 8, 8, 3, 1, 2000), (5, 48, 2, 100, 2, 90),
+         (6, 520, 9, 20), (5, 2064, 13, 40, 30, 5), (5, 264, 15, 30), (6, 1104, 16, 30, 20), (5, 1032, 17, 40, 30), (4, 264, 64, 100, 50, 20), (3, 2056, 256, 256, 200, 9)]
 
 
 @pytest.mark.parametrize("plan", PLANS, ids=lambda p: "-".join(map(str, p)))
