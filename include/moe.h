@@ -25,7 +25,8 @@
  *   - Limits: 1 <= k <= E <= 256, d % 64 == 0, F % 64 == 0, T >= 0, T*k <= 2^30, and the
  *     activation buffers (x, x_perm, h: T*k*max(d,F) elements of 2 bytes) below 4 GiB: the GEMM
  *     kernels address their rows with 32-bit byte offsets.  Beyond: MOE_ERR_UNSUPPORTED.
- *     T == 0 returns MOE_OK and enqueues nothing (but moe_grouped_ffn_backward: weight gradients of zero are written).
+ *     T == 0 returns MOE_OK and enqueues nothing (but moe_grouped_ffn_backward and moe_route_backward: gradients of weights
+ *     of zero are written; and moe_dispatch: counts and offsets of zero).
  *   - Stream capture: the calls record kernel launches only and may be captured into a HIP
  *     graph; replays equal the eager result.  The first use of a GEMM kernel in a process sets
  *     a function attribute (its LDS size), which HIP does not allow during capture: run the

@@ -5,6 +5,7 @@ End to end: a result went through n roundings to bf16 whose errors are independe
 result's norm; SiLU' passes a rounding of g on by |g SiLU''(g) / SiLU'(g)|, which is counted as two.  n is given with each check."""
 import os
 import sys
+import threading
 
 import numpy as np
 import pytest
@@ -212,6 +213,37 @@ def test_two_steps_at_once(moe):
             st.run(stream=stream)
     torch.cuda.synchronize()
     for st, w in zip((a, b), want):
+        assert all(torch.equal(t, w[n]) for n, t in st.results().items())
+
+
+def test_two_host_threads(moe):
+    """Each with a stream, a workspace and tensors of its own."""
+    steps = [Step(moe, *STEPS[i], seed=5 + i) for i in (1, 3)]
+    want = []
+    for st in steps:
+        st.run()
+        torch.cuda.synchronize()
+        want.append({n: t.clone() for n, t in st.results().items()})
+        st.clear()
+    torch.cuda.synchronize()
+    failed = []
+
+    def work(st):
+        try:
+            stream = torch.cuda.Stream()
+            for _ in range(20):
+                st.run(stream=stream)
+            stream.synchronize()
+        except Exception as e:  # noqa: BLE001
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=(st,)) for st in steps]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed, failed
+    for st, w in zip(steps, want):
         assert all(torch.equal(t, w[n]) for n, t in st.results().items())
 
 
