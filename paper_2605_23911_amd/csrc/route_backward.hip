@@ -12,11 +12,16 @@ namespace moe {
 
 namespace {
 
-// Tiles of the two products: of many tokens, of up to 2048, and of up to 64.  Mid has half of Many's area and three workgroups per CU: kernels of a call, us, Many / Mid:
-// 256 experts of 7168, 512 tokens 43.8 / 38.2, 2048 74.4 / 70.6, 4096 107 / 113; 64 of 3584, 1999 tokens 24.1 / 23.4, 4096 30.5 / 32.1; 8 of 4096, 512 18.8 / 18.1, 8192 52.6 / 59.9.
+// Tiles of the two products, by the size of one of them, T d E (E in whole tiles of 64), up to 2^31 Low, from there to 2^32 Mid, above that Many; up to 64 tokens Few.
+// Smaller tiles fill the CUs with fewer pieces to join and leave a shorter last round; larger ones read less from the caches.  dz, products and join, us, Low / Mid / Many:
+// 256 experts of 7168, 768 tokens 27.0 / 34.8 / 33.8, 1024 33.0 / 35.4 / 35.7, 2048 55.2 / 50.9 / 55.3, 4096 99 / 80.9 / 75.9; 256 of 2048, 2048 28.5 / 29.6 / 32.0, 8192 64.4 / 58.7 / 60.4;
+// 128 of 2048, 2048 22.4 / 26.3 / 28.2, 8192 41.7 / 42.8 / 47.0; 64 of 3584, 4096 28.8 / 31.4 / 29.9; 8 of 4096, 2048 18.8 / 20.7 / 20.4, 8192 37.0 / 43.3 / 37.7, 16384 79.7 / 91.9 / 74.1:
+// up to 64 experts fill no more than half of Mid's tiles of dW_r, and it is left out.
 typedef Pair Many;
 typedef Shape<128, 128, 2, 2, 32, 2, 3, 60> Mid;
+typedef Shape<64, 128, 1, 4, 32, 2, 3, 60> Low;
 typedef Shape<64, 64, 2, 2, 64, 2, 2, 60> Few;
+typedef Shape<64, 128, 1, 4, 64, 4, 1, 60> Slim;        // logits of few tokens
 
 struct RouteArgs {
     const uint16_t *x, *wr;
@@ -37,6 +42,7 @@ struct RouteArgs {
 
 // Tile: BM tokens x BN experts, one piece of d.  4096 tokens x 256 experts of 7168: 22.5 us (0.67 PFLOP/s; x, 59 MB, comes from memory, matrix cores 23 % busy) in four pieces (2: 30, 3: 24.5,
 // 6: 28, 8: 30) with Small (Tall 23, Half 24.5, Wide 28, Pair 32; 64 x 256, 128 x 256 and 128 x 128 of four wavefronts 23-24).  Few experts take Flat.
+// Products up to 2^31 take Slim, us, Small / Slim (Flat): 256 of 7168, 200 tokens 8.4 / 7.3 (7.0), 512 11.2 / 10.0 (10.6), 1024 11.4 / 10.4 (12.3), 4096 21.8 / 24.4; 128 of 2048, 4096 12.3 / 8.4 (10.9).
 template <class S>
 __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void route_logits_kernel(RouteArgs a) {
     __shared__ __attribute__((aligned(1024))) char lds[S::kLds];
@@ -364,7 +370,7 @@ __global__ __launch_bounds__(256) void route_bias_kernel(RouteArgs a) {
 
 bool few_tokens(const moe_config& c) { return c.T <= Few::BM; }
 // Experts rounded up to whole steps of the products' reduction.
-static_assert(Mid::BK == Many::BK, "one padding");
+static_assert(Mid::BK == Many::BK && Low::BK == Many::BK, "one padding");
 int padded(const moe_config& c) { return few_tokens(c) ? (c.E + Few::BK - 1) / Few::BK * Few::BK : (c.E + Many::BK - 1) / Many::BK * Many::BK; }
 bool few_experts(const moe_config& c) { return c.E <= Flat::BM; }
 
@@ -376,9 +382,12 @@ int logit_pieces_of(const moe_config& c) {
     if (n > most) n = most;
     return n < 1 ? 1 : (int)n;
 }
+long long size_of_product(const moe_config& c) { return (long long)c.T * c.d * ((c.E + 63) / 64 * 64); }
+bool low(const moe_config& c) { return size_of_product(c) <= 1LL << 31; }
+bool mid(const moe_config& c) { return size_of_product(c) <= 1LL << 32 && c.E > 64; }
 int logit_pieces(const moe_config& c) {
     if (c.gating == MOE_GATE_SOFTMAX_RENORM) return 0;
-    return few_experts(c) ? logit_pieces_of<Flat>(c) : logit_pieces_of<Small>(c);
+    return few_experts(c) ? logit_pieces_of<Flat>(c) : low(c) ? logit_pieces_of<Slim>(c) : logit_pieces_of<Small>(c);
 }
 constexpr int kMostParts = 3;
 // Pieces of the tokens that dW_r is summed over: one tile of it per CU, beside which the CU's other workgroups take tiles of dx; no shorter than four steps.
@@ -389,8 +398,9 @@ int weight_pieces_of(const moe_config& c) {
     if (n > most) n = most;
     return n < 1 ? 1 : (int)n;
 }
-bool mid_tokens(const moe_config& c) { return c.T <= 2048; }
-int weight_pieces(const moe_config& c) { return few_tokens(c) ? weight_pieces_of<Few>(c) : mid_tokens(c) ? weight_pieces_of<Mid>(c) : weight_pieces_of<Many>(c); }
+int weight_pieces(const moe_config& c) {
+    return few_tokens(c) ? weight_pieces_of<Few>(c) : low(c) ? weight_pieces_of<Low>(c) : mid(c) ? weight_pieces_of<Mid>(c) : weight_pieces_of<Many>(c);
+}
 int dz_blocks(const moe_config& c) {
     const int n = (c.T + kDzWaves - 1) / kDzWaves;
     return n < 1024 ? n : 1024;
@@ -444,6 +454,7 @@ hipError_t launch_route_backward(const moe_config& c, const RouteGrad& p, hipStr
     }
     if (a.logit_pieces > 0) {
         if (few_experts(c)) go_logits<Flat>(a, s);
+        else if (low(c)) go_logits<Slim>(a, s);
         else go_logits<Small>(a, s);
     }
     if (a.Ep <= kWave) hipLaunchKernelGGL(route_dz_kernel<1>, dim3(a.dz_blocks), dim3(kDzThreads), 0, s, a);
@@ -451,7 +462,8 @@ hipError_t launch_route_backward(const moe_config& c, const RouteGrad& p, hipStr
     else hipLaunchKernelGGL(route_dz_kernel<4>, dim3(a.dz_blocks), dim3(kDzThreads), 0, s, a);
     if (!p.dx && !p.dwr) hipLaunchKernelGGL(route_bias_kernel, dim3(bias_groups(a)), dim3(256), 0, s, a);
     else if (few_tokens(c)) go_products<Few>(a, s);
-    else if (mid_tokens(c)) go_products<Mid>(a, s);
+    else if (low(c)) go_products<Low>(a, s);
+    else if (mid(c)) go_products<Mid>(a, s);
     else go_products<Many>(a, s);
     if (p.dwr && a.weight_pieces > 1) hipLaunchKernelGGL(route_join_kernel, dim3(joins), dim3(256), 0, s, a);
     return hipGetLastError();

@@ -98,7 +98,7 @@ class Case:
 
 
 SHAPES = [(1, 64, 1, 1), (1, 4096, 8, 2), (3, 128, 2, 2), (17, 256, 7, 3), (64, 512, 64, 8), (65, 320, 65, 8), (130, 192, 128, 5), (257, 576, 60, 8), (100, 1024, 256, 8),
-          (700, 640, 200, 12), (1999, 128, 16, 4), (515, 1216, 129, 2), (63, 64, 256, 256), (5000, 64, 33, 6), (64, 64, 40, 2), (2048, 64, 40, 3), (2049, 192, 70, 4), (4100, 320, 256, 8)]
+          (700, 640, 200, 12), (1999, 128, 16, 4), (515, 1216, 129, 2), (63, 64, 256, 256), (5000, 64, 33, 6), (64, 64, 40, 2), (2048, 64, 40, 3), (2049, 192, 70, 4), (4100, 320, 256, 8), (65, 192, 129, 8), (512, 448, 65, 5), (513, 448, 65, 5), (300, 704, 256, 8), (2100, 4096, 200, 8), (2600, 7168, 256, 8), (9000, 4096, 8, 2)]
 
 
 @pytest.mark.parametrize("gating", [orc.SOFTMAX, orc.RENORM, orc.SIGMOID])
