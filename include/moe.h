@@ -286,8 +286,8 @@ moe_status moe_combine_backward(const moe_config* cfg, const void* dy, const voi
  * x or W_r comes out as NaN as a rule.
  * dx, dW_r and dbias may be NULL: not computed.  MOE_GRAD_ACCUMULATE: dW_r and dbias are added to what the tensors hold.  x's whole gradient: moe_dispatch_backward
  * with this dx as base.  A slot whose index is outside 0 .. E-1 has no part in anything.  T == 0: dW_r and dbias of zero are written unless they are added to.
- * Limit: d <= 2^20.  Outputs must not overlap inputs.  workspace: moe_route_backward_workspace_size(cfg) bytes, 256-byte aligned; calls that may run at
- * the same time need one each. */
+ * Limit: d <= 2^20.  Outputs must not overlap inputs.  workspace: moe_route_backward_workspace_size(cfg) bytes, 256-byte aligned, and no less for more
+ * tokens of the same shape; calls that may run at the same time need one each. */
 size_t moe_route_backward_workspace_size(const moe_config* cfg);
 moe_status moe_route_backward(const moe_config* cfg, const void* x, const void* W_r, const float* bias, const int32_t* topk_idx, const float* topk_w,
                               const float* d_topk_w, void* dx, void* dW_r, float* dbias, int32_t flags, void* workspace, size_t ws_bytes, void* stream);

@@ -6,6 +6,8 @@
 // Launches: logits in pieces of d (where needed), dz of a token by a wavefront, dx and dW_r (its sum over the tokens in pieces) side by side, the pieces' sum.
 // dz enters the products as two bf16 numbers (16 bits) where the result is bf16, as three (all 24 bits) for dW_r in fp32: results are then off by little more than
 // their own rounding.
+#include <algorithm>
+
 #include "mma_tile.hpp"
 
 namespace moe {
@@ -374,11 +376,12 @@ static_assert(Mid::BK == Many::BK && Low::BK == Many::BK, "one padding");
 int padded(const moe_config& c) { return few_tokens(c) ? (c.E + Few::BK - 1) / Few::BK * Few::BK : (c.E + Many::BK - 1) / Many::BK * Many::BK; }
 bool few_experts(const moe_config& c) { return c.E <= Flat::BM; }
 
+constexpr int kMostPieces = 16;
 template <class S>
 int logit_pieces_of(const moe_config& c) {
     const long long tiles = (long long)((c.T + S::BM - 1) / S::BM) * ((c.E + S::BN - 1) / S::BN), most = c.d / S::BK / 4;
     long long n = tiles > 0 ? 256 * S::PER / tiles : 1;
-    if (n > 16) n = 16;
+    if (n > kMostPieces) n = kMostPieces;
     if (n > most) n = most;
     return n < 1 ? 1 : (int)n;
 }
@@ -406,15 +409,20 @@ int dz_blocks(const moe_config& c) {
     return n < 1024 ? n : 1024;
 }
 
+// The size never falls as T grows, so that a workspace for the most tokens does for fewer: rows as wide as for the few; the logits' tiles, as many as the CUs hold where they are cut
+// into pieces, at their most.  (The pieces of dW_r only grow in number, as its tiles grow.)
 struct RouteSpace {
     size_t part, dz, bias, sums, total;
 };
+template <class S>
+constexpr size_t tiles_of_all_cus() { return (size_t)256 * S::PER * S::BM * S::BN; }
 RouteSpace space(const moe_config& c) {
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += (bytes + 255) / 256 * 256; return o; };
-    const size_t T = c.T, Ep = padded(c);
+    const size_t T = c.T, Ep = (c.E + Few::BK - 1) / Few::BK * Few::BK, full = few_experts(c) ? tiles_of_all_cus<Flat>() : tiles_of_all_cus<Small>();
+    static_assert(tiles_of_all_cus<Slim>() <= tiles_of_all_cus<Small>() && Few::BK % Many::BK == 0, "room for both");
     RouteSpace s;
-    s.part = take((size_t)logit_pieces(c) * T * Ep * sizeof(float));
+    s.part = take(logit_pieces(c) > 0 ? std::max(T * Ep, std::min(kMostPieces * T * Ep, full)) * sizeof(float) : 0);
     s.dz = take(T * kMostParts * Ep * sizeof(uint16_t));
     s.bias = take((size_t)dz_blocks(c) * Ep * sizeof(float));
     s.sums = take(weight_pieces(c) > 1 ? (size_t)weight_pieces(c) * c.E * c.d * sizeof(float) : 0);

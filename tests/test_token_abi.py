@@ -136,6 +136,17 @@ def test_route_backward_refuses(L):
         assert _route(L, bad) == status and moe.route_backward_workspace_size(bad) == 0
 
 
+@pytest.mark.parametrize("d,E,k", [(7168, 256, 8), (4096, 8, 2), (3584, 64, 8), (2048, 128, 8), (64, 40, 3), (64, 65, 1)])
+def test_a_workspace_for_the_most_tokens_does_for_fewer(d, E, k):
+    sizes = {}
+    for T in [*range(1200), *range(1200, 9000, 7), *range(9000, 37000, 61)]:
+        for gating in (0, 1, 2):
+            sizes.setdefault(gating, []).append(moe.route_backward_workspace_size(moe.MoEConfig.of(T, d, 64, E, k, gating)))
+        sizes.setdefault("dispatch", []).append(moe.dispatch_workspace_size(moe.DispatchConfig.of(T, d, k, E)))
+    for of, s in sizes.items():
+        assert s[0] > 0 and all(a <= b for a, b in zip(s, s[1:])), of
+
+
 T, W, K, E = 4, 64, 2, 2
 
 
