@@ -278,6 +278,18 @@ def test_in_place_on_the_residual_and_the_base(moe):
         assert torch.equal(want, got)
 
 
+@pytest.mark.parametrize("k,d", [(1, 8), (3, 64), (12, 136), (3, 264), (11, 1032), (17, 2048)])
+def test_gradients_of_rows_in_place_of_the_rows(moe, k, d):
+    p = Plan(moe, 41, d, k, 8, 6, 1)
+    for weights in (p.d_w, None):
+        for drop in (0.0, 0.3):
+            rows, dw = p.rows.cuda(), full((p.T, p.k), torch.float32)
+            want, want_dw = p.rows.cuda(), full((p.T, p.k), torch.float32)
+            moe.moe_collect_backward(p.cfg, p.add.cuda(), p.rows.cuda(), p.d_row, weights, want, d_topk_w=want_dw, p=drop, rng=p.drng)
+            moe.moe_collect_backward(p.cfg, p.add.cuda(), rows, p.d_row, weights, rows, d_topk_w=dw, p=drop, rng=p.drng)
+            assert torch.equal(rows.view(torch.int16), want.view(torch.int16)) and torch.equal(dw, want_dw)         # bits: rows of no slot hold NaN
+
+
 def test_infinities_stay_where_they_belong(moe):
     """NaN and infinities of a row reach its token alone; what dropout takes out is zero, whatever it was; a weight of a slot without a row is not used."""
     p = Plan(moe, 50, 136, 3, 8, 5, 1, capacity=12, seed=5)
