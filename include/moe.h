@@ -282,7 +282,7 @@ moe_status moe_combine_backward(const moe_config* cfg, const void* dy, const voi
  *   dz = the gate's gradient: MOE_GATE_SOFTMAX p_e (G_e - sum_i p_i d_i) over all experts (p = softmax(z), G_e: d of the slot that chose e, else 0);
  *        MOE_GATE_SOFTMAX_RENORM w_i (d_i - sum_j w_j d_j) over the chosen; MOE_GATE_SIGMOID_NORM the same times 1 - sigmoid(z_i)
  *   dx [T,d] bf16 = dz W_r,  dW_r [E,d] = dz^T x (bf16, or fp32 with MOE_GRAD_F32),  dbias [E] fp32 = sum_t dz
- * z is formed again (fp32 sums; not for MOE_GATE_SOFTMAX_RENORM); dz enters the products as two bf16 numbers (16 bits), for dW_r in fp32 as three (24 bits): an infinity in dz,
+ * z is formed again (fp32 sums; not for MOE_GATE_SOFTMAX_RENORM); dz enters the products as three bf16 numbers, all its 24 bits: an infinity in dz,
  * x or W_r comes out as NaN as a rule.
  * dx, dW_r and dbias may be NULL: not computed.  MOE_GRAD_ACCUMULATE: dW_r and dbias are added to what the tensors hold.  x's whole gradient: moe_dispatch_backward
  * with this dx as base.  A slot whose index is outside 0 .. E-1 has no part in anything.  T == 0: dW_r and dbias of zero are written unless they are added to.

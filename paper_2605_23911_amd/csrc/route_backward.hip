@@ -4,8 +4,8 @@
 //   sigmoid, normalised        the same times 1 - sigmoid(z_i)
 //   dx = dz W_r,  dW_r = dz^T x,  dbias = sum_t dz
 // Launches: logits in pieces of d (where needed), dz of a token by a wavefront, dx and dW_r (its sum over the tokens in pieces) side by side, the pieces' sum.
-// dz enters the products as two bf16 numbers (16 bits) where the result is bf16, as three (all 24 bits) for dW_r in fp32: results are then off by little more than
-// their own rounding.
+// dz enters the products as three bf16 numbers, all its 24 bits: with two, 16 bits, dx of a router whose rows have a large common part, and dW_r where tokens cancel, lose more
+// than their own rounding to bf16.
 #include <algorithm>
 
 #include "mma_tile.hpp"
@@ -24,6 +24,7 @@ typedef Shape<128, 128, 2, 2, 32, 2, 3, 60> Mid;
 typedef Shape<64, 128, 1, 4, 32, 2, 3, 60> Low;
 typedef Shape<64, 64, 2, 2, 64, 2, 2, 60> Few;
 typedef Shape<64, 128, 1, 4, 64, 4, 1, 60> Slim;        // logits of few tokens
+constexpr int kParts = 3;
 
 struct RouteArgs {
     const uint16_t *x, *wr;
@@ -35,10 +36,10 @@ struct RouteArgs {
     float* dbias;
     int f32, add;
     float* part;       // [logit_pieces][T, Ep]
-    uint16_t* dz;      // [T, parts Ep]: dz rounded, of all experts; what that leaves, rounded; and once more
+    uint16_t* dz;      // [T, kParts Ep]: dz rounded, of all experts; what that leaves, rounded; and once more
     float* bias_part;  // [dz_blocks][Ep]
     float* sums;       // [weight_pieces][E, d]
-    int T, d, E, k, Ep, gating, parts;
+    int T, d, E, k, Ep, gating;
     int logit_pieces, weight_pieces, dz_blocks;
 };
 
@@ -192,14 +193,15 @@ __global__ __launch_bounds__(kDzThreads) void route_dz_kernel(RouteArgs a) {
                 for (int q = 0; q < Q; ++q) dz[q] = dz[q] != 0.0f ? dz[q] / (1.0f + expf(z[q])) : 0.0f;
             }
         }
-        uint16_t* to = a.dz + (size_t)t * a.parts * a.Ep + e0;
+        uint16_t* to = a.dz + (size_t)t * kParts * a.Ep + e0;
         float left[Q];
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
             bias_acc[q] += dz[q];
             left[q] = dz[q];
         }
-        for (int h = 0; h < a.parts; ++h) {
+#pragma unroll
+        for (int h = 0; h < kParts; ++h) {
             Halves out;
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
@@ -222,10 +224,10 @@ __global__ __launch_bounds__(kDzThreads) void route_dz_kernel(RouteArgs a) {
     }
 }
 
-// Tile of dx = dz W_r: dz's first part over all experts, then its second.
+// Tile of dx = dz W_r, dz's parts one after the other in each step.
 template <class S>
 __device__ __forceinline__ void dx_tile(const RouteArgs& a, int m0, int n0, char* lds) {
-    const int rows = a.T - m0 < S::BM ? a.T - m0 : S::BM, ld = a.parts * a.Ep;
+    const int rows = a.T - m0 < S::BM ? a.T - m0 : S::BM, ld = kParts * a.Ep;
     const int wave = __builtin_amdgcn_readfirstlane(body_thread() / kWave), lane = body_thread() % kWave;
     typename S::template LoadA<true> la;
     typename S::template LoadB<false> lb;
@@ -287,11 +289,11 @@ __device__ __forceinline__ void bias_group(const RouteArgs& a, int group, float 
 }
 __host__ __device__ inline int bias_groups(const RouteArgs& a) { return a.dbias ? (a.E + kBiasExperts - 1) / kBiasExperts : 0; }
 
-// Tile of dW_r = dz^T x over one piece of the tokens, dz's parts one after the other.
+// Tile of dW_r = dz^T x over one piece of the tokens, dz's parts one after the other in each step.
 template <class S>
 __device__ __forceinline__ void dw_tile(const RouteArgs& a, int piece, int m0, int n0, char* lds) {
     const int all = (a.T + S::BK - 1) / S::BK, each = (all + a.weight_pieces - 1) / a.weight_pieces, s0 = piece * each, s1 = s0 + each < all ? s0 + each : all;
-    const int t0 = s0 * S::BK, tokens = a.T - t0 < (s1 - s0) * S::BK ? a.T - t0 : (s1 - s0) * S::BK, ld = a.parts * a.Ep;
+    const int t0 = s0 * S::BK, tokens = a.T - t0 < (s1 - s0) * S::BK ? a.T - t0 : (s1 - s0) * S::BK, ld = kParts * a.Ep;
     const int wave = __builtin_amdgcn_readfirstlane(body_thread() / kWave), lane = body_thread() % kWave;
     typename S::template LoadA<false> la;
     typename S::template LoadB<false> lb;
@@ -321,31 +323,29 @@ __device__ __forceinline__ void dw_tile(const RouteArgs& a, int piece, int m0, i
 // Both products in one launch, and dbias.  The tiles of dW_r, which are several times as long, come first: one per CU at most (weight_pieces_of), whose other workgroups
 // take tiles of dx; in turn with them a CU gets two (4096 x 256 x 7168: 92 us instead of 74).
 // Two long steps per ring: a step holds all parts of dz and the panel that they are multiplied with, which is loaded once and read from LDS once.  Mixtral-sized weights' gradients
-// have the same layouts (both operands with k across the rows).  4096 tokens x 256 experts of 7168: 75 GFLOP (two parts for dx, three for dW_r) in 70 us (1.07 PFLOP/s; matrix
-// cores 49 % busy at 2.0 GHz, 26 % of the wave cycles waits); step by step, us: dx and dW_r one after the other 95 with two parts, in one launch 86 with three, part by part
-// through all steps 83, one tile of dW_r per CU 74, shared panels 70.  dx alone 41, dW_r alone 56 (with two parts 39).
-template <class S, int PARTS>
-constexpr int products_per_cu() { return 160 * 1024 / Parted<S, PARTS, 2>::kLds < S::PER ? 160 * 1024 / Parted<S, PARTS, 2>::kLds : S::PER; }
-template <class S, int PARTS>
-__global__ __launch_bounds__(S::THREADS, (products_per_cu<S, PARTS>() * S::WAVES / 4)) void route_products_kernel(RouteArgs a) {
-    using Weights = Parted<S, PARTS, 2>;
-    using Rows = Parted<S, 2, 2>;
-    __shared__ __attribute__((aligned(1024))) char lds[Weights::kLds];
-    static_assert(Weights::kLds >= Rows::kLds, "room for both");
+// have the same layouts (both operands with k across the rows).  4096 tokens x 256 experts of 7168: 90 GFLOP in 78 us (1.15 PFLOP/s; with two parts for dx 75 GFLOP in 70).
+// How it got there, with two parts for dx, us: dx and dW_r one after the other 95 (two parts for dW_r, too), in one launch 86, part by part through all steps 83, one tile of dW_r per
+// CU 74, shared panels 70.
+template <class S>
+constexpr int products_per_cu() { return 160 * 1024 / Parted<S, kParts, 2>::kLds < S::PER ? 160 * 1024 / Parted<S, kParts, 2>::kLds : S::PER; }
+template <class S>
+__global__ __launch_bounds__(S::THREADS, (products_per_cu<S>() * S::WAVES / 4)) void route_products_kernel(RouteArgs a) {
+    using P = Parted<S, kParts, 2>;
+    __shared__ __attribute__((aligned(1024))) char lds[P::kLds];
     const int cols = (a.d + S::BN - 1) / S::BN, heads = (a.E + S::BM - 1) / S::BM, blocks = (a.T + S::BM - 1) / S::BM;
     const int weights = a.dwr ? a.weight_pieces * cols * heads : 0, rows = a.dx ? blocks * cols : 0, ids_w = (weights + 7) / 8 * 8, ids_r = (rows + 7) / 8 * 8;
     const int id = blockIdx.x;
     if (id >= ids_w + ids_r) return bias_group<S::THREADS>(a, id - ids_w - ids_r, reinterpret_cast<float(*)[kBiasExperts]>(lds));
     if (id < ids_w) {
         const int t = xcd_tile(id, weights);
-        if (t >= 0) dw_tile<Weights>(a, t / (cols * heads), t % heads * S::BM, t / heads % cols * S::BN, lds);
+        if (t >= 0) dw_tile<P>(a, t / (cols * heads), t % heads * S::BM, t / heads % cols * S::BN, lds);
         return;
     }
     const int t = xcd_tile(id - ids_w, rows);
     if (t < 0) return;
     int m, n;
     patch(t, blocks, cols, m, n);
-    dx_tile<Rows>(a, m * S::BM, n * S::BN, lds);
+    dx_tile<P>(a, m * S::BM, n * S::BN, lds);
 }
 
 // The pieces of dW_r, eight elements per thread, in their order: 6.6 us for four of 256 x 7168 (37 MB), 4 for small ones.
@@ -392,7 +392,6 @@ int logit_pieces(const moe_config& c) {
     if (c.gating == MOE_GATE_SOFTMAX_RENORM) return 0;
     return few_experts(c) ? logit_pieces_of<Flat>(c) : low(c) ? logit_pieces_of<Slim>(c) : logit_pieces_of<Small>(c);
 }
-constexpr int kMostParts = 3;
 // Pieces of the tokens that dW_r is summed over: one tile of it per CU, beside which the CU's other workgroups take tiles of dx; no shorter than four steps.
 template <class S>
 int weight_pieces_of(const moe_config& c) {
@@ -423,7 +422,7 @@ RouteSpace space(const moe_config& c) {
     static_assert(tiles_of_all_cus<Slim>() <= tiles_of_all_cus<Small>() && Few::BK % Many::BK == 0, "room for both");
     RouteSpace s;
     s.part = take(logit_pieces(c) > 0 ? std::max(T * Ep, std::min(kMostPieces * T * Ep, full)) * sizeof(float) : 0);
-    s.dz = take(T * kMostParts * Ep * sizeof(uint16_t));
+    s.dz = take(T * kParts * Ep * sizeof(uint16_t));
     s.bias = take((size_t)dz_blocks(c) * Ep * sizeof(float));
     s.sums = take(weight_pieces(c) > 1 ? (size_t)weight_pieces(c) * c.E * c.d * sizeof(float) : 0);
     s.total = at;
@@ -439,8 +438,7 @@ template <class S>
 void go_products(const RouteArgs& a, hipStream_t s) {
     const long long cols = (a.d + S::BN - 1) / S::BN, weights = a.dwr ? a.weight_pieces * cols * ((a.E + S::BM - 1) / S::BM) : 0, rows = a.dx ? cols * ((a.T + S::BM - 1) / S::BM) : 0;
     const dim3 grid(xcd_grid(weights) + xcd_grid(rows) + bias_groups(a));
-    if (a.parts == 3) hipLaunchKernelGGL((route_products_kernel<S, 3>), grid, dim3(S::THREADS), 0, s, a);
-    else hipLaunchKernelGGL((route_products_kernel<S, 2>), grid, dim3(S::THREADS), 0, s, a);
+    hipLaunchKernelGGL(route_products_kernel<S>, grid, dim3(S::THREADS), 0, s, a);
 }
 
 }  // namespace
@@ -450,7 +448,7 @@ size_t route_backward_workspace_bytes(const moe_config& c) { return space(c).tot
 hipError_t launch_route_backward(const moe_config& c, const RouteGrad& p, hipStream_t s) {
     const RouteSpace at = space(c);
     RouteArgs a{p.x, p.wr, p.bias, p.idx, p.w, p.g, p.dx, p.dwr, p.dbias, p.f32, p.add, (float*)(p.workspace + at.part), (uint16_t*)(p.workspace + at.dz),
-                (float*)(p.workspace + at.bias), (float*)(p.workspace + at.sums), c.T, c.d, c.E, c.k, padded(c), c.gating, p.dwr && p.f32 ? 3 : 2,
+                (float*)(p.workspace + at.bias), (float*)(p.workspace + at.sums), c.T, c.d, c.E, c.k, padded(c), c.gating,
                 logit_pieces(c), c.T > 0 ? weight_pieces(c) : 0, dz_blocks(c)};
     const bool add_nothing = c.T == 0 && p.add;
     if (add_nothing || (!(p.dx && c.T > 0) && !p.dwr && !p.dbias)) return hipSuccess;
