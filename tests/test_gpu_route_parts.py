@@ -87,6 +87,31 @@ def opposite_pairs_case(T, E, d):
     return np.concatenate([idx, idx]), np.concatenate([w, w]), np.concatenate([g, g2]), x, at, dz, dz2, want, bound
 
 
+def single_terms_case(T, d, E, gating):
+    """Token t is one in column t alone (T <= d), so its logits are that column of the router's, and column t of dW_r is its dz.  The logits, and their sums with the bias, are
+    exact.  The softmax over all experts: p is off by 16 u of itself (exp, the sum, the division), and the sum over p_i g_i and the difference by a few u more: 24 u of
+    their sizes; the sigmoid gate as the renormalised one."""
+    rng, idx, w, g = choices(T, E, K, 3)
+    column = rng.integers(-16, 17, size=(T, E)) / 8.0
+    bias = (rng.integers(-8, 9, size=E) / 8).astype(np.float32)
+    z = column + bias
+    if gating != orc.RENORM:
+        w = orc.gate(z, idx.astype(np.int64), gating).astype(np.float32)
+    dz = orc.gate_backward(z, idx, w.astype(np.float64), g.astype(np.float64), gating)
+    if gating == orc.SOFTMAX:
+        p = np.exp(z - z.max(1, keepdims=True))
+        p /= p.sum(1, keepdims=True)
+        G = np.zeros((T, E))
+        np.put_along_axis(G, idx.astype(np.int64), np.abs(g.astype(np.float64)), 1)
+        off = 24 * U * p * (G + 2 * (p * G).sum(1, keepdims=True))
+    else:
+        off = renormalised(idx, w, g, E)[1]
+    x, wr = torch.zeros((T, d), dtype=torch.bfloat16), torch.zeros((E, d), dtype=torch.bfloat16)
+    x[torch.arange(T), torch.arange(T)] = 1
+    wr[:, :T] = torch.from_numpy(column.T.copy()).bfloat16()
+    return idx, w, g, bias, x, wr, dz, off + PARTS * U * (np.abs(dz) + off)
+
+
 @pytest.mark.parametrize("shape", SHAPES, ids=str)
 def test_two_parts_would_be_seen(shape):
     """The bounds admit dz in three parts and not in two."""
@@ -95,6 +120,9 @@ def test_two_parts_would_be_seen(shape):
     assert (np.abs(LEVEL * held(dz, 3).sum(1) - want) <= bound).all() and (np.abs(LEVEL * held(dz, 2).sum(1) - want) > bound).any()
     *_, dz, dz2, want, bound = opposite_pairs_case(T, E, d)
     assert (np.abs(held(dz, 3) + held(dz2, 3) - want) <= bound).all() and (np.abs(held(dz, 2) + held(dz2, 2) - want) > bound).any()
+    for gating in (orc.SOFTMAX, orc.RENORM, orc.SIGMOID):
+        *_, dz, bound = single_terms_case(T, d, E, gating)
+        assert (np.abs(held(dz, 3) - dz) <= bound).all() and (np.abs(held(dz, 2) - dz) > bound).mean() > 0.001
 
 
 def run(moe, x, wr, idx, w, g, gating, dx, dwr, bias=None):
@@ -135,3 +163,17 @@ def test_bf16_weight_gradients_have_all_bits(moe, shape, rows):
     assert (off <= bound).all(), float((off / np.maximum(bound, 1e-300)).max())
     got[:, at] = 0
     assert (got == 0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [True, False], ids=["with dx", "alone"])
+@pytest.mark.parametrize("gating", [orc.SOFTMAX, orc.RENORM, orc.SIGMOID])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_fp32_weight_gradients_have_all_bits(moe, shape, gating, rows):
+    T, d, E = shape
+    idx, w, g, bias, x, wr, dz, bound = single_terms_case(T, d, E, gating)
+    dwr = full((E, d), torch.float32)
+    run(moe, x, wr, idx, w, g, gating, full((T, d)) if rows else None, dwr, bias)
+    off = np.abs(dwr[:, :T].double().cpu().numpy().T - dz)
+    assert (off <= bound).all(), float((off / np.maximum(bound, 1e-300)).max())
+    assert (dwr[:, T:] == 0).all()
