@@ -640,7 +640,7 @@ template <class F>
 void by_launch(CollectArgs a, F&& go) {
     a.whole = a.d > 1024;
     const int each = a.whole ? 1 : kTokenWaves * (a.d <= kNarrow ? kWave / (a.d / 8) : 1);       // tokens per workgroup
-    const int step = (1 << 23) * (each < 64 ? each : 64);
+    const int step = (1 << 23) * (each < 64 ? each : 64) / each * each;      // whole workgroups: a token of two launches would be added to twice where y is the residual
     for (long long t = 0; t < a.T; t += step) {
         a.t0 = (int)t;
         const long long n = a.T - t < step ? a.T - t : step;
@@ -762,3 +762,17 @@ hipError_t launch_dropout(long long n, const uint16_t* x, const uint16_t* residu
 }
 
 }  // namespace moe
+
+// Test hook (exported, not declared in include/moe.h): the launches that T tokens of width d take, on the host.  out[i] = {first token, workgroups}; returns how many there are, or -1 if
+// that is more than `capacity`.
+extern "C" __attribute__((visibility("default"))) int32_t moe_test_token_launches(int32_t T, int32_t d, int32_t capacity, int32_t* out) {
+    moe::CollectArgs a{};
+    a.T = T;
+    a.d = d;
+    int32_t n = 0;
+    moe::by_launch(a, [&](const moe::CollectArgs& b, dim3 grid) {
+        if (n < capacity) out[2 * n] = b.t0, out[2 * n + 1] = (int32_t)grid.x;
+        ++n;
+    });
+    return n <= capacity ? n : -1;
+}

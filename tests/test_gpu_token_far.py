@@ -145,3 +145,25 @@ def test_router_of_many_tokens(moe):
         want_b += dz.sum(0)
         size_b += (dz.abs() * (2**13) * 2.0**-24 + off).sum(0)           # 4096 wavefronts' sums of 733 tokens, then their sum
     assert ((dwr.double() - want_w).abs() <= size_w).all() and ((dbias.double() - want_b).abs() <= size_b).all()
+
+
+def test_in_place_over_several_launches(moe):
+    """More tokens than a launch takes, at the width whose workgroups hold a number of tokens that does not divide it (84 at 24 elements): in place each is added to once.  All values are
+    exact."""
+    T, d = (1 << 29) + 60, 24
+    cfg = moe.DispatchConfig.of(T, d, 1, 1)
+    row = torch.arange(T, dtype=torch.int32, device="cuda").view(T, 1)
+    rows, y = (torch.full((T, d), v, dtype=torch.bfloat16, device="cuda") for v in (0.5, 0.25))
+
+    def check(t, value):
+        for a in range(0, T, 1 << 26):
+            assert bool((t[a:a + (1 << 26)] == value).all()), a
+
+    moe.moe_collect(cfg, rows, row, None, y, residual=y)
+    check(y, 0.75)
+    moe.moe_dispatch_backward(cfg, rows, row, None, y, base=y)
+    check(y, 1.25)
+    dw = torch.empty((T, 1), device="cuda")
+    moe.moe_collect_backward(cfg, y, rows, row, None, rows, d_topk_w=dw)
+    check(rows, 1.25)
+    check(dw, 24 * 0.5 * 1.25)
