@@ -284,6 +284,7 @@ moe_status moe_combine_backward(const moe_config* cfg, const void* dy, const voi
  *   dx [T,d] bf16 = dz W_r,  dW_r [E,d] = dz^T x (bf16, or fp32 with MOE_GRAD_F32),  dbias [E] fp32 = sum_t dz
  * z is formed again (fp32 sums; not for MOE_GATE_SOFTMAX_RENORM); dz enters the products as three bf16 numbers, all its 24 bits: an infinity in dz,
  * x or W_r comes out as NaN as a rule.
+ * Of a token with one large weight dz is off as if every d were off by a few of its own fp32 roundings; weights that add up to one but for (k + 4) 2^-24 count as adding up to one.
  * dx, dW_r and dbias may be NULL: not computed.  MOE_GRAD_ACCUMULATE: dW_r and dbias are added to what the tensors hold.  x's whole gradient: moe_dispatch_backward
  * with this dx as base.  A slot whose index is outside 0 .. E-1 has no part in anything.  T == 0: dW_r and dbias of zero are written unless they are added to.
  * Limit: d <= 2^20.  Outputs must not overlap inputs.  workspace: moe_route_backward_workspace_size(cfg) bytes, 256-byte aligned, and no less for more
