@@ -216,3 +216,25 @@ def test_no_scratch_memory():
         scratch[m[1].decode()] = n[0] if len(n) == 1 else int.from_bytes(n[1:], "big")
     mine = {k: v for k, v in scratch.items() if re.search(r"dispatch_kernel|gather_kernel|scatter_kernel|dropout_kernel|count_chunks|sum_chunks|route_(logits|dz|dx|dw|join)", k)}
     assert len(mine) >= 20 and not any(mine.values()), {k: v for k, v in mine.items() if v} or sorted(mine)
+
+
+KERNELS = ("count_chunks_kernel", "sum_chunks_kernel", "tables_kernel", "dispatch_kernel", "gather_kernel", "scatter_kernel", "narrow_gather_kernel", "narrow_scatter_kernel", "dropout_kernel",
+           "route_logits_kernel", "route_dz_kernel", "route_products_kernel", "route_join_kernel", "route_bias_kernel")
+
+
+def _kernels_scratch():
+    """Mangled name and scratch bytes of every kernel in the library, from the notes that the compiler wrote beside its code."""
+    blob = open(moe.library_path(), "rb").read()
+    number = {0xCC: 1, 0xCD: 2, 0xCE: 4}
+    for m in re.finditer(rb"\xa5\.name(?:\xd9.|\xda..|[\xa0-\xbf])(_Z\w+?)\xbb\.private_segment_fixed_size(.....)", blob, re.S):
+        n = m[2]
+        yield m[1].decode(), n[0] if n[0] < 0x80 else int.from_bytes(n[1:1 + number[n[0]]], "big")
+
+
+def test_no_kernel_of_these_operators_has_scratch_memory():
+    """All of them, by their names: each is in the library, and none of its instances spills."""
+    scratch = list(_kernels_scratch())
+    for name in KERNELS:
+        mine = {k: v for k, v in scratch if f"{len(name)}{name}" in k}      # the length in front: a whole name
+        assert mine, name
+        assert not any(mine.values()), {k: v for k, v in mine.items() if v}
