@@ -443,7 +443,8 @@ __global__ __launch_bounds__(kTokenThreads) void gather_kernel(CollectArgs a) {
     }
 }
 
-// The gradient of collect: rows read (DOT) and their gradients written.  Bound by memory: 4096 x 8 x 7168, 1.0 GB, 191-209 us (4.8-5.2 TB/s, a copy's rate), 1999 x 8 x 3584 31.
+// The gradient of collect: rows read (DOT) and their gradients written.  Bound by memory where there is much: 4096 x 8 x 7168, 1.0 GB, 192-215 us (4.6-5.2 TB/s; a copy 4.9).  1999 x 8 x 3584 with
+// 0.14 GB 31: the slots' numbers and weights fetched one after the other, and five wavefronts per SIMD (84 registers, 78 scalars spilled into lanes of them), 1.6 rounds.
 template <int N, bool DOT, int PAST>
 __global__ __launch_bounds__(kTokenThreads) void scatter_kernel(CollectArgs a) {
     __shared__ float part[kTokenWaves][8];

@@ -15,9 +15,10 @@ namespace moe {
 namespace {
 
 // Tiles of the two products, by the size of one of them, T d E (E in whole tiles of 64), up to 2^31 Low, from there to 2^32 Mid, above that Many; up to 64 tokens Few.
-// Smaller tiles fill the CUs with fewer pieces to join and leave a shorter last round; larger ones read less from the caches.  dz, products and join, us, Low / Mid / Many:
-// 256 experts of 7168, 768 tokens 27.0 / 34.8 / 33.8, 1024 33.0 / 35.4 / 35.7, 2048 55.2 / 50.9 / 55.3, 4096 99 / 80.9 / 75.9; 256 of 2048, 2048 28.5 / 29.6 / 32.0, 8192 64.4 / 58.7 / 60.4;
-// 128 of 2048, 2048 22.4 / 26.3 / 28.2, 8192 41.7 / 42.8 / 47.0; 64 of 3584, 4096 28.8 / 31.4 / 29.9; 8 of 4096, 2048 18.8 / 20.7 / 20.4, 8192 37.0 / 43.3 / 37.7, 16384 79.7 / 91.9 / 74.1:
+// Smaller tiles fill the CUs with fewer pieces to join and leave a shorter last round; larger ones read less from the caches.  dz, products and join, us, Low / Mid / Many, of the
+// renormalised gate, two sets of inputs in turn:
+// 256 experts of 7168, 768 tokens 27.6 / 36.5 / 35.1, 1024 32.8 / 36.5 / 36.8, 2048 54.6 / 53.2 / 52.3, 4096 117 / 97.3 / 83.1; 256 of 2048, 2048 27.7 / 29.2 / 33.3, 8192 67.8 / 59.4 / 64.7;
+// 128 of 2048, 2048 22.5 / 23.9 / 24.3, 8192 43.6 / 45.4 / 49.9; 64 of 3584, 4096 29.3 / 31.7 / 31.0; 8 of 4096, 2048 19.1 / 19.9 / 20.1, 8192 48.3 / 53.6 / 43.8, 16384 93.4 / 108 / 82.9:
 // up to 64 experts fill no more than half of Mid's tiles of dW_r, and it is left out.
 typedef Pair Many;
 typedef Shape<128, 128, 2, 2, 32, 2, 3, 60> Mid;
@@ -43,8 +44,9 @@ struct RouteArgs {
     int logit_pieces, weight_pieces, dz_blocks;
 };
 
-// Tile: BM tokens x BN experts, one piece of d.  4096 tokens x 256 experts of 7168: 22.5 us (0.67 PFLOP/s; x, 59 MB, comes from memory, matrix cores 23 % busy) in four pieces (2: 30, 3: 24.5,
-// 6: 28, 8: 30) with Small (Tall 23, Half 24.5, Wide 28, Pair 32; 64 x 256, 128 x 256 and 128 x 128 of four wavefronts 23-24).  Few experts take Flat.
+// Tile: BM tokens x BN experts, one piece of d.  4096 tokens x 256 experts of 7168: 25-30 us (0.50-0.60 PFLOP/s) with two sets of inputs in turn, x (59 MB) coming from memory; 22.4-24.4
+// (0.62-0.67 PFLOP/s, matrix cores 22-24 % busy) with one set again and again, x in the caches.  Compared on such a set: four pieces 22.5, 2: 30, 3: 24.5, 6: 28, 8: 30; Small 22.5, Tall 23,
+// Half 24.5, Wide 28, Pair 32, 64 x 256, 128 x 256 and 128 x 128 of four wavefronts 23-24.  Few experts take Flat.
 // Products up to 2^31 take Slim, us, Small / Slim (Flat): 256 of 7168, 200 tokens 8.4 / 7.3 (7.0), 512 11.2 / 10.0 (10.6), 1024 11.4 / 10.4 (12.3), 4096 21.8 / 24.4; 128 of 2048, 4096 12.3 / 8.4 (10.9).
 template <class S>
 __global__ __launch_bounds__(S::THREADS, S::SIMD_WAVES) void route_logits_kernel(RouteArgs a) {
@@ -125,7 +127,7 @@ __device__ __forceinline__ auto part_of(const V& v, int q) {
 // (sum of the others' w g) instead, which nothing cancels in, so that dz is off as if every g were off by a few of its own roundings.  (With g - c for all, dz of an expert
 // with a weight of 1 - 10^-6 was off by several percent.)  The others' sum and 1 - w differ by the weights' own rounding where they add up to one; a slot without an expert has its
 // share of the rest.
-// Bound by latency: one load of the pieces of the logits, the exchanges between lanes, one store; 4.4 us for a token, 8.7 for 4096 x 256.
+// Bound by latency: one load of the pieces of the logits, the exchanges between lanes, one store; 4.5 us for a token, 9 for 4096 x 256.
 template <int Q>
 __global__ __launch_bounds__(kDzThreads) void route_dz_kernel(RouteArgs a) {
     typedef typename Lot<Q>::f Floats;
@@ -366,7 +368,8 @@ __device__ __forceinline__ void dw_tile(const RouteArgs& a, int piece, int m0, i
 // Both products in one launch, and dbias.  The tiles of dW_r, which are several times as long, come first: one per CU at most (weight_pieces_of), whose other workgroups
 // take tiles of dx; in turn with them a CU gets two (4096 x 256 x 7168: 92 us instead of 74).
 // Two long steps per ring: a step holds all parts of dz and the panel that they are multiplied with, which is loaded once and read from LDS once.  Mixtral-sized weights' gradients
-// have the same layouts (both operands with k across the rows).  4096 tokens x 256 experts of 7168: 90 GFLOP in 78 us (1.15 PFLOP/s; with two parts for dx 75 GFLOP in 70).
+// have the same layouts (both operands with k across the rows).  4096 tokens x 256 experts of 7168: 90 GFLOP in 78 us (1.15 PFLOP/s; matrix
+// cores 56 % busy at 1.94 GHz, 23 % of the wave cycles waits; with two parts for dx 75 GFLOP in 70).
 // How it got there, with two parts for dx, us: dx and dW_r one after the other 95 (two parts for dW_r, too), in one launch 86, part by part through all steps 83, one tile of dW_r per
 // CU 74, shared panels 70.
 template <class S>
@@ -391,7 +394,7 @@ __global__ __launch_bounds__(S::THREADS, (products_per_cu<S>() * S::WAVES / 4)) 
     dx_tile<P>(a, m * S::BM, n * S::BN, lds);
 }
 
-// The pieces of dW_r, eight elements per thread, in their order: 6.6 us for four of 256 x 7168 (37 MB), 4 for small ones.
+// The pieces of dW_r, eight elements per thread, in their order: 7 us for four of 256 x 7168 (37 MB), 4 for small ones.
 __global__ __launch_bounds__(256) void route_join_kernel(RouteArgs a) {
     const size_t at = ((size_t)blockIdx.x * 256 + threadIdx.x) * 8, n = (size_t)a.E * a.d;
     if (at >= n) return;

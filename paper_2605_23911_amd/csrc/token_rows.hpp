@@ -2,7 +2,8 @@
 // <v[t], row(t,i)> where they are asked for, over slots of which some have no row.  And dropout, whose mask is a function of (seed, offset, element).
 //
 // A row is read and written through a buffer descriptor of its own, which is empty (range 0) where the slot has no row: loads from it give zeros, stores to it
-// are dropped, neither goes to memory, and no branch stands between the loads of a token's rows.  The hardware also ends them at the row's last element.
+// are dropped, neither goes to memory, and no branch stands between the loads of a token's rows.  The hardware also ends them at the row's last element.  What comes before them does wait: row numbers
+// and weights are fetched slot by slot, each behind the one before (in dispatch's gradient 7 waits for two slots, 19 for eight).
 #pragma once
 
 #include "moe_internal.hpp"
